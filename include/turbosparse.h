@@ -264,6 +264,144 @@ ts_status ts_moe_dense(const float *x, const void *w_router, const void *w_gate,
                        int n_experts, int top_k, float *out, int32_t *topk_idx, float *topk_w,
                        void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * The MoE layer on any number of tokens, its gradients and its 8-bit form.
+ *
+ * T tokens take K of E experts each (a "pair" is one token's slot, p = t * K
+ * + k).  The pairs sorted by expert are the layer's rows: expert e's rows are
+ * offsets[e] .. offsets[e + 1) - 1.  The layer is
+ *     ts_moe_route        logits -> chosen experts, their weights, row maps
+ *     ts_grouped_drelu    rows of x (gathered) -> Combined, per expert
+ *     ts_grouped_mm       Combined W_down
+ *     ts_moe_combine      the tokens' weighted sums of their rows
+ * and each has its gradients; ts_fp8_* are the products with 8-bit operands.
+ * The conventions above hold, but for these:
+ *   - Row types: activations are TS_BF16 or TS_F32, as stated per argument;
+ *     products accumulate in fp32 and round once.
+ *   - Limits: tokens, rows and pairs <= 2^23, each may be 0 (nothing is
+ *     enqueued and device pointers may be NULL, except that gradients of
+ *     weights and offsets are written); n_experts, n_groups <= 64; n, k and
+ *     hidden <= 131072, multiples of 8 (TS_BF16), 4 (TS_F32) or 16 (fp8); one
+ *     group's weight matrix below 4 GB.
+ *   - `offsets` is device int32 [n_groups + 1], ascending, within [0, rows];
+ *     NULL with n_groups == 1: the group holds all rows.  Values out of range
+ *     or order are clamped (no access leaves the arrays; which rows are
+ *     computed is unspecified).  Rows before offsets[0] or from
+ *     offsets[n_groups] on are not read, and outputs there stay as they were.
+ *   - `row_src` is device int32 [rows] or NULL: row r reads x[row_src[r]]
+ *     (x has src_rows rows), or x[r].  Entries are clamped into range.
+ *   - Non-finite values stay in the rows (and columns) that hold them, as the
+ *     formulas have it; dReLU takes a NaN projection as closed.
+ *   - No state: results depend on the arguments only, and are the same bits on
+ *     every run.  Outputs must not overlap inputs.
+ */
+
+/* Workspace bytes of ts_moe_route / ts_moe_group (0 if out of range). */
+size_t ts_moe_route_workspace_bytes(int tokens, int n_experts, int top_k);
+
+/*
+ * Routing: per token the top_k largest logits (ties: the lower expert; NaN
+ * counts as -inf; -0 equals 0) in rank order, and the softmax over them.  An
+ * expert with logit -inf has weight 0; where every chosen logit is -inf all
+ * weights are 0; logits of +inf share the weight.
+ *   logits [tokens][n_experts] fp32; topk_idx, topk_w [tokens][top_k];
+ *   offsets [n_experts + 1], row_token [tokens * top_k] (token of a row),
+ *   pair_row [tokens][top_k] (row of a pair): all three or none (then no
+ *   workspace is needed).  Rows of an expert are in pair order.
+ */
+ts_status ts_moe_route(const float *logits, int tokens, int n_experts, int top_k, int32_t *topk_idx, float *topk_w,
+                       int32_t *offsets, int32_t *row_token, int32_t *pair_row, void *ws, size_t ws_bytes,
+                       void *stream);
+
+/* The row maps of a given choice.  A pair whose expert is outside [0,
+ * n_experts) gets no row (pair_row -1); row_token entries from offsets[E] on
+ * stay as they were. */
+ts_status ts_moe_group(const int32_t *topk_idx, int tokens, int n_experts, int top_k, int32_t *offsets,
+                       int32_t *row_token, int32_t *pair_row, void *ws, size_t ws_bytes, void *stream);
+
+/* Gradient of topk_w with respect to the logits: d_logits[t][idx_k] = w_k
+ * (d_w_k - sum_j w_j d_w_j), 0 at the experts not chosen; all of d_logits
+ * [tokens][n_experts] is written. */
+ts_status ts_moe_route_grad(const int32_t *topk_idx, const float *topk_w, const float *d_w, int tokens, int n_experts,
+                            int top_k, float *d_logits, void *stream);
+
+/*
+ * Product grouped by expert: out[r][j] = sum_i x[src(r)][i] w[g][j][i] for
+ * the rows r of group g.
+ *   x [src_rows][k], w [n_groups][n][k] (w_kn 0, as w_gate, or the gradient
+ *   through w_down_t) or [n_groups][k][n] (w_kn 1, as w_down_t, or the
+ *   gradient through w_gate), both `dtype`; out [rows][n] `odtype`.
+ *   x2, w2 (both or neither): a second pair of the same shapes, whose product
+ *   is added before the one rounding (the gradient of x through gate and up).
+ */
+ts_status ts_grouped_mm(const void *x, const void *w, const void *x2, const void *w2, ts_dtype dtype, int w_kn,
+                        const int32_t *row_src, const int32_t *offsets, int rows, int src_rows, int n_groups, int n,
+                        int k, void *out, ts_dtype odtype, void *stream);
+
+/*
+ * Gate and up products with dReLU: c[r] = max(0, gate) * max(0, up), gate =
+ * x w_gate^T, up = x w_up^T ([n_groups][n][k] each), one pass over x.  gate,
+ * up: NULL, or both [rows][n] `odtype`: the projections, for ts_drelu_grad.
+ */
+ts_status ts_grouped_drelu(const void *x, const void *w_gate, const void *w_up, ts_dtype dtype,
+                           const int32_t *row_src, const int32_t *offsets, int rows, int src_rows, int n_groups,
+                           int n, int k, void *c, void *gate, void *up, ts_dtype odtype, void *stream);
+
+/* Gradient of dReLU: d_gate = d_c * up, d_up = d_c * gate where gate > 0 and
+ * up > 0, otherwise 0.  All [rows][n] `dtype`. */
+ts_status ts_drelu_grad(const void *gate, const void *up, const void *d_c, ts_dtype dtype, int rows, int n,
+                        void *d_gate, void *d_up, void *stream);
+
+/*
+ * Gradient of a grouped product's weights: d_w[g][j][i] = sum over the rows r
+ * of group g of d_y[r][j] x[src(r)][i], zeros for a group without rows.
+ *   d_y [rows][n], x [src_rows][k] `dtype`; d_w [n_groups][n][k] `odtype`.
+ *   (w_kn matrices: exchange d_y and x where x is not gathered.)
+ */
+ts_status ts_grouped_mm_dw(const void *d_y, const void *x, ts_dtype dtype, const int32_t *row_src,
+                           const int32_t *offsets, int rows, int src_rows, int n_groups, int n, int k, void *d_w,
+                           ts_dtype odtype, void *stream);
+
+/*
+ * 8-bit floating point (OCP e4m3), a scale for each block of 128: codes q =
+ * e4m3(448 x / amax), scale = amax / 448, amax = max(2^-100, |x| over the
+ * block).  A block that holds an infinity gets NaN codes, a NaN makes its own
+ * code NaN.
+ * ts_fp8_quant: rows, blocks along a row: x [rows][cols] `dtype`, q
+ * [rows][cols], scale [rows][ceil(cols / 128)].
+ * ts_fp8_quant_weights: tiles of 128 x 128: w [n_groups][n][k] (w_kn 0) or
+ * [n_groups][k][n] (w_kn 1), q [n_groups][n][k], scale [n_groups][ceil(n /
+ * 128)][ceil(k / 128)].
+ */
+ts_status ts_fp8_quant(const void *x, ts_dtype dtype, int rows, int cols, void *q, float *scale, void *stream);
+ts_status ts_fp8_quant_weights(const void *w, ts_dtype dtype, int w_kn, int n_groups, int n, int k, void *q,
+                               float *scale, void *stream);
+
+/* ts_grouped_mm and ts_grouped_drelu on quantised rows and weights
+ * ([n_groups][n][k]): out[r][j] = sum over blocks b of x_scale[src(r)][b]
+ * w_scale[g][j / 128][b] sum over i in b of x[src(r)][i] w[g][j][i]. */
+ts_status ts_fp8_mm(const void *x, const float *x_scale, const void *w, const float *w_scale, const int32_t *row_src,
+                    const int32_t *offsets, int rows, int src_rows, int n_groups, int n, int k, void *out,
+                    ts_dtype odtype, void *stream);
+ts_status ts_fp8_drelu(const void *x, const float *x_scale, const void *w_gate, const float *gate_scale,
+                       const void *w_up, const float *up_scale, const int32_t *row_src, const int32_t *offsets,
+                       int rows, int src_rows, int n_groups, int n, int k, void *c, ts_dtype odtype, void *stream);
+
+/*
+ * Combine: out[t] = sum_k w[t][k] y[pair_row[t][k]]; w NULL: weights of one
+ * (the sum of the rows' gradients into their token's).  Pairs whose row is
+ * outside [0, rows) are left out; a token without rows gets zeros.
+ *   y [rows][hidden] `ydtype`; out [tokens][hidden] `odtype`.
+ * Its gradients: d_y[pair_row[t][k]] = w[t][k] d_out[t] (rows that no pair
+ * names stay as they were), d_w[t][k] = <d_out[t], y[pair_row[t][k]]> (0 for a
+ * pair without a row).  No two pairs may name one row.
+ */
+ts_status ts_moe_combine(const void *y, ts_dtype ydtype, const int32_t *pair_row, const float *w, int tokens,
+                         int top_k, int hidden, int rows, void *out, ts_dtype odtype, void *stream);
+ts_status ts_moe_combine_grad(const void *d_out, ts_dtype odtype, const void *y, ts_dtype ydtype,
+                              const int32_t *pair_row, const float *w, int tokens, int top_k, int hidden, int rows,
+                              void *d_y, float *d_w, void *stream);
+
 /* Human-readable name of a status code (static string). */
 const char *ts_status_str(ts_status s);
 
@@ -283,7 +421,10 @@ const char *ts_version(void);
  * synchronises on the recorded events and returns, for the kernel named
  * `kernel` ("ffn_main", "ffn_reduce", "ffn_gate_up", "ffn_down",
  * "ffn_topk_select", "ffn_topk_down", "ffn_given", "given_counts", "ffn_stats", "ffn_union",
- * "moe_router", "batch_prep", "batch_gate_up", "batch_down",
+ * "moe_router", "moe_route", "moe_place", "moe_route_grad", "grouped_mm",
+ * "grouped_drelu", "drelu_grad", "grouped_mm_dw", "fp8_quant",
+ * "fp8_quant_weights", "fp8_mm", "fp8_drelu", "moe_combine",
+ * "moe_combine_grad", "batch_prep", "batch_gate_up", "batch_down",
  * "batch_reduce", "batch_stats", "batch_union", "probe_read",
  * "probe_copy"), the number of launches and their summed duration in
  * milliseconds since the last ts_prof_reset.  Returns TS_ERR_HIP on a

@@ -24,7 +24,10 @@ EXPORTED = ["ts_ffn_workspace_bytes", "ts_ffn_sparse", "ts_ffn_sparse_act", "ts_
             "ts_ffn_given_workspace_bytes", "ts_ffn_sparse_noalloc",
             "ts_ffn_sparse_given", "ts_moe_workspace_bytes", "ts_moe_sparse",
             "ts_moe_dense", "ts_status_str", "ts_last_error", "ts_version", "ts_prof_enable", "ts_prof_reset",
-            "ts_prof_read", "ts_probe_read", "ts_probe_copy", "ts_tune_set"]
+            "ts_prof_read", "ts_probe_read", "ts_probe_copy", "ts_tune_set",
+            "ts_moe_route_workspace_bytes", "ts_moe_route", "ts_moe_group", "ts_moe_route_grad", "ts_grouped_mm",
+            "ts_grouped_drelu", "ts_drelu_grad", "ts_grouped_mm_dw", "ts_fp8_quant", "ts_fp8_quant_weights",
+            "ts_fp8_mm", "ts_fp8_drelu", "ts_moe_combine", "ts_moe_combine_grad"]
 
 
 class TSError(RuntimeError):
@@ -67,6 +70,25 @@ def _load() -> ctypes.CDLL:
     lib.ts_moe_sparse.restype = st
     lib.ts_moe_dense.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, i, i, vp, vp, vp, vp, sz, vp]
     lib.ts_moe_dense.restype = st
+    lib.ts_moe_route_workspace_bytes.argtypes = [i, i, i]
+    lib.ts_moe_route_workspace_bytes.restype = sz
+    for name, args in (
+            ("ts_moe_route", [vp, i, i, i, vp, vp, vp, vp, vp, vp, sz, vp]),
+            ("ts_moe_group", [vp, i, i, i, vp, vp, vp, vp, sz, vp]),
+            ("ts_moe_route_grad", [vp, vp, vp, i, i, i, vp, vp]),
+            ("ts_grouped_mm", [vp, vp, vp, vp, i, i, vp, vp, i, i, i, i, i, vp, i, vp]),
+            ("ts_grouped_drelu", [vp, vp, vp, i, vp, vp, i, i, i, i, i, vp, vp, vp, i, vp]),
+            ("ts_drelu_grad", [vp, vp, vp, i, i, i, vp, vp, vp]),
+            ("ts_grouped_mm_dw", [vp, vp, i, vp, vp, i, i, i, i, i, vp, i, vp]),
+            ("ts_fp8_quant", [vp, i, i, i, vp, vp, vp]),
+            ("ts_fp8_quant_weights", [vp, i, i, i, i, i, vp, vp, vp]),
+            ("ts_fp8_mm", [vp, vp, vp, vp, vp, vp, i, i, i, i, i, vp, i, vp]),
+            ("ts_fp8_drelu", [vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, vp, i, vp]),
+            ("ts_moe_combine", [vp, i, vp, vp, i, i, i, i, vp, i, vp]),
+            ("ts_moe_combine_grad", [vp, i, vp, i, vp, vp, i, i, i, i, vp, vp, vp])):
+        f = getattr(lib, name)
+        f.argtypes = args
+        f.restype = st
     lib.ts_status_str.argtypes = [st]
     lib.ts_status_str.restype = ctypes.c_char_p
     lib.ts_last_error.argtypes = []
@@ -398,6 +420,332 @@ def moe_sparse(x, w_router, w_gate, w_up, w_down_t, top_k: int, out=None, stats:
 
 def moe_dense(x, w_router, w_gate, w_up, w_down_t, top_k: int, out=None, ws=None, stream=None):
     return moe_sparse(x, w_router, w_gate, w_up, w_down_t, top_k, out=out, ws=ws, stream=stream, dense=True)
+
+
+# ---------------------------------------------------------------------------
+# The MoE layer on any number of tokens, its gradients, its 8-bit form.
+
+_i32, _e4m3 = torch.int32, torch.float8_e4m3fn
+
+
+def _need(t, name, dtype, shape):
+    """Raises unless t has this dtype and shape (None: any extent)."""
+    dts = dtype if isinstance(dtype, tuple) else (dtype,)
+    if t.dtype not in dts:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dts)}, got {t.dtype}")
+    if len(t.shape) != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
+        want = "".join(f"[{'*' if w is None else w}]" for w in shape)
+        raise ValueError(f"{name} must be {want}, got {tuple(t.shape)}")
+
+
+def _here(stream, *ts):
+    """All tensors contiguous on the current device; the stream to launch on."""
+    d = _cur_device() if _cur_device is not None and torch.cuda.is_initialized() else None
+    for t in ts:
+        if t is None:
+            continue
+        if not t.is_cuda or not t.is_contiguous():
+            raise ValueError("tensors must be contiguous device tensors")
+        if d is None:
+            d = torch.cuda.current_device()
+        if t.get_device() != d:
+            raise ValueError(f"tensor on {t.device}, current device cuda:{d}")
+    if stream is not None and stream.device.index != d:
+        raise ValueError(f"stream on {stream.device}, current device cuda:{d}")
+    return _stream(stream)
+
+
+def _new(out, name, shape, dtype, device):
+    """The caller's output, checked, or a new one."""
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _need(out, name, dtype, shape)
+    return out
+
+
+def moe_route_workspace_bytes(tokens: int, n_experts: int, top_k: int) -> int:
+    return int(lib.ts_moe_route_workspace_bytes(tokens, n_experts, top_k))
+
+
+def _maps(T, E, K, dev):
+    return (torch.empty(E + 1, dtype=_i32, device=dev), torch.empty(T * K, dtype=_i32, device=dev),
+            torch.empty(T, K, dtype=_i32, device=dev))
+
+
+def moe_route(logits, top_k: int, maps: bool = True, ws=None, stream=None):
+    """ts_moe_route.  logits [T][E] f32.  Returns topk_idx, topk_w [T][K] and,
+    with maps, offsets [E + 1], row_token [T K], pair_row [T][K]."""
+    _need(logits, "logits", _f32, (None, None))
+    st = _here(stream, logits, ws)
+    T, E = logits.shape
+    K = int(top_k)
+    if not 1 <= K <= E:
+        raise ValueError(f"top_k must be in 1..{E}, got {K}")
+    dev = logits.device
+    idx, w = torch.empty(T, K, dtype=_i32, device=dev), torch.empty(T, K, dtype=_f32, device=dev)
+    m = _maps(T, E, K, dev) if maps else (None, None, None)
+    if maps:
+        ws = _workspace(moe_route_workspace_bytes, dev, ws, T, E, K)
+    code = lib.ts_moe_route(_ptr(logits), T, E, K, _ptr(idx), _ptr(w), _ptr(m[0]), _ptr(m[1]), _ptr(m[2]), _ptr(ws),
+                            _nbytes(ws) if ws is not None else 0, st)
+    if code:
+        _check(code, "ts_moe_route")
+    return (idx, w, *m) if maps else (idx, w)
+
+
+def moe_group(topk_idx, n_experts: int, ws=None, stream=None):
+    """ts_moe_group.  topk_idx [T][K] int32.  Returns offsets [E + 1],
+    row_token [T K] (entries from offsets[E] on unspecified), pair_row [T][K]."""
+    _need(topk_idx, "topk_idx", _i32, (None, None))
+    st = _here(stream, topk_idx, ws)
+    T, K = topk_idx.shape
+    E = int(n_experts)
+    if E < 1:
+        raise ValueError(f"n_experts must be positive, got {E}")
+    m = _maps(T, E, K, topk_idx.device)
+    ws = _workspace(moe_route_workspace_bytes, topk_idx.device, ws, T, E, K)
+    code = lib.ts_moe_group(_ptr(topk_idx), T, E, K, _ptr(m[0]), _ptr(m[1]), _ptr(m[2]), _ptr(ws), _nbytes(ws), st)
+    if code:
+        _check(code, "ts_moe_group")
+    return m
+
+
+def moe_route_grad(topk_idx, topk_w, d_w, n_experts: int, out=None, stream=None):
+    """ts_moe_route_grad: d_logits [T][E] from d_w [T][K] (the gradient of topk_w)."""
+    _need(topk_idx, "topk_idx", _i32, (None, None))
+    T, K = topk_idx.shape
+    E = int(n_experts)
+    if E < 1:
+        raise ValueError(f"n_experts must be positive, got {E}")
+    _need(topk_w, "topk_w", _f32, (T, K))
+    _need(d_w, "d_w", _f32, (T, K))
+    st = _here(stream, topk_idx, topk_w, d_w, out)
+    out = _new(out, "out", (T, E), _f32, topk_idx.device)
+    code = lib.ts_moe_route_grad(_ptr(topk_idx), _ptr(topk_w), _ptr(d_w), T, E, K, _ptr(out), st)
+    if code:
+        _check(code, "ts_moe_route_grad")
+    return out
+
+
+def _rows_of(x, offsets, row_src, G):
+    """Rows of a grouped product; checks offsets [G + 1] and row_src."""
+    if offsets is not None:
+        _need(offsets, "offsets", _i32, (G + 1,))
+    elif G != 1:
+        raise ValueError(f"{G} groups need offsets")
+    if row_src is not None:
+        _need(row_src, "row_src", _i32, (None,))
+        if x.shape[0] == 0 and row_src.shape[0] > 0:
+            raise ValueError("row_src names rows of an empty x")
+        return row_src.shape[0]
+    return x.shape[0]
+
+
+def _odtype(out, out_dtype, default):
+    dt = out_dtype if out_dtype is not None else (out.dtype if out is not None else default)
+    return dt, wdtype_of_rows(dt)
+
+
+def wdtype_of_rows(dt) -> int:
+    if dt is _f32:
+        return TS_F32
+    if dt is _bf16:
+        return TS_BF16
+    raise TypeError(f"rows must be float32 or bfloat16, got {dt}")
+
+
+def grouped_mm(x, w, offsets=None, row_src=None, x2=None, w2=None, w_kn: bool = False, out=None, out_dtype=None,
+               stream=None):
+    """ts_grouped_mm.  x [S][k]; w [G][n][k], or [G][k][n] with w_kn; bf16 or
+    f32, one dtype; x2, w2: a second product added to the first.  Returns out
+    [rows][n] (out_dtype: x's unless given), rows = len(row_src) or S; rows
+    outside the groups are not written."""
+    _need(x, "x", (_f32, _bf16), (None, None))
+    S, k = x.shape
+    _need(w, "w", x.dtype, (None, None, None))
+    G, n = w.shape[0], w.shape[2] if w_kn else w.shape[1]
+    _need(w, "w", x.dtype, (None, k, n) if w_kn else (None, n, k))
+    if (x2 is None) != (w2 is None):
+        raise ValueError("x2 and w2 go together")
+    if x2 is not None:
+        _need(x2, "x2", x.dtype, (S, k))
+        _need(w2, "w2", x.dtype, tuple(w.shape))
+    R = _rows_of(x, offsets, row_src, G)
+    odt, od = _odtype(out, out_dtype, x.dtype)
+    st = _here(stream, x, w, x2, w2, offsets, row_src, out)
+    out = _new(out, "out", (R, n), odt, x.device)
+    code = lib.ts_grouped_mm(_ptr(x), _ptr(w), _ptr(x2), _ptr(w2), wdtype_of_rows(x.dtype), int(bool(w_kn)),
+                             _ptr(row_src), _ptr(offsets), R, S, G, n, k, _ptr(out), od, st)
+    if code:
+        _check(code, "ts_grouped_mm")
+    return out
+
+
+def grouped_drelu(x, w_gate, w_up, offsets=None, row_src=None, keep: bool = False, out=None, out_dtype=None,
+                  stream=None):
+    """ts_grouped_drelu.  x [S][k]; w_gate, w_up [G][n][k].  Returns c
+    [rows][n], or (c, gate, up) with keep."""
+    _need(x, "x", (_f32, _bf16), (None, None))
+    S, k = x.shape
+    _need(w_gate, "w_gate", x.dtype, (None, None, k))
+    _need(w_up, "w_up", x.dtype, tuple(w_gate.shape))
+    G, n = w_gate.shape[:2]
+    R = _rows_of(x, offsets, row_src, G)
+    odt, od = _odtype(out, out_dtype, x.dtype)
+    st = _here(stream, x, w_gate, w_up, offsets, row_src, out)
+    out = _new(out, "out", (R, n), odt, x.device)
+    gate, up = (torch.empty_like(out), torch.empty_like(out)) if keep else (None, None)
+    code = lib.ts_grouped_drelu(_ptr(x), _ptr(w_gate), _ptr(w_up), wdtype_of_rows(x.dtype), _ptr(row_src),
+                                _ptr(offsets), R, S, G, n, k, _ptr(out), _ptr(gate), _ptr(up), od, st)
+    if code:
+        _check(code, "ts_grouped_drelu")
+    return (out, gate, up) if keep else out
+
+
+def drelu_grad(gate, up, d_c, stream=None):
+    """ts_drelu_grad: (d_gate, d_up) of c = max(0, gate) * max(0, up)."""
+    _need(gate, "gate", (_f32, _bf16), (None, None))
+    _need(up, "up", gate.dtype, tuple(gate.shape))
+    _need(d_c, "d_c", gate.dtype, tuple(gate.shape))
+    st = _here(stream, gate, up, d_c)
+    dg, du = torch.empty_like(gate), torch.empty_like(gate)
+    code = lib.ts_drelu_grad(_ptr(gate), _ptr(up), _ptr(d_c), wdtype_of_rows(gate.dtype), gate.shape[0],
+                             gate.shape[1], _ptr(dg), _ptr(du), st)
+    if code:
+        _check(code, "ts_drelu_grad")
+    return dg, du
+
+
+def grouped_mm_dw(d_y, x, offsets=None, row_src=None, out=None, out_dtype=None, stream=None):
+    """ts_grouped_mm_dw.  d_y [rows][n], x [S][k] -> d_w [G][n][k] (f32 unless
+    out_dtype or out says otherwise), G = len(offsets) - 1."""
+    _need(x, "x", (_f32, _bf16), (None, None))
+    _need(d_y, "d_y", x.dtype, (None, None))
+    if offsets is not None:
+        _need(offsets, "offsets", _i32, (None,))
+    G = 1 if offsets is None else offsets.shape[0] - 1
+    R = _rows_of(x, offsets, row_src, G)
+    if d_y.shape[0] != R:
+        raise ValueError(f"d_y has {d_y.shape[0]} rows, the product {R}")
+    (S, k), n = x.shape, d_y.shape[1]
+    odt, od = _odtype(out, out_dtype, _f32)
+    st = _here(stream, d_y, x, offsets, row_src, out)
+    out = _new(out, "out", (G, n, k), odt, x.device)
+    code = lib.ts_grouped_mm_dw(_ptr(d_y), _ptr(x), wdtype_of_rows(x.dtype), _ptr(row_src), _ptr(offsets), R, S, G,
+                                n, k, _ptr(out), od, st)
+    if code:
+        _check(code, "ts_grouped_mm_dw")
+    return out
+
+
+def _nblk(n):
+    return (n + 127) // 128
+
+
+def fp8_quant(x, stream=None):
+    """ts_fp8_quant.  x [rows][cols] bf16 / f32 -> (codes float8_e4m3fn
+    [rows][cols], scale f32 [rows][ceil(cols / 128)])."""
+    _need(x, "x", (_f32, _bf16), (None, None))
+    st = _here(stream, x)
+    R, C = x.shape
+    q = torch.empty(R, C, dtype=_e4m3, device=x.device)
+    s = torch.empty(R, _nblk(C), dtype=_f32, device=x.device)
+    code = lib.ts_fp8_quant(_ptr(x), wdtype_of_rows(x.dtype), R, C, _ptr(q), _ptr(s), st)
+    if code:
+        _check(code, "ts_fp8_quant")
+    return q, s
+
+
+def fp8_quant_weights(w, w_kn: bool = False, stream=None):
+    """ts_fp8_quant_weights.  w [G][n][k], or [G][k][n] with w_kn -> (codes
+    [G][n][k], scale [G][ceil(n / 128)][ceil(k / 128)])."""
+    _need(w, "w", (_f32, _bf16), (None, None, None))
+    st = _here(stream, w)
+    G, n, k = (w.shape[0], w.shape[2], w.shape[1]) if w_kn else w.shape
+    q = torch.empty(G, n, k, dtype=_e4m3, device=w.device)
+    s = torch.empty(G, _nblk(n), _nblk(k), dtype=_f32, device=w.device)
+    code = lib.ts_fp8_quant_weights(_ptr(w), wdtype_of_rows(w.dtype), int(bool(w_kn)), G, n, k, _ptr(q), _ptr(s), st)
+    if code:
+        _check(code, "ts_fp8_quant_weights")
+    return q, s
+
+
+def _fp8_shapes(x, x_scale, ws):
+    _need(x, "x", _e4m3, (None, None))
+    S, k = x.shape
+    _need(x_scale, "x_scale", _f32, (S, _nblk(k)))
+    G, n = None, None
+    for name, w, scale in ws:
+        _need(w, name, _e4m3, (G, n, k))
+        G, n = w.shape[:2]
+        _need(scale, f"scale of {name}", _f32, (G, _nblk(n), _nblk(k)))
+    return S, k, G, n
+
+
+def fp8_mm(x, x_scale, w, w_scale, offsets=None, row_src=None, out=None, out_dtype=None, stream=None):
+    """ts_fp8_mm on the codes and scales of fp8_quant and fp8_quant_weights.
+    Returns out [rows][n] (bf16 unless out_dtype or out says otherwise)."""
+    S, k, G, n = _fp8_shapes(x, x_scale, (("w", w, w_scale),))
+    R = _rows_of(x, offsets, row_src, G)
+    odt, od = _odtype(out, out_dtype, _bf16)
+    st = _here(stream, x, x_scale, w, w_scale, offsets, row_src, out)
+    out = _new(out, "out", (R, n), odt, x.device)
+    code = lib.ts_fp8_mm(_ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(row_src), _ptr(offsets), R, S, G, n, k,
+                         _ptr(out), od, st)
+    if code:
+        _check(code, "ts_fp8_mm")
+    return out
+
+
+def fp8_drelu(x, x_scale, w_gate, gate_scale, w_up, up_scale, offsets=None, row_src=None, out=None, out_dtype=None,
+              stream=None):
+    """ts_fp8_drelu: grouped_drelu on quantised rows and weights."""
+    S, k, G, n = _fp8_shapes(x, x_scale, (("w_gate", w_gate, gate_scale), ("w_up", w_up, up_scale)))
+    R = _rows_of(x, offsets, row_src, G)
+    odt, od = _odtype(out, out_dtype, _bf16)
+    st = _here(stream, x, x_scale, w_gate, gate_scale, w_up, up_scale, offsets, row_src, out)
+    out = _new(out, "out", (R, n), odt, x.device)
+    code = lib.ts_fp8_drelu(_ptr(x), _ptr(x_scale), _ptr(w_gate), _ptr(gate_scale), _ptr(w_up), _ptr(up_scale),
+                            _ptr(row_src), _ptr(offsets), R, S, G, n, k, _ptr(out), od, st)
+    if code:
+        _check(code, "ts_fp8_drelu")
+    return out
+
+
+def moe_combine(y, pair_row, w=None, out=None, out_dtype=None, stream=None):
+    """ts_moe_combine.  y [rows][H] bf16 / f32, pair_row [T][K] int32, w [T][K]
+    f32 or None (weights of one).  Returns out [T][H] (y's dtype unless given)."""
+    _need(y, "y", (_f32, _bf16), (None, None))
+    _need(pair_row, "pair_row", _i32, (None, None))
+    T, K = pair_row.shape
+    if w is not None:
+        _need(w, "w", _f32, (T, K))
+    odt, od = _odtype(out, out_dtype, y.dtype)
+    st = _here(stream, y, pair_row, w, out)
+    R, H = y.shape
+    out = _new(out, "out", (T, H), odt, y.device)
+    code = lib.ts_moe_combine(_ptr(y), wdtype_of_rows(y.dtype), _ptr(pair_row), _ptr(w), T, K, H, R, _ptr(out), od, st)
+    if code:
+        _check(code, "ts_moe_combine")
+    return out
+
+
+def moe_combine_grad(d_out, y, pair_row, w, d_y=None, stream=None):
+    """ts_moe_combine_grad.  Returns d_y [rows][H] (y's dtype; rows that no
+    pair names are not written) and d_w [T][K]."""
+    _need(y, "y", (_f32, _bf16), (None, None))
+    _need(pair_row, "pair_row", _i32, (None, None))
+    (R, H), (T, K) = y.shape, pair_row.shape
+    _need(d_out, "d_out", (_f32, _bf16), (T, H))
+    _need(w, "w", _f32, (T, K))
+    st = _here(stream, d_out, y, pair_row, w, d_y)
+    d_y = _new(d_y, "d_y", (R, H), y.dtype, y.device)
+    d_w = torch.empty(T, K, dtype=_f32, device=y.device)
+    code = lib.ts_moe_combine_grad(_ptr(d_out), wdtype_of_rows(d_out.dtype), _ptr(y), wdtype_of_rows(y.dtype),
+                                   _ptr(pair_row), _ptr(w), T, K, H, R, _ptr(d_y), _ptr(d_w), st)
+    if code:
+        _check(code, "ts_moe_combine_grad")
+    return d_y, d_w
 
 
 def probe_read(src: torch.Tensor, sink: torch.Tensor, stream=None):

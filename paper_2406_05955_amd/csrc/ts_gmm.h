@@ -1,0 +1,463 @@
+// The tiled kernel of the grouped products (bf16, fp32, fp8 operands).
+//
+// A workgroup computes a BP x BQ tile of one group's output, contracting 128
+// bytes of both operands per step.  Both operands go from global memory
+// straight into LDS (16 bytes a lane), two steps' buffers in turn: the next
+// step's loads run behind the present step's matrix instructions, one barrier
+// a step.  Loads into LDS put lane i's 16 bytes at 16 i, so the layout that
+// keeps operand reads off each other's banks is made by choosing which global
+// chunk a lane fetches.
+//   row layout ([row][contraction]): LDS row of 128 bytes, chunk c of row r at
+//     position c ^ (r / 2 % 8); an operand register is one 16-byte read.
+//   column layout ([contraction][column], columns contiguous): LDS row of one
+//     contraction index, its 32-byte units (fp32: 64) permuted by the index;
+//     bf16 operands come out through transposing reads (ds_read_b64_tr_b16),
+//     fp32 ones through 4-byte reads.
+// Which contraction indices a lane holds is the same for both operands, all
+// that the products need.
+//
+// The fp8 matrix instructions (all forms alike) add products in groups of 8
+// consecutive indices aligned to the group's largest and cut what is below
+// 2^-13 of it: with values drawn evenly over the codes 5e-5 of the result's
+// 2-norm, far under the codes' own 2^-4; everything behind is fp32.
+//
+// Chunks past the contraction's end come from a block of zeros (both operands:
+// 0 x 0, whatever lies behind), rows past a group's end repeat its last row
+// and are not stored.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "ts_device.h"
+#include "ts_group.h"
+#include "ts_runtime.h"
+
+namespace ts {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4g __attribute__((ext_vector_type(4)));
+
+static __device__ const u32x4 g_zero_chunk = {0u, 0u, 0u, 0u};
+
+enum GmmMode { kFwd = 0, kDrelu = 1, kGradW = 2 };
+
+// 16 bytes a lane from global memory into LDS at `l` + 16 x lane.
+__device__ __forceinline__ void ld_lds16(const void *g, void *l) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g,
+                                     (__attribute__((address_space(3))) void *)l, 16, 0, 0);
+}
+
+// Inclusive sums and maxima over the wave's lanes (maxima of values >= 0):
+// inside rows of 16 lanes, then each row's last lane into the rows behind it.
+template <bool MAX>
+__device__ __forceinline__ int wave_scan(int v) {
+    auto op = [](int x, int y) { return MAX ? max(x, y) : x + y; };
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));  // row_shr:1
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));  // row_bcast:15 into rows 1, 3
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));  // row_bcast:31 into rows 2, 3
+    return v;
+}
+
+// Rows [b, e) of group `lane`.  Offsets are brought into [0, rows] and
+// ascending order, whatever they hold: no two groups share a row.
+__device__ __forceinline__ void seg_bounds(const GmmArgs &a, int lane, int &b, int &e) {
+    if (!a.offsets) {
+        b = 0;
+        e = lane == 0 ? a.rows : 0;
+        return;
+    }
+    b = min(max(a.offsets[min(lane, a.groups)], 0), a.rows);
+    e = min(max(a.offsets[min(lane + 1, a.groups)], 0), a.rows);
+    b = wave_scan<true>(b);
+    e = max(b, e);
+}
+
+template <GmmKind KIND>
+struct GmmElem;
+template <>
+struct GmmElem<kGmmBf16> {
+    static constexpr int SZ = 2;
+};
+template <>
+struct GmmElem<kGmmF32> {
+    static constexpr int SZ = 4;
+};
+template <>
+struct GmmElem<kGmmFp8> {
+    static constexpr int SZ = 1;
+};
+
+// One operand's share of a step: tile of R rows (P or Q indices).
+template <GmmKind KIND, bool COL, int R, int THREADS>
+struct GmmTile {
+    static constexpr int SZ = GmmElem<KIND>::SZ;
+    static constexpr int KS = 128 / SZ;               // contraction indices per step
+    static constexpr int CHUNKS = R * 8;              // 16-byte chunks per step
+    static constexpr int NJ = CHUNKS / THREADS;       // per thread
+    static constexpr int RC = R * SZ / 16;            // column layout: chunks per LDS row
+    static constexpr int UC = KIND == kGmmF32 ? 4 : 2;  // and per 16-column unit
+    static constexpr int NU = RC / UC;                // units per row (a power of two)
+    static_assert(CHUNKS % THREADS == 0 && THREADS % 64 == 0, "whole waves load whole chunks");
+
+    // column layout: what a row's units are permuted by
+    __device__ static __forceinline__ int perm(int kk) {
+        if constexpr (KIND == kGmmF32) return (kk >> 2) & (NU - 1) & 3;
+        else return ((kk & 3) | ((kk >> 1) & 4)) & (NU - 1);
+    }
+    // chunk index -> (row, chunk in row) of what is fetched for it
+    __device__ static __forceinline__ void at(int c, int &row, int &chunk) {
+        if constexpr (COL) {
+            row = c / RC;
+            const int slot = c % RC;
+            chunk = ((slot / UC) ^ perm(row)) * UC + slot % UC;
+        } else {
+            row = c >> 3;
+            chunk = (c & 7) ^ ((row >> 1) & 7);
+        }
+    }
+    // Operand registers of 16-row block `blk`, sub-step s (0 or 1): 16 bytes
+    // of contraction per lane.
+    __device__ static __forceinline__ u32x4 frag(const u32x4 *t, int blk, int s, int lane) {
+        const int lm = lane & 15, lq = lane >> 4;
+        if constexpr (!COL) {
+            const int r = blk * 16 + lm;
+            return t[r * 8 + ((s * 4 + lq) ^ ((r >> 1) & 7))];
+        } else if constexpr (KIND == kGmmF32) {
+            const float *f = reinterpret_cast<const float *>(t);
+            const int k0 = 16 * s + 4 * lq;
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = f[(k0 + i) * R + ((blk ^ perm(k0 + i)) * 16) + lm];
+            return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        } else {
+            // 4 consecutive contraction rows x 16 columns per 16 lanes, twice
+            typedef __attribute__((address_space(3))) s16x4g lds_s16x4;
+            const uint16_t *h = reinterpret_cast<const uint16_t *>(t);
+            const int kk = 32 * s + 8 * lq + (lm >> 2);
+            const s16x4g p = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4 *)(h + kk * R + (blk ^ perm(kk)) * 16 + 4 * (lm & 3)));
+            const s16x4g q = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4 *)(h + (kk + 4) * R + (blk ^ perm(kk + 4)) * 16 + 4 * (lm & 3)));
+            return __builtin_bit_cast(u32x4, __builtin_shufflevector(p, q, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+// 4 consecutive outputs.
+__device__ __forceinline__ void store4(void *out, int f32, size_t i, f32x4 v) {
+    if (f32) {
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(out) + i) = v;
+    } else {
+        // hardware conversion: round to nearest even, NaN stays NaN
+        typedef __bf16 b16x4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<b16x4 *>(static_cast<__bf16 *>(out) + i) = __builtin_convertvector(v, b16x4);
+    }
+}
+
+// dReLU of a gate and an up projection (strict comparisons: a NaN closes).
+__device__ __forceinline__ float drelu1(float g, float u) { return g > 0.f && u > 0.f ? g * u : 0.f; }
+
+// WP x WQ waves; a wave's tile is (BP / WP) x (BQ / WQ).
+template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
+    constexpr int THREADS = 64 * WP * WQ;
+    constexpr bool BCOL = MODE == kGradW;
+    using TA = GmmTile<KIND, ACOL, BP, THREADS>;
+    using TB = GmmTile<KIND, BCOL, BQ, THREADS>;
+    constexpr int SZ = TA::SZ, KS = TA::KS;
+    constexpr int MI = BP / WP / 16, MJ = BQ / WQ / 16;
+    constexpr int PT = MODE == kDrelu ? BP / 2 : BP;  // output columns per tile
+    static_assert(MODE != kGradW || ACOL, "the weight gradient contracts over rows");
+    static_assert(MODE != kDrelu || (!ACOL && MI % 2 == 0), "gate and up in pairs of 16 rows");
+
+    // separate arrays: loads into one are known not to touch the others
+    __shared__ u32x4 sa0[TA::CHUNKS], sb0[TB::CHUNKS], sa1[TA::CHUNKS], sb1[TB::CHUNKS];
+
+    const int tid = threadIdx.x, lane = tid & 63, lm = lane & 15, lq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wp = wave / WQ, wq = wave % WQ;
+
+    const int P = MODE == kGradW ? a.k : a.n;
+    const int npt = (P + PT - 1) / PT;
+    int sb_, se_;
+    seg_bounds(a, lane, sb_, se_);
+    int g, b, e, q0, q_end, pt;
+    {
+        // the dispatcher hands workgroup i to XCD i % 8: each XCD takes one
+        // run of tiles, so that the tiles it works on share operands in its L2
+        const int tiles = MODE == kGradW ? 0 : (se_ - sb_ + BQ - 1) / BQ;
+        const int scan = wave_scan<false>(tiles);
+        const int nqt = MODE == kGradW ? a.groups * ((a.n + BQ - 1) / BQ) : __builtin_amdgcn_readlane(scan, 63);
+        const int total = nqt * npt;
+        const int per = (total + 7) / 8;
+        const int slot = blockIdx.x / 8, id = (blockIdx.x % 8) * per + slot;
+        if (slot >= per || id >= total) return;
+        // strips of up to 4 Q tiles, P tile by P tile
+        const int strip = id / (4 * npt), r = id - strip * 4 * npt;
+        const int sw = min(4, nqt - strip * 4);
+        const int qt = strip * 4 + r % sw;
+        pt = r / sw;
+        if constexpr (MODE == kGradW) {
+            const int per_g = (a.n + BQ - 1) / BQ;
+            g = qt / per_g;
+            q0 = (qt - g * per_g) * BQ;
+            q_end = a.n;
+            b = __builtin_amdgcn_readlane(sb_, g);
+            e = __builtin_amdgcn_readlane(se_, g);
+        } else {
+            const uint64_t before = __ballot(scan - tiles <= qt && tiles > 0);
+            g = 63 - __clzll(before);
+            b = __builtin_amdgcn_readlane(sb_, g);
+            e = __builtin_amdgcn_readlane(se_, g);
+            q0 = b + (qt - __builtin_amdgcn_readlane(scan - tiles, g)) * BQ;
+            q_end = e;
+        }
+    }
+    const int p0 = pt * PT;
+    // contraction: k, or the group's rows
+    const int C = MODE == kGradW ? e - b : a.k;
+    const int steps1 = (C + KS - 1) / KS, steps = steps1 * a.pairs;
+
+    const char *zero = reinterpret_cast<const char *>(&g_zero_chunk);
+    const size_t wbytes = (size_t)a.n * a.k * SZ;
+    // P operand's chunk pointers at step 0, advancing by astep
+    const char *pa[TA::NJ];
+    const char *pb[TB::NJ];
+    int ka, kb;  // first contraction index of this thread's chunks (row layout: the same for each)
+    size_t astep, bstep;
+    auto source = [&](int r) {
+        return a.row_src ? min(max(a.row_src[r], 0), a.src_rows - 1) : min(r, a.src_rows - 1);
+    };
+#pragma unroll
+    for (int j = 0; j < TA::NJ; ++j) {
+        int row, ch;
+        TA::at(tid + THREADS * j, row, ch);
+        if constexpr (MODE == kGradW) {
+            // set per step (rows are gathered); here the column only
+            pa[j] = a.w[0] + (size_t)min(p0 * SZ + ch * 16, a.k * SZ - 16);
+        } else if constexpr (ACOL) {
+            pa[j] = a.w[0] + g * wbytes + (size_t)row * a.n * SZ + min(p0 * SZ + ch * 16, a.n * SZ - 16);
+        } else {
+            const char *m = a.w[0];
+            int n = p0 + row;
+            if constexpr (MODE == kDrelu) {
+                m = (row >> 4) & 1 ? a.w[1] : a.w[0];
+                n = p0 + (row >> 5) * 16 + (row & 15);
+            }
+            pa[j] = m + g * wbytes + (size_t)min(n, a.n - 1) * a.k * SZ + ch * 16;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < TB::NJ; ++j) {
+        int row, ch;
+        TB::at(tid + THREADS * j, row, ch);
+        if constexpr (MODE == kGradW) pb[j] = a.x[0] + (size_t)min(q0 * SZ + ch * 16, a.n * SZ - 16);
+        else pb[j] = a.x[0] + (size_t)source(min(q0 + row, e - 1)) * a.k * SZ + ch * 16;
+    }
+    {
+        int row, ch;
+        TA::at(tid, row, ch);
+        ka = ACOL ? row : ch * (16 / SZ);
+        TB::at(tid, row, ch);
+        kb = BCOL ? row : ch * (16 / SZ);
+    }
+    astep = ACOL && MODE != kGradW ? (size_t)KS * a.n * SZ : 128;
+    bstep = 128;
+    constexpr int JA = ACOL ? THREADS / TA::RC : 0;  // contraction rows between a thread's chunks
+    constexpr int JB = BCOL ? THREADS / TB::RC : 0;
+
+    // loads of step st, the one after the last issued
+    auto issue = [&](u32x4 *A, u32x4 *B, int st) {
+        u32x4 *la = A + wave * 64, *lb = B + wave * 64;
+        if constexpr (MODE == kGradW) {
+#pragma unroll
+            for (int j = 0; j < TA::NJ; ++j) {
+                const int r = st * KS + ka + JA * j;
+                ld_lds16(r < C ? pa[j] + (size_t)source(b + r) * a.k * SZ : zero, la + THREADS * j);
+            }
+#pragma unroll
+            for (int j = 0; j < TB::NJ; ++j) {
+                const int r = st * KS + kb + JB * j;
+                ld_lds16(r < C ? pb[j] + (size_t)(b + r) * a.n * SZ : zero, lb + THREADS * j);
+            }
+        } else {
+            const int s1 = st >= steps1 ? st - steps1 : st;
+            const int left = C - s1 * KS;
+            if (left >= KS) {
+#pragma unroll
+                for (int j = 0; j < TA::NJ; ++j) ld_lds16(pa[j], la + THREADS * j);
+#pragma unroll
+                for (int j = 0; j < TB::NJ; ++j) ld_lds16(pb[j], lb + THREADS * j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < TA::NJ; ++j) ld_lds16(ka + JA * j < left ? pa[j] : zero, la + THREADS * j);
+#pragma unroll
+                for (int j = 0; j < TB::NJ; ++j) ld_lds16(kb < left ? pb[j] : zero, lb + THREADS * j);
+            }
+            // the second pair's operands have the first one's layout
+            const ptrdiff_t da = st + 1 == steps1 && a.pairs == 2
+                                     ? a.w[1] - a.w[0] - (ptrdiff_t)((steps1 - 1) * astep) : (ptrdiff_t)astep;
+            const ptrdiff_t db = st + 1 == steps1 && a.pairs == 2
+                                     ? a.x[1] - a.x[0] - (ptrdiff_t)((steps1 - 1) * bstep) : (ptrdiff_t)bstep;
+#pragma unroll
+            for (int j = 0; j < TA::NJ; ++j) pa[j] += da;
+#pragma unroll
+            for (int j = 0; j < TB::NJ; ++j) pb[j] += db;
+        }
+    };
+
+    f32x4 acc[MI][MJ] = {};
+
+    // fp8: the scales of this lane's columns and this wave's rows, a step ahead
+    const float *psx[MJ];
+    const float *psw[2];
+    float sx[MJ], sw[2] = {0.f, 0.f};
+    if constexpr (KIND == kGmmFp8) {
+        const int kbn = (a.k + kScaleBlock - 1) / kScaleBlock, nbn = (a.n + kScaleBlock - 1) / kScaleBlock;
+#pragma unroll
+        for (int j = 0; j < MJ; ++j)
+            psx[j] = a.xs + (size_t)source(min(q0 + (wq * MJ + j) * 16 + lm, e - 1)) * kbn;
+        const int nb = min((p0 + wp * (PT / WP)) / kScaleBlock, nbn - 1);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+            psw[m] = (MODE == kDrelu && m ? a.ws[1] : a.ws[0]) + ((size_t)g * nbn + nb) * kbn;
+    }
+    auto scales = [&](int st) {
+        if constexpr (KIND == kGmmFp8) {
+#pragma unroll
+            for (int j = 0; j < MJ; ++j) sx[j] = psx[j][st];
+            sw[0] = psw[0][st];
+            if constexpr (MODE == kDrelu) sw[1] = psw[1][st];
+        }
+    };
+
+    auto contract = [&](const u32x4 *A, const u32x4 *B, int st) {
+        if constexpr (KIND == kGmmFp8) {
+            float f[2][MJ];
+#pragma unroll
+            for (int j = 0; j < MJ; ++j) {
+                f[0][j] = sx[j] * sw[0];
+                f[1][j] = MODE == kDrelu ? sx[j] * sw[1] : f[0][j];
+            }
+            if (st + 1 < steps) scales(st + 1);
+            i32x8 bf[MJ];
+#pragma unroll
+            for (int j = 0; j < MJ; ++j) {
+                const u32x4 lo = TB::frag(B, wq * MJ + j, 0, lane), hi = TB::frag(B, wq * MJ + j, 1, lane);
+                bf[j] = i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+            }
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const u32x4 lo = TA::frag(A, wp * MI + i, 0, lane), hi = TA::frag(A, wp * MI + i, 1, lane);
+                const i32x8 af = {(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w,
+                                  (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+#pragma unroll
+                for (int j = 0; j < MJ; ++j) {
+                    // both formats e4m3; block exponents 127: factors of one
+                    const f32x4 d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                        af, bf[j], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+                    acc[i][j] += d * f[i & 1][j];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                u32x4 bf[MJ];
+#pragma unroll
+                for (int j = 0; j < MJ; ++j) bf[j] = TB::frag(B, wq * MJ + j, s, lane);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    const u32x4 af = TA::frag(A, wp * MI + i, s, lane);
+                    if constexpr (KIND == kGmmBf16) {
+#pragma unroll
+                        for (int j = 0; j < MJ; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                __builtin_bit_cast(bf16x8, af), __builtin_bit_cast(bf16x8, bf[j]), acc[i][j], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+#pragma unroll
+                            for (int j = 0; j < MJ; ++j)
+                                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                                    __uint_as_float(af[v]), __uint_as_float(bf[j][v]), acc[i][j], 0, 0, 0);
+                    }
+                }
+            }
+        }
+    };
+
+    if (steps > 0) {
+        scales(0);
+        issue(sa0, sb0, 0);
+        __syncthreads();
+        for (int st = 0; st < steps; st += 2) {
+            if (st + 1 < steps) issue(sa1, sb1, st + 1);
+            contract(sa0, sb0, st);
+            __syncthreads();
+            if (st + 1 >= steps) break;
+            if (st + 2 < steps) issue(sa0, sb0, st + 2);
+            contract(sa1, sb1, st + 1);
+            __syncthreads();
+        }
+    }
+
+    // lane (lm, lq) holds, of the 16 x 16 block (i, j), column lm (Q) and rows
+    // 4 lq .. 4 lq + 3 (P)
+#pragma unroll
+    for (int j = 0; j < MJ; ++j) {
+        const int q = q0 + (wq * MJ + j) * 16 + lm;
+        if (q >= q_end) continue;
+        if constexpr (MODE == kDrelu) {
+#pragma unroll
+            for (int i = 0; i < MI; i += 2) {
+                const int p = p0 + (wp * MI + i) / 2 * 16 + 4 * lq;
+                if (p >= a.n) continue;
+                const size_t at = (size_t)q * a.n + p;
+                const f32x4 gt = acc[i][j], u = acc[i + 1][j];
+                f32x4 c;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) c[v] = drelu1(gt[v], u[v]);
+                store4(a.out, a.out_f32, at, c);
+                if (a.gate) {
+                    store4(a.gate, a.out_f32, at, gt);
+                    store4(a.up, a.out_f32, at, u);
+                }
+            }
+        } else {
+            const size_t base = MODE == kGradW ? ((size_t)g * a.n + q) * a.k : (size_t)q * a.n;
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const int p = p0 + (wp * MI + i) * 16 + 4 * lq;
+                if (p < P) store4(a.out, a.out_f32, base + p, acc[i][j]);
+            }
+        }
+    }
+}
+
+// Grid of gmm_tiled: an upper bound of its tiles (how many row tiles the
+// groups have is known on the device only), a multiple of the 8 XCDs.
+template <GmmMode MODE, int BP, int BQ>
+inline long long gmm_grid(const GmmArgs &a) {
+    const int PT = MODE == kDrelu ? BP / 2 : BP;
+    const long long npt = ceil_div(MODE == kGradW ? a.k : a.n, PT);
+    const long long nqt = MODE == kGradW ? (long long)a.groups * ceil_div(a.n, BQ)
+                                         : (a.offsets ? (long long)a.rows / BQ + a.groups : ceil_div(a.rows, BQ));
+    return (npt * nqt + 7) / 8 * 8;
+}
+
+// Launches it; a grid beyond the runtime's 2^32 threads is refused.
+template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ>
+ts_status run_tiled(const char *name, const GmmArgs &a, hipStream_t st) {
+    const long long grid = gmm_grid<MODE, BP, BQ>(a);
+    if (grid * (64 * WP * WQ) >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
+    launch<GmmArgs>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ>, dim3((unsigned)grid), dim3(64 * WP * WQ), st, a);
+    return check_launch(name);
+}
+
+}  // namespace ts

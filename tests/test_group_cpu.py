@@ -1,0 +1,199 @@
+"""Refusals of the grouped operators, on the CPU: the C entry points' status
+codes (nothing is enqueued) and the binding's own checks.  The plain 64-bit
+forms that the GPU tests compare with are held against one another here."""
+import itertools
+
+import pytest
+import torch
+
+import group_util as ref
+from paper_2406_05955_amd import binding as ts
+
+OK, NULL, SHAPE, DTYPE, ALIGN, WS, HIP, UNSUP = range(8)
+A = 0x10000  # a 16-byte aligned fake device address; never dereferenced
+lib = ts.lib
+
+
+def mm(x=A, w=A, x2=None, w2=None, dt=1, kn=0, src=None, off=A, rows=8, S=8, G=2, n=16, k=16, out=A, odt=1):
+    return lib.ts_grouped_mm(x, w, x2, w2, dt, kn, src, off, rows, S, G, n, k, out, odt, None)
+
+
+def drelu(x=A, wg=A, wu=A, dt=1, src=None, off=A, rows=8, S=8, G=2, n=16, k=16, c=A, gate=None, up=None, odt=1):
+    return lib.ts_grouped_drelu(x, wg, wu, dt, src, off, rows, S, G, n, k, c, gate, up, odt, None)
+
+
+def dw(x=A, w=A, dt=1, src=None, off=A, rows=8, S=8, G=2, n=16, k=16, out=A, odt=1):
+    return lib.ts_grouped_mm_dw(w, x, dt, src, off, rows, S, G, n, k, out, odt, None)
+
+
+def fp8(x=A, xs=A, w=A, ws=A, src=None, off=A, rows=8, S=8, G=2, n=16, k=16, out=A, odt=1):
+    return lib.ts_fp8_mm(x, xs, w, ws, src, off, rows, S, G, n, k, out, odt, None)
+
+
+def fp8_drelu(x=A, wu=A, us=A, src=None, off=A, rows=8, S=8, G=2, n=16, k=16, out=A, odt=1):
+    return lib.ts_fp8_drelu(x, A, A, A, wu, us, src, off, rows, S, G, n, k, out, odt, None)
+
+
+@pytest.mark.parametrize("call", [mm, drelu, dw, fp8, fp8_drelu])
+def test_products_refuse_sizes_and_pointers(call):
+    for bad in (dict(rows=-1), dict(rows=(1 << 23) + 1, S=1 << 23), dict(G=0), dict(G=65), dict(n=0), dict(k=0),
+                dict(n=12), dict(k=20), dict(n=1 << 18), dict(S=0), dict(S=7), dict(S=(1 << 23) + 1),
+                dict(n=131072, k=131072)):
+        assert call(**bad) == SHAPE, bad
+    assert call(odt=3) == DTYPE
+    assert call(off=None) == NULL
+    assert call(off=A + 2) == ALIGN and call(src=A + 1, S=3) == ALIGN
+    assert call(x=A + 8) == ALIGN and call(x=None) == NULL
+
+
+def test_products_refuse_the_rest():
+    assert mm(dt=2) == DTYPE and dw(dt=2) == DTYPE and drelu(dt=2) == DTYPE
+    assert mm(w=None) == NULL and mm(out=None) == NULL and dw(out=None) == NULL and dw(w=None) == NULL
+    assert mm(x2=A) == NULL and mm(w2=A) == NULL and mm(x2=A, w2=A + 4) == ALIGN and mm(out=A + 8) == ALIGN
+    assert mm(dt=0, n=12, k=20, out=None) == NULL and mm(dt=0, n=14) == SHAPE
+    assert drelu(gate=A) == NULL and drelu(up=A) == NULL and drelu(wu=None) == NULL and drelu(c=None) == NULL
+    assert drelu(gate=A + 4, up=A) == ALIGN and drelu(wu=A + 2) == ALIGN
+    assert fp8(xs=None) == NULL and fp8(ws=None) == NULL and fp8(xs=A + 2) == ALIGN and fp8(n=24) == SHAPE
+    assert fp8_drelu(wu=None) == NULL and fp8_drelu(us=None) == NULL and fp8_drelu(wu=A + 8) == ALIGN
+
+
+def test_no_rows_is_nothing_to_do():
+    assert mm(rows=0, S=0, x=None, w=None, out=None) == OK
+    assert drelu(rows=0, S=0, x=None, c=None) == OK
+    assert fp8(rows=0, S=0, x=None, xs=None) == OK
+    assert dw(rows=0, S=0, x=None, w=None, out=None) == NULL  # its zeros are written all the same
+    assert lib.ts_drelu_grad(None, None, None, 1, 0, 16, None, None, None) == OK
+    assert lib.ts_fp8_quant(None, 1, 0, 16, None, None, None) == OK
+    assert lib.ts_moe_combine(None, 1, None, None, 0, 2, 16, 0, None, 1, None) == OK
+    assert lib.ts_moe_route(None, 0, 8, 2, None, None, None, None, None, None, 0, None) == OK
+    assert lib.ts_moe_route_grad(None, None, None, 0, 8, 2, None, None) == OK
+
+
+def test_drelu_grad_and_quantisers():
+    f = lib.ts_drelu_grad
+    assert f(A, A, A, 5, 4, 16, A, A, None) == DTYPE
+    assert f(A, A, A, 1, -1, 16, A, A, None) == SHAPE and f(A, A, A, 1, 4, 12, A, A, None) == SHAPE
+    assert f(A, None, A, 1, 4, 16, A, A, None) == NULL and f(A, A, A, 1, 4, 16, A, None, None) == NULL
+    assert f(A, A, A + 2, 1, 4, 16, A, A, None) == ALIGN
+    q = lib.ts_fp8_quant
+    assert q(A, 4, 4, 16, A, A, None) == DTYPE and q(A, 1, 4, 24, A, A, None) == SHAPE
+    assert q(A, 1, -4, 16, A, A, None) == SHAPE and q(A, 1, 4, 16, None, A, None) == NULL
+    assert q(A + 8, 1, 4, 16, A, A, None) == ALIGN and q(A, 1, 4, 16, A, A + 2, None) == ALIGN
+    w = lib.ts_fp8_quant_weights
+    assert w(A, 9, 0, 1, 16, 16, A, A, None) == DTYPE and w(A, 1, 0, 0, 16, 16, A, A, None) == SHAPE
+    assert w(A, 1, 0, 1, 16, 8, A, A, None) == SHAPE and w(A, 1, 0, 1, 16, 16, A, None, None) == NULL
+
+
+def test_routing():
+    def route(l=A, T=8, E=8, K=2, idx=A, w=A, off=A, tok=A, pair=A, ws=A, n=1 << 20):
+        return lib.ts_moe_route(l, T, E, K, idx, w, off, tok, pair, ws, n, None)
+    for bad in (dict(T=-1), dict(E=0), dict(E=65), dict(K=0), dict(K=9, E=16), dict(K=3, E=2), dict(T=(1 << 22) + 1)):
+        assert route(**bad) == SHAPE, bad
+    assert route(l=None) == NULL and route(idx=None) == NULL and route(w=None) == NULL
+    assert route(off=None) == NULL and route(tok=None) == NULL and route(pair=None) == NULL
+    assert route(l=A + 2) == ALIGN and route(pair=A + 1) == ALIGN
+    need = ts.moe_route_workspace_bytes(5000, 8, 2)
+    assert need > 0 and ts.moe_route_workspace_bytes(-1, 8, 2) == 0
+    assert route(T=5000, ws=None) == WS and route(T=5000, n=need - 1) == WS and route(T=5000, ws=A + 4, n=need) == ALIGN
+
+    def group(idx=A, T=8, E=8, K=2, off=A, tok=A, pair=A, ws=A, n=1 << 20):
+        return lib.ts_moe_group(idx, T, E, K, off, tok, pair, ws, n, None)
+    assert group(T=-1) == SHAPE and group(idx=None) == NULL and group(off=None) == NULL and group(tok=None) == NULL
+    assert group(off=A + 2) == ALIGN and group(T=5000, ws=None) == WS
+    g = lib.ts_moe_route_grad
+    assert g(A, A, A, 4, 65, 2, A, None) == SHAPE and g(A, None, A, 4, 8, 2, A, None) == NULL
+    assert g(A, A, A + 2, 4, 8, 2, A, None) == ALIGN
+
+
+def test_combine():
+    def f(y=A, yd=1, pair=A, w=A, T=4, K=2, H=16, R=8, out=A, od=1):
+        return lib.ts_moe_combine(y, yd, pair, w, T, K, H, R, out, od, None)
+    for bad in (dict(T=-1), dict(K=0), dict(K=9), dict(H=12), dict(H=0), dict(R=-1), dict(H=1 << 18), dict(T=1 << 23)):
+        assert f(**bad) == SHAPE, bad
+    assert f(yd=2) == DTYPE and f(od=2) == DTYPE and f(y=None) == NULL and f(pair=None) == NULL and f(out=None) == NULL
+    assert f(y=A + 8) == ALIGN and f(w=A + 2) == ALIGN
+
+    def g(do=A, od=1, y=A, yd=1, pair=A, w=A, T=4, K=2, H=16, R=8, dy=A, dw_=A):
+        return lib.ts_moe_combine_grad(do, od, y, yd, pair, w, T, K, H, R, dy, dw_, None)
+    assert g(H=12) == SHAPE and g(od=7) == DTYPE and g(w=None) == NULL and g(dy=None) == NULL and g(dw_=None) == NULL
+    assert g(do=A + 4) == ALIGN and g(dw_=A + 2) == ALIGN
+
+
+def z(*shape, dtype=torch.bfloat16):
+    return torch.zeros(*shape, dtype=dtype)
+
+
+def test_binding_checks():
+    i32, f32, e4 = torch.int32, torch.float32, torch.float8_e4m3fn
+    x, w, off = z(8, 16), z(2, 24, 16), z(3, dtype=i32)
+    for call, err in (
+            (lambda: ts.grouped_mm(z(8, 16, dtype=torch.float16), w, off), TypeError),
+            (lambda: ts.grouped_mm(x, w.float(), off), TypeError),
+            (lambda: ts.grouped_mm(x, z(2, 24, 32), off), ValueError),
+            (lambda: ts.grouped_mm(x, w, off, w_kn=True), ValueError),
+            (lambda: ts.grouped_mm(x, w), ValueError),
+            (lambda: ts.grouped_mm(x, w, z(4, dtype=i32)), ValueError),
+            (lambda: ts.grouped_mm(x, w, off.long()), TypeError),
+            (lambda: ts.grouped_mm(x, w, off, row_src=z(8, dtype=torch.int64)), TypeError),
+            (lambda: ts.grouped_mm(z(0, 16), w, off, row_src=z(8, dtype=i32)), ValueError),
+            (lambda: ts.grouped_mm(x, w, off, x2=x), ValueError),
+            (lambda: ts.grouped_mm(x, w, off, x2=z(7, 16), w2=w), ValueError),
+            (lambda: ts.grouped_mm(x, w, off, out_dtype=torch.float16), TypeError),
+            (lambda: ts.grouped_mm(x, w, off), ValueError),  # host tensors
+            (lambda: ts.grouped_drelu(x, w, z(2, 16, 16), off), ValueError),
+            (lambda: ts.grouped_mm_dw(z(7, 24), x, off), ValueError),
+            (lambda: ts.grouped_mm_dw(z(8, 24, dtype=f32), x, off), TypeError),
+            (lambda: ts.drelu_grad(x, x, z(8, 24)), ValueError),
+            (lambda: ts.fp8_quant(z(8, 16, dtype=torch.float16)), TypeError),
+            (lambda: ts.fp8_mm(z(8, 16, dtype=e4), z(8, 2, dtype=f32), z(2, 24, 16, dtype=e4), z(2, 1, 1, dtype=f32), off),
+             ValueError),
+            (lambda: ts.fp8_mm(x, z(8, 1, dtype=f32), w, z(2, 1, 1, dtype=f32), off), TypeError),
+            (lambda: ts.moe_route(z(8, 4, dtype=f32), 5), ValueError),
+            (lambda: ts.moe_route(x, 2), TypeError),
+            (lambda: ts.moe_group(z(8, 2, dtype=i32), 0), ValueError),
+            (lambda: ts.moe_route_grad(z(8, 2, dtype=i32), z(8, 2, dtype=f32), z(8, 3, dtype=f32), 8), ValueError),
+            (lambda: ts.moe_combine(x, z(4, 2, dtype=i32), z(4, 3, dtype=f32)), ValueError),
+            (lambda: ts.moe_combine_grad(z(3, 16), x, z(4, 2, dtype=i32), z(4, 2, dtype=f32)), ValueError)):
+        with pytest.raises(err):
+            call()
+
+
+# --- the plain forms ---------------------------------------------------------------
+
+def test_plain_products_against_loops():
+    g = torch.Generator().manual_seed(1)
+    x, w = torch.randn(9, 5, generator=g), torch.randn(3, 4, 5, generator=g)
+    off, src = torch.tensor([1, 4, 4, 8]), torch.tensor([8, 0, 3, 3, 1, 2, 7, 5, 6])
+    y, mag = ref.mm(x, w, off, src)
+    d, _ = ref.dw(y.nan_to_num(0).float(), x, off, src)
+    assert torch.isnan(y[[0, 8]]).all() and (d[1] == 0).all()
+    for e, r in ((0, 1), (0, 2), (0, 3), (2, 4), (2, 7)):
+        for j in range(4):
+            terms = [float(x[src[r], i]) * float(w[e, j, i]) for i in range(5)]
+            assert abs(sum(terms) - y[r, j]) < 1e-12 and abs(sum(map(abs, terms)) - mag[r, j]) < 1e-12
+    assert torch.allclose(d[2], sum(y[r].float().double()[:, None] * x[src[r]].double() for r in range(4, 8)))
+
+
+def test_plain_routing_against_all_choices():
+    """Top-k as the best of all ordered choices; rows by counting."""
+    l = torch.tensor([[1.0, 3.0, 3.0, 2.0], [float("nan"), -float("inf"), 0.0, 0.0]])
+    idx, w, off, tok, pair = ref.route(l, 2)
+    for t in range(2):
+        v = [-float("inf") if a != a else a for a in l[t].tolist()]
+        best = max(itertools.permutations(range(4), 2), key=lambda c: [(v[i], -i) for i in c])
+        assert idx[t].tolist() == list(best)
+    assert idx.tolist() == [[1, 2], [2, 3]] and torch.allclose(w, torch.full((2, 2), 0.5, dtype=ref.D))
+    assert off.tolist() == [0, 0, 1, 3, 4] and tok.tolist() == [0, 0, 1, 1] and pair.tolist() == [[0, 1], [2, 3]]
+
+
+def test_plain_quantiser():
+    """Every e4m3 value times a power of two keeps its code; scales as defined."""
+    v = torch.arange(256, dtype=torch.uint8).view(ref.E4M3).float()
+    v = v[torch.isfinite(v)]
+    x = torch.zeros(1, 384)
+    x[0, :254] = v[:254]
+    x[0, 254] = x[0, 0:1].new_tensor(448.0)
+    x[0, 0] = 448.0
+    q, s = ref.quant_rows(x)
+    assert torch.equal(ref.row_values(q, s).float(), x)
+    assert s.tolist()[0][:2] == [1.0, 1.0]
