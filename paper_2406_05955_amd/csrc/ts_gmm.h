@@ -163,8 +163,9 @@ __device__ __forceinline__ void store4(void *out, int f32, size_t i, f32x4 v) {
 // dReLU of a gate and an up projection (strict comparisons: a NaN closes).
 __device__ __forceinline__ float drelu1(float g, float u) { return g > 0.f && u > 0.f ? g * u : 0.f; }
 
-// WP x WQ waves; a wave's tile is (BP / WP) x (BQ / WQ).
-template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ>
+// WP x WQ waves; a wave's tile is (BP / WP) x (BQ / WQ).  WIDE: x is 4 GB or
+// more, its rows' offsets take 64 bits.
+template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, bool WIDE>
 __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
     constexpr int THREADS = 64 * WP * WQ;
     constexpr bool BCOL = MODE == kGradW;
@@ -220,101 +221,53 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
         }
     }
     const int p0 = pt * PT;
-    // contraction: k, or the group's rows
+    // contraction: k, or the group's rows, in blocks of KS
     const int C = MODE == kGradW ? e - b : a.k;
-    const int steps1 = (C + KS - 1) / KS, steps = steps1 * a.pairs;
+    const int blocks = (C + KS - 1) / KS;
 
     const char *zero = reinterpret_cast<const char *>(&g_zero_chunk);
     const size_t wbytes = (size_t)a.n * a.k * SZ;
-    // P operand's chunk pointers at step 0, advancing by astep
-    const char *pa[TA::NJ];
-    const char *pb[TB::NJ];
-    int ka, kb;  // first contraction index of this thread's chunks (row layout: the same for each)
-    size_t astep, bstep;
+    constexpr int JA = ACOL ? THREADS / TA::RC : 0;  // contraction indices between a thread's chunks
+    constexpr int JB = BCOL ? THREADS / TB::RC : 0;
+    using Off = std::conditional_t<WIDE, size_t, uint32_t>;  // of a row of x
+    const Off xrow = (Off)a.k * SZ;
     auto source = [&](int r) {
         return a.row_src ? min(max(a.row_src[r], 0), a.src_rows - 1) : min(r, a.src_rows - 1);
     };
+    // Offsets of what this thread fetches in block 0, behind bases that are the
+    // same for the whole wave; the contraction index of its first chunk.
+    // (weight gradient: aoff in a row of x, whose rows are looked up block by block)
+    uint32_t aoff[TA::NJ];
+    std::conditional_t<MODE == kGradW, uint32_t, Off> boff[TB::NJ];
+    int ka, kb;
 #pragma unroll
     for (int j = 0; j < TA::NJ; ++j) {
         int row, ch;
         TA::at(tid + THREADS * j, row, ch);
+        if (j == 0) ka = ACOL ? row : ch * (16 / SZ);
         if constexpr (MODE == kGradW) {
-            // set per step (rows are gathered); here the column only
-            pa[j] = a.w[0] + (size_t)min(p0 * SZ + ch * 16, a.k * SZ - 16);
+            aoff[j] = (uint32_t)min(p0 * SZ + ch * 16, a.k * SZ - 16);
         } else if constexpr (ACOL) {
-            pa[j] = a.w[0] + g * wbytes + (size_t)row * a.n * SZ + min(p0 * SZ + ch * 16, a.n * SZ - 16);
+            aoff[j] = (uint32_t)row * (uint32_t)(a.n * SZ) + (uint32_t)min(p0 * SZ + ch * 16, a.n * SZ - 16);
         } else {
-            const char *m = a.w[0];
-            int n = p0 + row;
-            if constexpr (MODE == kDrelu) {
-                m = (row >> 4) & 1 ? a.w[1] : a.w[0];
-                n = p0 + (row >> 5) * 16 + (row & 15);
-            }
-            pa[j] = m + g * wbytes + (size_t)min(n, a.n - 1) * a.k * SZ + ch * 16;
+            const int n = MODE == kDrelu ? p0 + (row >> 5) * 16 + (row & 15) : p0 + row;
+            aoff[j] = (uint32_t)min(n, a.n - 1) * (uint32_t)(a.k * SZ) + ch * 16;
         }
     }
 #pragma unroll
     for (int j = 0; j < TB::NJ; ++j) {
         int row, ch;
         TB::at(tid + THREADS * j, row, ch);
-        if constexpr (MODE == kGradW) pb[j] = a.x[0] + (size_t)min(q0 * SZ + ch * 16, a.n * SZ - 16);
-        else pb[j] = a.x[0] + (size_t)source(min(q0 + row, e - 1)) * a.k * SZ + ch * 16;
+        if (j == 0) kb = BCOL ? row : ch * (16 / SZ);
+        if constexpr (MODE == kGradW)
+            boff[j] = (uint32_t)row * (uint32_t)(a.n * SZ) + (uint32_t)min(q0 * SZ + ch * 16, a.n * SZ - 16);
+        else
+            boff[j] = (Off)source(min(q0 + row, e - 1)) * xrow + ch * 16;
     }
-    {
-        int row, ch;
-        TA::at(tid, row, ch);
-        ka = ACOL ? row : ch * (16 / SZ);
-        TB::at(tid, row, ch);
-        kb = BCOL ? row : ch * (16 / SZ);
-    }
-    astep = ACOL && MODE != kGradW ? (size_t)KS * a.n * SZ : 128;
-    bstep = 128;
-    constexpr int JA = ACOL ? THREADS / TA::RC : 0;  // contraction rows between a thread's chunks
-    constexpr int JB = BCOL ? THREADS / TB::RC : 0;
-
-    // loads of step st, the one after the last issued
-    auto issue = [&](u32x4 *A, u32x4 *B, int st) {
-        u32x4 *la = A + wave * 64, *lb = B + wave * 64;
-        if constexpr (MODE == kGradW) {
-#pragma unroll
-            for (int j = 0; j < TA::NJ; ++j) {
-                const int r = st * KS + ka + JA * j;
-                ld_lds16(r < C ? pa[j] + (size_t)source(b + r) * a.k * SZ : zero, la + THREADS * j);
-            }
-#pragma unroll
-            for (int j = 0; j < TB::NJ; ++j) {
-                const int r = st * KS + kb + JB * j;
-                ld_lds16(r < C ? pb[j] + (size_t)(b + r) * a.n * SZ : zero, lb + THREADS * j);
-            }
-        } else {
-            const int s1 = st >= steps1 ? st - steps1 : st;
-            const int left = C - s1 * KS;
-            if (left >= KS) {
-#pragma unroll
-                for (int j = 0; j < TA::NJ; ++j) ld_lds16(pa[j], la + THREADS * j);
-#pragma unroll
-                for (int j = 0; j < TB::NJ; ++j) ld_lds16(pb[j], lb + THREADS * j);
-            } else {
-#pragma unroll
-                for (int j = 0; j < TA::NJ; ++j) ld_lds16(ka + JA * j < left ? pa[j] : zero, la + THREADS * j);
-#pragma unroll
-                for (int j = 0; j < TB::NJ; ++j) ld_lds16(kb < left ? pb[j] : zero, lb + THREADS * j);
-            }
-            // the second pair's operands have the first one's layout
-            const ptrdiff_t da = st + 1 == steps1 && a.pairs == 2
-                                     ? a.w[1] - a.w[0] - (ptrdiff_t)((steps1 - 1) * astep) : (ptrdiff_t)astep;
-            const ptrdiff_t db = st + 1 == steps1 && a.pairs == 2
-                                     ? a.x[1] - a.x[0] - (ptrdiff_t)((steps1 - 1) * bstep) : (ptrdiff_t)bstep;
-#pragma unroll
-            for (int j = 0; j < TA::NJ; ++j) pa[j] += da;
-#pragma unroll
-            for (int j = 0; j < TB::NJ; ++j) pb[j] += db;
-        }
-    };
 
     f32x4 acc[MI][MJ] = {};
 
-    // fp8: the scales of this lane's columns and this wave's rows, a step ahead
+    // fp8: the scales of this lane's columns and this wave's rows, a block ahead
     const float *psx[MJ];
     const float *psw[2];
     float sx[MJ], sw[2] = {0.f, 0.f};
@@ -328,16 +281,18 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
         for (int m = 0; m < 2; ++m)
             psw[m] = (MODE == kDrelu && m ? a.ws[1] : a.ws[0]) + ((size_t)g * nbn + nb) * kbn;
     }
-    auto scales = [&](int st) {
+    auto scales = [&](int blk) {
         if constexpr (KIND == kGmmFp8) {
 #pragma unroll
-            for (int j = 0; j < MJ; ++j) sx[j] = psx[j][st];
-            sw[0] = psw[0][st];
-            if constexpr (MODE == kDrelu) sw[1] = psw[1][st];
+            for (int j = 0; j < MJ; ++j) sx[j] = psx[j][blk];
+            sw[0] = psw[0][blk];
+            if constexpr (MODE == kDrelu) sw[1] = psw[1][blk];
         }
     };
 
-    auto contract = [&](const u32x4 *A, const u32x4 *B, int st) {
+    const int last = blocks - 1;
+    // contracts the block in A, B; fp8: loads the scales of block `next`
+    auto contract = [&](const u32x4 *A, const u32x4 *B, int next) {
         if constexpr (KIND == kGmmFp8) {
             float f[2][MJ];
 #pragma unroll
@@ -345,7 +300,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
                 f[0][j] = sx[j] * sw[0];
                 f[1][j] = MODE == kDrelu ? sx[j] * sw[1] : f[0][j];
             }
-            if (st + 1 < steps) scales(st + 1);
+            scales(min(next, last));
             i32x8 bf[MJ];
 #pragma unroll
             for (int j = 0; j < MJ; ++j) {
@@ -392,18 +347,48 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
         }
     };
 
-    if (steps > 0) {
-        scales(0);
-        issue(sa0, sb0, 0);
+    // The last block, the only one that may be partial, is contracted first;
+    // the loads of the others check nothing.
+    for (int pair = 0; blocks > 0 && pair < a.pairs; ++pair) {
+        // dReLU: a wave's chunks are of 8 rows (and of those 32 or 64 further
+        // on), so all of w_gate or all of w_up
+        const bool second = MODE == kDrelu ? (wave >> 1) & 1 : pair == 1;
+        const char *abase = (second ? a.w[1] : a.w[0]) + (MODE == kGradW ? 0 : g * wbytes);
+        const char *bbase = (pair == 1 ? a.x[1] : a.x[0]) + (MODE == kGradW ? (size_t)b * a.n * SZ : 0);
+        Off src[TA::NJ];  // weight gradient: offsets of the next block's rows
+        auto fetch_src = [&](int blk) {
+            if constexpr (MODE == kGradW)
+#pragma unroll
+                for (int j = 0; j < TA::NJ; ++j)
+                    src[j] = (Off)source(b + min(blk * KS + ka + JA * j, C - 1)) * xrow + aoff[j];
+        };
+        auto issue = [&](u32x4 *A, u32x4 *B, int blk, int left) {
+            const char *ab = abase + (size_t)blk * (MODE == kGradW ? 0 : ACOL ? (size_t)KS * a.n * SZ : 128);
+            const char *bb = bbase + (size_t)blk * (MODE == kGradW ? (size_t)KS * a.n * SZ : 128);
+            u32x4 *la = A + wave * 64, *lb = B + wave * 64;
+#pragma unroll
+            for (int j = 0; j < TA::NJ; ++j) {
+                const char *p = MODE == kGradW ? ab + src[j] : ab + aoff[j];
+                ld_lds16(left >= KS || ka + JA * j < left ? p : zero, la + THREADS * j);
+            }
+#pragma unroll
+            for (int j = 0; j < TB::NJ; ++j)
+                ld_lds16(left >= KS || kb + JB * j < left ? bb + boff[j] : zero, lb + THREADS * j);
+            fetch_src(blk == last ? 0 : blk + 1);
+        };
+        fetch_src(last);
+        scales(last);
+        issue(sa0, sb0, last, C - last * KS);
         __syncthreads();
-        for (int st = 0; st < steps; st += 2) {
-            if (st + 1 < steps) issue(sa1, sb1, st + 1);
+        for (int st = 0;; st += 2) {
+            if (st < last) issue(sa1, sb1, st, KS);
             contract(sa0, sb0, st);
             __syncthreads();
-            if (st + 1 >= steps) break;
-            if (st + 2 < steps) issue(sa0, sb0, st + 2);
+            if (st >= last) break;
+            if (st + 1 < last) issue(sa0, sb0, st + 1, KS);
             contract(sa1, sb1, st + 1);
             __syncthreads();
+            if (st + 1 >= last) break;
         }
     }
 
@@ -452,12 +437,19 @@ inline long long gmm_grid(const GmmArgs &a) {
 }
 
 // Launches it; a grid beyond the runtime's 2^32 threads is refused.
-template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ>
+template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, bool WIDE = false>
 ts_status run_tiled(const char *name, const GmmArgs &a, hipStream_t st) {
     const long long grid = gmm_grid<MODE, BP, BQ>(a);
     if (grid * (64 * WP * WQ) >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
-    launch<GmmArgs>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ>, dim3((unsigned)grid), dim3(64 * WP * WQ), st, a);
+    launch<GmmArgs>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, WIDE>, dim3((unsigned)grid), dim3(64 * WP * WQ),
+                    st, a);
     return check_launch(name);
+}
+
+// Whether offsets of x's rows need 64 bits.
+template <GmmKind KIND>
+inline bool gmm_wide(const GmmArgs &a) {
+    return (unsigned long long)a.src_rows * a.k * GmmElem<KIND>::SZ >= (1ull << 32);
 }
 
 }  // namespace ts
