@@ -1,14 +1,14 @@
 // The tiled kernel of the grouped products (bf16, fp32, fp8 operands).
 //
-// A workgroup computes a BP x BQ tile of one group's output, contracting 128
-// bytes of both operands per step.  Both operands go from global memory
-// straight into LDS (16 bytes a lane), two steps' buffers in turn: the next
-// step's loads run behind the present step's matrix instructions, one barrier
-// a step.  Loads into LDS put lane i's 16 bytes at 16 i, so the layout that
-// keeps operand reads off each other's banks is made by choosing which global
-// chunk a lane fetches.
-//   row layout ([row][contraction]): LDS row of 128 bytes, chunk c of row r at
-//     position c ^ (r / 2 % 8); an operand register is one 16-byte read.
+// A workgroup computes a BP x BQ tile of one group's output, contracting RB
+// bytes of both operands' rows per step.  Both operands go from global memory
+// straight into LDS (16 bytes a lane) through S stage buffers: S - 1 steps'
+// loads are in flight behind the present step's matrix instructions, one
+// barrier a step.  Loads into LDS put lane i's 16 bytes at 16 i, so the layout
+// that keeps operand reads off each other's banks is made by choosing which
+// global chunk a lane fetches.
+//   row layout ([row][contraction]): LDS row of RB bytes, its chunks permuted
+//     by the row's number; an operand register is one 16-byte read.
 //   column layout ([contraction][column], columns contiguous): LDS row of one
 //     contraction index, its 32-byte units (fp32: 64) permuted by the index;
 //     bf16 operands come out through transposing reads (ds_read_b64_tr_b16),
@@ -44,11 +44,22 @@ static __device__ const u32x4 g_zero_chunk = {0u, 0u, 0u, 0u};
 
 enum GmmMode { kFwd = 0, kDrelu = 1, kGradW = 2 };
 
-// 16 bytes a lane from global memory into LDS at `l` + 16 x lane.
-__device__ __forceinline__ void ld_lds16(const void *g, void *l) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g,
-                                     (__attribute__((address_space(3))) void *)l, 16, 0, 0);
+// 16 bytes a lane from global memory into LDS at byte `l` + 16 x lane (all
+// lanes active).  Written out, with no register to return to: the compiler
+// follows its own loads into LDS and waits for all of them before any read of
+// LDS that it cannot tell apart, which empties the pipeline at every step.
+// The waits are the kernel's: gmm_barrier.
+__device__ __forceinline__ uint32_t lds_addr(const void *p) {
+    return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p);
 }
+__device__ __forceinline__ void ld_lds16(const char *p, uint32_t l) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(l) : "memory", "m0");
+}
+__device__ __forceinline__ void ld_lds16(const char *base, uint32_t off, uint32_t l) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(l)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void ld_lds16(const char *base, size_t off, uint32_t l) { ld_lds16(base + off, l); }
 
 // Inclusive sums and maxima over the wave's lanes (maxima of values >= 0):
 // inside rows of 16 lanes, then each row's last lane into the rows behind it.
@@ -93,18 +104,26 @@ struct GmmElem<kGmmFp8> {
     static constexpr int SZ = 1;
 };
 
-// One operand's share of a step: tile of R rows (P or Q indices).
-template <GmmKind KIND, bool COL, int R, int THREADS>
+// One operand's share of a step: RB bytes of contraction (row layout's terms)
+// of a tile of R rows (P or Q indices).
+template <GmmKind KIND, bool COL, int R, int RB, int THREADS>
 struct GmmTile {
     static constexpr int SZ = GmmElem<KIND>::SZ;
-    static constexpr int KS = 128 / SZ;               // contraction indices per step
-    static constexpr int CHUNKS = R * 8;              // 16-byte chunks per step
+    static constexpr int KS = RB / SZ;                // contraction indices per step
+    static constexpr int CHUNKS = R * RB / 16;        // 16-byte chunks per step
     static constexpr int NJ = CHUNKS / THREADS;       // per thread
+    static constexpr int CR = RB / 16;                // row layout: chunks per LDS row
     static constexpr int RC = R * SZ / 16;            // column layout: chunks per LDS row
     static constexpr int UC = KIND == kGmmF32 ? 4 : 2;  // and per 16-column unit
     static constexpr int NU = RC / UC;                // units per row (a power of two)
     static_assert(CHUNKS % THREADS == 0 && THREADS % 64 == 0, "whole waves load whole chunks");
+    static_assert(RB == 64 || RB == 128, "one or two 64-byte sub-steps");
 
+    // row layout: what a row's chunks are permuted by: the 16 rows of a read
+    // cover all 64 banks
+    __device__ static __forceinline__ int rot(int row) {
+        return RB == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+    }
     // column layout: what a row's units are permuted by
     __device__ static __forceinline__ int perm(int kk) {
         if constexpr (KIND == kGmmF32) return (kk >> 2) & (NU - 1) & 3;
@@ -117,17 +136,17 @@ struct GmmTile {
             const int slot = c % RC;
             chunk = ((slot / UC) ^ perm(row)) * UC + slot % UC;
         } else {
-            row = c >> 3;
-            chunk = (c & 7) ^ ((row >> 1) & 7);
+            row = c / CR;
+            chunk = (c % CR) ^ rot(row);
         }
     }
-    // Operand registers of 16-row block `blk`, sub-step s (0 or 1): 16 bytes
-    // of contraction per lane.
+    // Operand registers of 16-row block `blk`, 64-byte sub-step s: 16 bytes of
+    // contraction per lane.
     __device__ static __forceinline__ u32x4 frag(const u32x4 *t, int blk, int s, int lane) {
         const int lm = lane & 15, lq = lane >> 4;
         if constexpr (!COL) {
             const int r = blk * 16 + lm;
-            return t[r * 8 + ((s * 4 + lq) ^ ((r >> 1) & 7))];
+            return t[r * CR + ((s * 4 + lq) ^ rot(r))];
         } else if constexpr (KIND == kGmmF32) {
             const float *f = reinterpret_cast<const float *>(t);
             const int k0 = 16 * s + 4 * lq;
@@ -149,6 +168,16 @@ struct GmmTile {
     }
 };
 
+// Until at most N of this wave's loads are on their way, then the workgroup's
+// barrier for LDS (its other loads stay in flight).
+template <int N>
+__device__ __forceinline__ void gmm_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // 4 consecutive outputs.
 __device__ __forceinline__ void store4(void *out, int f32, size_t i, f32x4 v) {
     if (f32) {
@@ -163,22 +192,35 @@ __device__ __forceinline__ void store4(void *out, int f32, size_t i, f32x4 v) {
 // dReLU of a gate and an up projection (strict comparisons: a NaN closes).
 __device__ __forceinline__ float drelu1(float g, float u) { return g > 0.f && u > 0.f ? g * u : 0.f; }
 
+__device__ __forceinline__ float ld_f32(const float *base, uint32_t bytes) {
+    return *reinterpret_cast<const float *>(reinterpret_cast<const char *>(base) + bytes);
+}
+
+// f(0), f(1), ... f(N - 1) with constants.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void unroll(F f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        unroll<N, I + 1>(f);
+    }
+}
+
 // WP x WQ waves; a wave's tile is (BP / WP) x (BQ / WQ).  WIDE: x is 4 GB or
 // more, its rows' offsets take 64 bits.
-template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, bool WIDE>
+template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int RB, bool WIDE>
 __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
     constexpr int THREADS = 64 * WP * WQ;
     constexpr bool BCOL = MODE == kGradW;
-    using TA = GmmTile<KIND, ACOL, BP, THREADS>;
-    using TB = GmmTile<KIND, BCOL, BQ, THREADS>;
+    using TA = GmmTile<KIND, ACOL, BP, RB, THREADS>;
+    using TB = GmmTile<KIND, BCOL, BQ, RB, THREADS>;
     constexpr int SZ = TA::SZ, KS = TA::KS;
     constexpr int MI = BP / WP / 16, MJ = BQ / WQ / 16;
     constexpr int PT = MODE == kDrelu ? BP / 2 : BP;  // output columns per tile
     static_assert(MODE != kGradW || ACOL, "the weight gradient contracts over rows");
     static_assert(MODE != kDrelu || (!ACOL && MI % 2 == 0), "gate and up in pairs of 16 rows");
 
-    // separate arrays: loads into one are known not to touch the others
-    __shared__ u32x4 sa0[TA::CHUNKS], sb0[TB::CHUNKS], sa1[TA::CHUNKS], sb1[TB::CHUNKS];
+    constexpr int SC = TA::CHUNKS + TB::CHUNKS;  // chunks of a stage
+    __shared__ u32x4 s_stage[2 * SC];
 
     const int tid = threadIdx.x, lane = tid & 63, lm = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -234,162 +276,212 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
     auto source = [&](int r) {
         return a.row_src ? min(max(a.row_src[r], 0), a.src_rows - 1) : min(r, a.src_rows - 1);
     };
-    // Offsets of what this thread fetches in block 0, behind bases that are the
-    // same for the whole wave; the contraction index of its first chunk.
-    // (weight gradient: aoff in a row of x, whose rows are looked up block by block)
-    uint32_t aoff[TA::NJ];
-    std::conditional_t<MODE == kGradW, uint32_t, Off> boff[TB::NJ];
-    int ka, kb;
-#pragma unroll
-    for (int j = 0; j < TA::NJ; ++j) {
-        int row, ch;
-        TA::at(tid + THREADS * j, row, ch);
-        if (j == 0) ka = ACOL ? row : ch * (16 / SZ);
-        if constexpr (MODE == kGradW) {
-            aoff[j] = (uint32_t)min(p0 * SZ + ch * 16, a.k * SZ - 16);
-        } else if constexpr (ACOL) {
-            aoff[j] = (uint32_t)row * (uint32_t)(a.n * SZ) + (uint32_t)min(p0 * SZ + ch * 16, a.n * SZ - 16);
-        } else {
-            const int n = MODE == kDrelu ? p0 + (row >> 5) * 16 + (row & 15) : p0 + row;
-            aoff[j] = (uint32_t)min(n, a.n - 1) * (uint32_t)(a.k * SZ) + ch * 16;
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < TB::NJ; ++j) {
-        int row, ch;
-        TB::at(tid + THREADS * j, row, ch);
-        if (j == 0) kb = BCOL ? row : ch * (16 / SZ);
-        if constexpr (MODE == kGradW)
-            boff[j] = (uint32_t)row * (uint32_t)(a.n * SZ) + (uint32_t)min(q0 * SZ + ch * 16, a.n * SZ - 16);
-        else
-            boff[j] = (Off)source(min(q0 + row, e - 1)) * xrow + ch * 16;
-    }
-
     f32x4 acc[MI][MJ] = {};
 
     // fp8: the scales of this lane's columns and this wave's rows, a block ahead
-    const float *psx[MJ];
-    const float *psw[2];
-    float sx[MJ], sw[2] = {0.f, 0.f};
+    uint32_t xso[MJ], wso = 0;
+    float sx[MJ] = {}, sw[2] = {0.f, 0.f};
     if constexpr (KIND == kGmmFp8) {
         const int kbn = (a.k + kScaleBlock - 1) / kScaleBlock, nbn = (a.n + kScaleBlock - 1) / kScaleBlock;
+        // (32 times fewer bytes than x: 32 bits wherever x's offsets have them)
 #pragma unroll
         for (int j = 0; j < MJ; ++j)
-            psx[j] = a.xs + (size_t)source(min(q0 + (wq * MJ + j) * 16 + lm, e - 1)) * kbn;
+            xso[j] = 4u * (uint32_t)source(min(q0 + (wq * MJ + j) * 16 + lm, e - 1)) * (uint32_t)kbn;
         const int nb = min((p0 + wp * (PT / WP)) / kScaleBlock, nbn - 1);
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-            psw[m] = (MODE == kDrelu && m ? a.ws[1] : a.ws[0]) + ((size_t)g * nbn + nb) * kbn;
+        // (a matrix has below 4 GB / 2^14 scales, 64 groups of it 32 bits' worth;
+        // a vector load: a scalar one would be waited for with the LDS reads)
+        wso = 4u * (uint32_t)((g * nbn + nb) * kbn);
+        asm volatile("" : "+v"(wso));
     }
-    auto scales = [&](int blk) {
+    float f[2][MJ];
+    // fp8: the present block's factors; asks for the scales of block `next`
+    auto scales = [&](int next) {
         if constexpr (KIND == kGmmFp8) {
-#pragma unroll
-            for (int j = 0; j < MJ; ++j) sx[j] = psx[j][blk];
-            sw[0] = psw[0][blk];
-            if constexpr (MODE == kDrelu) sw[1] = psw[1][blk];
-        }
-    };
-
-    const int last = blocks - 1;
-    // contracts the block in A, B; fp8: loads the scales of block `next`
-    auto contract = [&](const u32x4 *A, const u32x4 *B, int next) {
-        if constexpr (KIND == kGmmFp8) {
-            float f[2][MJ];
 #pragma unroll
             for (int j = 0; j < MJ; ++j) {
                 f[0][j] = sx[j] * sw[0];
                 f[1][j] = MODE == kDrelu ? sx[j] * sw[1] : f[0][j];
-            }
-            scales(min(next, last));
-            i32x8 bf[MJ];
-#pragma unroll
-            for (int j = 0; j < MJ; ++j) {
-                const u32x4 lo = TB::frag(B, wq * MJ + j, 0, lane), hi = TB::frag(B, wq * MJ + j, 1, lane);
-                bf[j] = i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+                // (computed here: behind the next stage's loads, the wait for
+                // the scales would be one for those too)
+                asm volatile("" : "+v"(f[0][j]), "+v"(f[1][j]));
             }
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const u32x4 lo = TA::frag(A, wp * MI + i, 0, lane), hi = TA::frag(A, wp * MI + i, 1, lane);
-                const i32x8 af = {(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w,
-                                  (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+            for (int j = 0; j < MJ; ++j) sx[j] = ld_f32(a.xs, xso[j] + 4u * next);
+            sw[0] = ld_f32(a.ws[0], wso + 4u * next);
+            if constexpr (MODE == kDrelu) sw[1] = ld_f32(a.ws[1], wso + 4u * next);
+        }
+    };
+
+    const int last = blocks - 1;
+    // Contracts the stage in `A`.  Groups of MJ matrix instructions (one block
+    // of 16 P rows, one sub-step); operand reads run a group or two (where the registers allow) ahead, and
+    // between(group) issues the next stages' loads spread over the groups: all
+    // at once they hold up the waves that issue them.
+    constexpr int NS = KIND == kGmmFp8 ? 1 : RB / 64, NG = NS * MI;
+    auto contract = [&](const u32x4 *A, auto between) {
+        const u32x4 *B = A + TA::CHUNKS;
+        using Frag = std::conditional_t<KIND == kGmmFp8, i32x8, u32x4>;
+        auto read = [&](auto tile, const u32x4 *t, int blk, int s) -> Frag {
+            using T = decltype(tile);
+            if constexpr (KIND == kGmmFp8) {
+                const u32x4 lo = T::frag(t, blk, 0, lane), hi = T::frag(t, blk, 1, lane);
+                return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+            } else {
+                return T::frag(t, blk, s, lane);
+            }
+        };
+        constexpr int AHEAD = KIND == kGmmFp8 || MODE == kGradW ? 1 : 2;
+        Frag af[AHEAD + 1], bf[NS][MJ];
+#pragma unroll
+        for (int j = 0; j < MJ; ++j) bf[0][j] = read(TB{}, B, wq * MJ + j, 0);
+        unroll<AHEAD>([&](auto gi) {
+            if constexpr (gi < NG) af[gi] = read(TA{}, A, wp * MI + gi % MI, gi / MI);
+        });
+        unroll<NG>([&](auto gi) {
+            constexpr int G = gi, s = G / MI, i = G % MI;
+            constexpr int NX = G + AHEAD;
+            if constexpr (NX < NG) af[NX % (AHEAD + 1)] = read(TA{}, A, wp * MI + NX % MI, NX / MI);
+            if constexpr (s + 1 < NS) {
+                // the next sub-step's Q operands, over this one's groups
+#pragma unroll
+                for (int j = i * MJ / MI; j < (i + 1) * MJ / MI; ++j) bf[s + 1][j] = read(TB{}, B, wq * MJ + j, s + 1);
+            }
+            const Frag a_ = af[G % (AHEAD + 1)];
+            if constexpr (KIND == kGmmFp8) {
 #pragma unroll
                 for (int j = 0; j < MJ; ++j) {
                     // both formats e4m3; block exponents 127: factors of one
                     const f32x4 d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                        af, bf[j], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+                        a_, bf[0][j], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
                     acc[i][j] += d * f[i & 1][j];
                 }
+            } else if constexpr (KIND == kGmmBf16) {
+#pragma unroll
+                for (int j = 0; j < MJ; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8, a_), __builtin_bit_cast(bf16x8, bf[s][j]), acc[i][j], 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+#pragma unroll
+                    for (int j = 0; j < MJ; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                            __uint_as_float(a_[v]), __uint_as_float(bf[s][j][v]), acc[i][j], 0, 0, 0);
             }
-        } else {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                u32x4 bf[MJ];
-#pragma unroll
-                for (int j = 0; j < MJ; ++j) bf[j] = TB::frag(B, wq * MJ + j, s, lane);
-#pragma unroll
-                for (int i = 0; i < MI; ++i) {
-                    const u32x4 af = TA::frag(A, wp * MI + i, s, lane);
-                    if constexpr (KIND == kGmmBf16) {
-#pragma unroll
-                        for (int j = 0; j < MJ; ++j)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                __builtin_bit_cast(bf16x8, af), __builtin_bit_cast(bf16x8, bf[j]), acc[i][j], 0, 0, 0);
-                    } else {
-#pragma unroll
-                        for (int v = 0; v < 4; ++v)
-#pragma unroll
-                            for (int j = 0; j < MJ; ++j)
-                                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                                    __uint_as_float(af[v]), __uint_as_float(bf[j][v]), acc[i][j], 0, 0, 0);
-                    }
-                }
-            }
-        }
+            between(gi);
+            __builtin_amdgcn_sched_barrier(0);
+        });
     };
 
     // The last block, the only one that may be partial, is contracted first;
     // the loads of the others check nothing.
     for (int pair = 0; blocks > 0 && pair < a.pairs; ++pair) {
-        // dReLU: a wave's chunks are of 8 rows (and of those 32 or 64 further
-        // on), so all of w_gate or all of w_up
-        const bool second = MODE == kDrelu ? (wave >> 1) & 1 : pair == 1;
+        // dReLU: a wave's chunks are of 64 / CR consecutive rows (and of those
+        // 32 or more further on), so all of w_gate or all of w_up
+        const bool second = MODE == kDrelu ? ((wave * (64 / TA::CR)) >> 4) & 1 : pair == 1;
         const char *abase = (second ? a.w[1] : a.w[0]) + (MODE == kGradW ? 0 : g * wbytes);
         const char *bbase = (pair == 1 ? a.x[1] : a.x[0]) + (MODE == kGradW ? (size_t)b * a.n * SZ : 0);
-        Off src[TA::NJ];  // weight gradient: offsets of the next block's rows
-        auto fetch_src = [&](int blk) {
+        // bytes from one block to the next
+        size_t astep = MODE == kGradW ? 0 : ACOL ? (size_t)KS * a.n * SZ : RB;
+        size_t bstep = MODE == kGradW ? (size_t)KS * a.n * SZ : RB;
+        // Offsets of what this thread fetches in block 0, behind those bases
+        // (weight gradient: aoff in a row of x; the rows are looked up block by
+        // block); the contraction index of its first chunk.
+        std::conditional_t<MODE == kGradW, Off, uint32_t> aoff[TA::NJ];
+        std::conditional_t<MODE == kGradW, uint32_t, Off> boff[TB::NJ];
+        Off rowoff[MODE == kGradW ? TA::NJ : 1];
+        int ka, kb;
+#pragma unroll
+        for (int j = 0; j < TA::NJ; ++j) {
+            int row, ch;
+            TA::at(tid + THREADS * j, row, ch);
+            if (j == 0) ka = ACOL ? row : ch * (16 / SZ);
+            if constexpr (MODE == kGradW) {
+                aoff[j] = (Off)min(p0 * SZ + ch * 16, a.k * SZ - 16);
+            } else if constexpr (ACOL) {
+                aoff[j] = (uint32_t)row * (uint32_t)(a.n * SZ) + (uint32_t)min(p0 * SZ + ch * 16, a.n * SZ - 16);
+            } else {
+                const int n = MODE == kDrelu ? p0 + (row >> 5) * 16 + (row & 15) : p0 + row;
+                aoff[j] = (uint32_t)min(n, a.n - 1) * (uint32_t)(a.k * SZ) + ch * 16;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < TB::NJ; ++j) {
+            int row, ch;
+            TB::at(tid + THREADS * j, row, ch);
+            if (j == 0) kb = BCOL ? row : ch * (16 / SZ);
+            if constexpr (MODE == kGradW)
+                boff[j] = (uint32_t)row * (uint32_t)(a.n * SZ) + (uint32_t)min(q0 * SZ + ch * 16, a.n * SZ - 16);
+            else
+                boff[j] = (Off)source(min(q0 + row, e - 1)) * xrow + ch * 16;
+        }
+        // weight gradient: the offsets of block blk's rows of x
+        auto look_up = [&](int blk) {
             if constexpr (MODE == kGradW)
 #pragma unroll
                 for (int j = 0; j < TA::NJ; ++j)
-                    src[j] = (Off)source(b + min(blk * KS + ka + JA * j, C - 1)) * xrow + aoff[j];
+                    rowoff[j] = (Off)source(b + min(blk * KS + ka + JA * j, C - 1)) * xrow;
         };
-        auto issue = [&](u32x4 *A, u32x4 *B, int blk, int left) {
-            const char *ab = abase + (size_t)blk * (MODE == kGradW ? 0 : ACOL ? (size_t)KS * a.n * SZ : 128);
-            const char *bb = bbase + (size_t)blk * (MODE == kGradW ? (size_t)KS * a.n * SZ : 128);
-            u32x4 *la = A + wave * 64, *lb = B + wave * 64;
-#pragma unroll
-            for (int j = 0; j < TA::NJ; ++j) {
-                const char *p = MODE == kGradW ? ab + src[j] : ab + aoff[j];
-                ld_lds16(left >= KS || ka + JA * j < left ? p : zero, la + THREADS * j);
-            }
-#pragma unroll
-            for (int j = 0; j < TB::NJ; ++j)
-                ld_lds16(left >= KS || kb + JB * j < left ? bb + boff[j] : zero, lb + THREADS * j);
-            fetch_src(blk == last ? 0 : blk + 1);
+        auto a_off = [&](auto j) {
+            if constexpr (MODE == kGradW) return (Off)(rowoff[j] + aoff[j]);
+            else return aoff[j];
         };
-        fetch_src(last);
+        const uint32_t lds = lds_addr(s_stage) + wave * 1024;
+        constexpr int LOADS = TA::NJ + TB::NJ;  // of a stage, per wave
+        // load L of a whole block into stage `to`
+        auto load = [&](auto l, int blk, int to) {
+            constexpr int L = l, J = L < TA::NJ ? L : L - TA::NJ;
+            const uint32_t at = lds + (uint32_t)to * (SC * 16) + 16 * THREADS * J;
+            if constexpr (L < TA::NJ)
+                ld_lds16(abase + blk * astep, a_off(std::integral_constant<int, J>{}), at);
+            else
+                ld_lds16(bbase + blk * bstep, boff[J], at + TA::CHUNKS * 16);
+        };
+
+        look_up(last);
         scales(last);
-        issue(sa0, sb0, last, C - last * KS);
-        __syncthreads();
-        for (int st = 0;; st += 2) {
-            if (st < last) issue(sa1, sb1, st, KS);
-            contract(sa0, sb0, st);
-            __syncthreads();
-            if (st >= last) break;
-            if (st + 1 < last) issue(sa0, sb0, st + 1, KS);
-            contract(sa1, sb1, st + 1);
-            __syncthreads();
-            if (st + 1 >= last) break;
+        {
+            const int left = C - last * KS;
+            unroll<TA::NJ>([&](auto j) {
+                ld_lds16(ka + JA * j < left ? abase + last * astep + a_off(j) : zero, lds + 16 * THREADS * j);
+            });
+            unroll<TB::NJ>([&](auto j) {
+                ld_lds16(kb + JB * j < left ? bbase + last * bstep + boff[j] : zero,
+                         lds + TA::CHUNKS * 16 + 16 * THREADS * j);
+            });
         }
+        look_up(0);
+        if (last == 0) {
+            // no whole block to load: zeros
+            abase = bbase = zero;
+            astep = bstep = 0;
+#pragma unroll
+            for (int j = 0; j < TA::NJ; ++j) aoff[j] = 0;
+#pragma unroll
+            for (int j = 0; j < TB::NJ; ++j) boff[j] = 0;
+            if constexpr (MODE == kGradW)
+#pragma unroll
+                for (int j = 0; j < TA::NJ; ++j) rowoff[j] = 0;
+        }
+        // Step t contracts block t - 1 (step 0: the last) out of stage t % 2 and
+        // loads block t into the other one.  The last step has none to load and
+        // loads the one before it again: no branch between the matrix
+        // instructions.
+        for (int t = 0; t <= last; ++t) {
+            gmm_barrier<0>();
+            scales(t);
+            const int blk = max(min(t, last - 1), 0), to = ~t & 1;
+            contract(s_stage + (t & 1) * SC, [&](auto gi) {
+                // (in the earlier half of the groups: the later half covers the
+                // last loads' way)
+                constexpr int G = gi, OVER = NG < 2 ? NG : NG / 2;
+                if constexpr (G < OVER)
+                    unroll<(G + 1) * LOADS / OVER - G * LOADS / OVER>(
+                        [&](auto l) { load(std::integral_constant<int, G * LOADS / OVER + l>{}, blk, to); });
+            });
+            if (last > 0) look_up(min(t + 1, last - 1));
+        }
+        gmm_barrier<0>();
     }
 
     // lane (lm, lq) holds, of the 16 x 16 block (i, j), column lm (Q) and rows
@@ -437,12 +529,14 @@ inline long long gmm_grid(const GmmArgs &a) {
 }
 
 // Launches it; a grid beyond the runtime's 2^32 threads is refused.
+// Stages: 4 of 64 bytes; 2 of 128 bytes where the fp8 instructions want them or
+// a stage of 64 has less than a chunk for every thread.
 template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, bool WIDE = false>
 ts_status run_tiled(const char *name, const GmmArgs &a, hipStream_t st) {
     const long long grid = gmm_grid<MODE, BP, BQ>(a);
     if (grid * (64 * WP * WQ) >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
-    launch<GmmArgs>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, WIDE>, dim3((unsigned)grid), dim3(64 * WP * WQ),
-                    st, a);
+    launch<GmmArgs>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, 128, WIDE>, dim3((unsigned)grid),
+                    dim3(64 * WP * WQ), st, a);
     return check_launch(name);
 }
 
