@@ -154,12 +154,12 @@ namespace {
 
 template <GmmMode MODE>
 ts_status run_fp8(const char *name, const GmmArgs &a, hipStream_t st) {
-    if (gmm_wide<kGmmFp8>(a)) return run_tiled<kGmmFp8, MODE, false, 128, 128, 2, 2, true>(name, a, st);
+    if (gmm_wide<kGmmFp8>(a)) return run_tiled<kGmmFp8, MODE, false, 128, 128, 2, 2, 2, 2, true>(name, a, st);
     const int mean = a.rows / a.groups;
-    if (mean > 128) return run_tiled<kGmmFp8, MODE, false, 256, 256, 2, 4>(name, a, st);
-    if (mean > 48) return run_tiled<kGmmFp8, MODE, false, 128, 128, 2, 2>(name, a, st);
-    if (mean > 24) return run_tiled<kGmmFp8, MODE, false, 128, 64, 4, 1>(name, a, st);
-    return run_tiled<kGmmFp8, MODE, false, 128, 32, 4, 1>(name, a, st);
+    if (mean > 128) return run_tiled<kGmmFp8, MODE, false, 256, 256, 2, 4, 2, 2>(name, a, st);
+    if (mean > 48) return run_tiled<kGmmFp8, MODE, false, 128, 128, 2, 2, 2, 2>(name, a, st);
+    if (mean > 24) return run_tiled<kGmmFp8, MODE, false, 128, 64, 4, 1, 3, 3>(name, a, st);
+    return run_tiled<kGmmFp8, MODE, false, 128, 32, 4, 1, 4, 4>(name, a, st);
 }
 
 ts_status fp8_args(GmmArgs *a, const void *x, const float *x_scale, const void *w, const float *w_scale,

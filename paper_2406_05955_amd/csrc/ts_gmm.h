@@ -1,13 +1,13 @@
 // The tiled kernel of the grouped products (bf16, fp32, fp8 operands).
 //
-// A workgroup computes a BP x BQ tile of one group's output, contracting RB
+// A workgroup computes a BP x BQ tile of one group's output, contracting 128
 // bytes of both operands' rows per step.  Both operands go from global memory
-// straight into LDS (16 bytes a lane) through S stage buffers: S - 1 steps'
+// straight into LDS (16 bytes a lane), into rings of stages: the next steps'
 // loads are in flight behind the present step's matrix instructions, one
 // barrier a step.  Loads into LDS put lane i's 16 bytes at 16 i, so the layout
 // that keeps operand reads off each other's banks is made by choosing which
 // global chunk a lane fetches.
-//   row layout ([row][contraction]): LDS row of RB bytes, its chunks permuted
+//   row layout ([row][contraction]): LDS row of 128 bytes, its chunks permuted
 //     by the row's number; an operand register is one 16-byte read.
 //   column layout ([contraction][column], columns contiguous): LDS row of one
 //     contraction index, its 32-byte units (fp32: 64) permuted by the index;
@@ -60,6 +60,21 @@ __device__ __forceinline__ void ld_lds16(const char *base, uint32_t off, uint32_
                  : "memory", "m0");
 }
 __device__ __forceinline__ void ld_lds16(const char *base, size_t off, uint32_t l) { ld_lds16(base + off, l); }
+// A wave-uniform address in scalar registers.
+__device__ __forceinline__ const char *uniform(const void *p) {
+    const uint64_t v = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return reinterpret_cast<const char *>((uint64_t)hi << 32 | lo);
+}
+// 4 bytes a lane, at `l` + 4 x lane.
+__device__ __forceinline__ void ld_lds4(const char *base, uint32_t off, uint32_t l) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(l)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void ld_lds4(const char *base, size_t off, uint32_t l) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(base + off), "s"(l)
+                 : "memory", "m0");
+}
 
 // Inclusive sums and maxima over the wave's lanes (maxima of values >= 0):
 // inside rows of 16 lanes, then each row's last lane into the rows behind it.
@@ -104,10 +119,11 @@ struct GmmElem<kGmmFp8> {
     static constexpr int SZ = 1;
 };
 
-// One operand's share of a step: RB bytes of contraction (row layout's terms)
+// One operand's share of a step: RB = 128 bytes of contraction (row layout's terms)
 // of a tile of R rows (P or Q indices).
-template <GmmKind KIND, bool COL, int R, int RB, int THREADS>
+template <GmmKind KIND, bool COL, int R, int THREADS>
 struct GmmTile {
+    static constexpr int RB = 128;
     static constexpr int SZ = GmmElem<KIND>::SZ;
     static constexpr int KS = RB / SZ;                // contraction indices per step
     static constexpr int CHUNKS = R * RB / 16;        // 16-byte chunks per step
@@ -117,12 +133,11 @@ struct GmmTile {
     static constexpr int UC = KIND == kGmmF32 ? 4 : 2;  // and per 16-column unit
     static constexpr int NU = RC / UC;                // units per row (a power of two)
     static_assert(CHUNKS % THREADS == 0 && THREADS % 64 == 0, "whole waves load whole chunks");
-    static_assert(RB == 64 || RB == 128, "one or two 64-byte sub-steps");
 
     // row layout: what a row's chunks are permuted by: the 16 rows of a read
     // cover all 64 banks
     __device__ static __forceinline__ int rot(int row) {
-        return RB == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+        return (row >> 1) & 7;
     }
     // column layout: what a row's units are permuted by
     __device__ static __forceinline__ int perm(int kk) {
@@ -192,10 +207,6 @@ __device__ __forceinline__ void store4(void *out, int f32, size_t i, f32x4 v) {
 // dReLU of a gate and an up projection (strict comparisons: a NaN closes).
 __device__ __forceinline__ float drelu1(float g, float u) { return g > 0.f && u > 0.f ? g * u : 0.f; }
 
-__device__ __forceinline__ float ld_f32(const float *base, uint32_t bytes) {
-    return *reinterpret_cast<const float *>(reinterpret_cast<const char *>(base) + bytes);
-}
-
 // f(0), f(1), ... f(N - 1) with constants.
 template <int N, int I = 0, typename F>
 __device__ __forceinline__ void unroll(F f) {
@@ -205,22 +216,33 @@ __device__ __forceinline__ void unroll(F f) {
     }
 }
 
-// WP x WQ waves; a wave's tile is (BP / WP) x (BQ / WQ).  WIDE: x is 4 GB or
+constexpr int kStrip = 8;
+
+// WP x WQ waves; a wave's tile is (BP / WP) x (BQ / WQ).  AR, BR: stages of the P
+// operand (weights) and of the other; AR may be one more.  WIDE: x is 4 GB or
 // more, its rows' offsets take 64 bits.
-template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int RB, bool WIDE>
+template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int AR, int BR, bool WIDE>
 __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
     constexpr int THREADS = 64 * WP * WQ;
     constexpr bool BCOL = MODE == kGradW;
-    using TA = GmmTile<KIND, ACOL, BP, RB, THREADS>;
-    using TB = GmmTile<KIND, BCOL, BQ, RB, THREADS>;
-    constexpr int SZ = TA::SZ, KS = TA::KS;
+    using TA = GmmTile<KIND, ACOL, BP, THREADS>;
+    using TB = GmmTile<KIND, BCOL, BQ, THREADS>;
+    constexpr int SZ = TA::SZ, KS = TA::KS, RB = TA::RB;
     constexpr int MI = BP / WP / 16, MJ = BQ / WQ / 16;
     constexpr int PT = MODE == kDrelu ? BP / 2 : BP;  // output columns per tile
     static_assert(MODE != kGradW || ACOL, "the weight gradient contracts over rows");
     static_assert(MODE != kDrelu || (!ACOL && MI % 2 == 0), "gate and up in pairs of 16 rows");
 
-    constexpr int SC = TA::CHUNKS + TB::CHUNKS;  // chunks of a stage
-    __shared__ u32x4 s_stage[2 * SC];
+    static_assert(BR >= 2 && (AR == BR || AR == BR + 1), "P stages");
+    // fp8: a step's scales: NX waves fetch those of the rows, the others those
+    // of the tile's weight blocks
+    constexpr bool FP8 = KIND == kGmmFp8;
+    constexpr int NX = BQ < 64 ? 1 : BQ / 64, SS = FP8 ? THREADS : 0;
+    static_assert(!FP8 || THREADS / 64 >= NX + 2, "two waves for weight scales");
+    constexpr int ALL = AR * TA::CHUNKS + BR * TB::CHUNKS + BR * SS / 4;
+    __shared__ u32x4 s_a[ALL];
+    u32x4 *const s_b = s_a + AR * TA::CHUNKS;
+    const float *const s_s = reinterpret_cast<const float *>(s_b + BR * TB::CHUNKS);
 
     const int tid = threadIdx.x, lane = tid & 63, lm = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -241,10 +263,10 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
         const int per = (total + 7) / 8;
         const int slot = blockIdx.x / 8, id = (blockIdx.x % 8) * per + slot;
         if (slot >= per || id >= total) return;
-        // strips of up to 4 Q tiles, P tile by P tile
-        const int strip = id / (4 * npt), r = id - strip * 4 * npt;
-        const int sw = min(4, nqt - strip * 4);
-        const int qt = strip * 4 + r % sw;
+        // strips of up to kStrip Q tiles, P tile by P tile
+        const int strip = id / (kStrip * npt), r = id - strip * kStrip * npt;
+        const int sw = min(kStrip, nqt - strip * kStrip);
+        const int qt = strip * kStrip + r % sw;
         pt = r / sw;
         if constexpr (MODE == kGradW) {
             const int per_g = (a.n + BQ - 1) / BQ;
@@ -278,48 +300,13 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
     };
     f32x4 acc[MI][MJ] = {};
 
-    // fp8: the scales of this lane's columns and this wave's rows, a block ahead
-    uint32_t xso[MJ], wso = 0;
-    float sx[MJ] = {}, sw[2] = {0.f, 0.f};
-    if constexpr (KIND == kGmmFp8) {
-        const int kbn = (a.k + kScaleBlock - 1) / kScaleBlock, nbn = (a.n + kScaleBlock - 1) / kScaleBlock;
-        // (32 times fewer bytes than x: 32 bits wherever x's offsets have them)
-#pragma unroll
-        for (int j = 0; j < MJ; ++j)
-            xso[j] = 4u * (uint32_t)source(min(q0 + (wq * MJ + j) * 16 + lm, e - 1)) * (uint32_t)kbn;
-        const int nb = min((p0 + wp * (PT / WP)) / kScaleBlock, nbn - 1);
-        // (a matrix has below 4 GB / 2^14 scales, 64 groups of it 32 bits' worth;
-        // a vector load: a scalar one would be waited for with the LDS reads)
-        wso = 4u * (uint32_t)((g * nbn + nb) * kbn);
-        asm volatile("" : "+v"(wso));
-    }
-    float f[2][MJ];
-    // fp8: the present block's factors; asks for the scales of block `next`
-    auto scales = [&](int next) {
-        if constexpr (KIND == kGmmFp8) {
-#pragma unroll
-            for (int j = 0; j < MJ; ++j) {
-                f[0][j] = sx[j] * sw[0];
-                f[1][j] = MODE == kDrelu ? sx[j] * sw[1] : f[0][j];
-                // (computed here: behind the next stage's loads, the wait for
-                // the scales would be one for those too)
-                asm volatile("" : "+v"(f[0][j]), "+v"(f[1][j]));
-            }
-#pragma unroll
-            for (int j = 0; j < MJ; ++j) sx[j] = ld_f32(a.xs, xso[j] + 4u * next);
-            sw[0] = ld_f32(a.ws[0], wso + 4u * next);
-            if constexpr (MODE == kDrelu) sw[1] = ld_f32(a.ws[1], wso + 4u * next);
-        }
-    };
-
     const int last = blocks - 1;
-    // Contracts the stage in `A`.  Groups of MJ matrix instructions (one block
+    // Contracts the stages A, B.  Groups of MJ matrix instructions (one block
     // of 16 P rows, one sub-step); operand reads run a group or two (where the registers allow) ahead, and
     // between(group) issues the next stages' loads spread over the groups: all
     // at once they hold up the waves that issue them.
     constexpr int NS = KIND == kGmmFp8 ? 1 : RB / 64, NG = NS * MI;
-    auto contract = [&](const u32x4 *A, auto between) {
-        const u32x4 *B = A + TA::CHUNKS;
+    auto contract = [&](const u32x4 *A, const u32x4 *B, [[maybe_unused]] const float *scale, auto between) {
         using Frag = std::conditional_t<KIND == kGmmFp8, i32x8, u32x4>;
         auto read = [&](auto tile, const u32x4 *t, int blk, int s) -> Frag {
             using T = decltype(tile);
@@ -337,6 +324,18 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
         unroll<AHEAD>([&](auto gi) {
             if constexpr (gi < NG) af[gi] = read(TA{}, A, wp * MI + gi % MI, gi / MI);
         });
+        // the factors of this lane's columns (dReLU: for gate and for up)
+        [[maybe_unused]] float f[2][MJ];
+        if constexpr (FP8) {
+            const int sel = MODE == kDrelu ? 0 : wp * (BP / WP) / kScaleBlock;
+            const float w0 = scale[(NX + sel) * 64 + lane], w1 = MODE == kDrelu ? scale[(NX + 1) * 64 + lane] : w0;
+#pragma unroll
+            for (int j = 0; j < MJ; ++j) {
+                const float x = scale[(wq * MJ + j) * 16 + lm];
+                f[0][j] = x * w0;
+                f[1][j] = x * w1;
+            }
+        }
         unroll<NG>([&](auto gi) {
             constexpr int G = gi, s = G / MI, i = G % MI;
             constexpr int NX = G + AHEAD;
@@ -426,28 +425,40 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
             if constexpr (MODE == kGradW) return (Off)(rowoff[j] + aoff[j]);
             else return aoff[j];
         };
-        const uint32_t lds = lds_addr(s_stage) + wave * 1024;
-        constexpr int LOADS = TA::NJ + TB::NJ;  // of a stage, per wave
-        // load L of a whole block into stage `to`
-        auto load = [&](auto l, int blk, int to) {
-            constexpr int L = l, J = L < TA::NJ ? L : L - TA::NJ;
-            const uint32_t at = lds + (uint32_t)to * (SC * 16) + 16 * THREADS * J;
-            if constexpr (L < TA::NJ)
-                ld_lds16(abase + blk * astep, a_off(std::integral_constant<int, J>{}), at);
-            else
-                ld_lds16(bbase + blk * bstep, boff[J], at + TA::CHUNKS * 16);
+        const uint32_t lds_a = lds_addr(s_a) + wave * 1024, lds_b = lds_a + AR * TA::CHUNKS * 16;
+        [[maybe_unused]] const uint32_t lds_s = lds_addr(s_s) + wave * 256;
+        // this wave's scales: a row's (or a weight block's) are one after another
+        const float *sbase = a.xs;
+        Off soff = 0;
+        if constexpr (FP8) {
+            const int kbn = (a.k + kScaleBlock - 1) / kScaleBlock, nbn = (a.n + kScaleBlock - 1) / kScaleBlock;
+            if (wave < NX) {
+                soff = (Off)source(min(q0 + wave * 64 + lane, e - 1)) * (Off)(4 * kbn);
+            } else {
+                const int sel = (wave - NX) & 1;
+                const int nb = min(p0 / kScaleBlock + (MODE == kDrelu ? 0 : sel), nbn - 1);
+                sbase = (MODE == kDrelu && sel ? a.ws[1] : a.ws[0]) + ((size_t)g * nbn + nb) * kbn;
+            }
+        }
+        constexpr int LOADS_A = TA::NJ, LOADS_B = TB::NJ + FP8, LOADS = LOADS_A + LOADS_B;  // of a stage, per wave
+        auto load_a = [&](auto j, int blk, int to) {
+            ld_lds16(abase + blk * astep, a_off(j), lds_a + (uint32_t)(to * TA::CHUNKS + THREADS * j) * 16);
+        };
+        auto load_b = [&](auto j, int blk, int to) {
+            if constexpr (j == TB::NJ)
+                ld_lds4(uniform(sbase + blk), soff, lds_s + (uint32_t)(to * SS) * 4);
+            else ld_lds16(bbase + blk * bstep, boff[j], lds_b + (uint32_t)(to * TB::CHUNKS + THREADS * j) * 16);
         };
 
         look_up(last);
-        scales(last);
         {
             const int left = C - last * KS;
-            unroll<TA::NJ>([&](auto j) {
-                ld_lds16(ka + JA * j < left ? abase + last * astep + a_off(j) : zero, lds + 16 * THREADS * j);
-            });
             unroll<TB::NJ>([&](auto j) {
-                ld_lds16(kb + JB * j < left ? bbase + last * bstep + boff[j] : zero,
-                         lds + TA::CHUNKS * 16 + 16 * THREADS * j);
+                ld_lds16(kb + JB * j < left ? bbase + last * bstep + boff[j] : zero, lds_b + 16 * THREADS * j);
+            });
+            if constexpr (FP8) load_b(std::integral_constant<int, TB::NJ>{}, last, 0);
+            unroll<TA::NJ>([&](auto j) {
+                ld_lds16(ka + JA * j < left ? abase + last * astep + a_off(j) : zero, lds_a + 16 * THREADS * j);
             });
         }
         look_up(0);
@@ -463,23 +474,36 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
 #pragma unroll
                 for (int j = 0; j < TA::NJ; ++j) rowoff[j] = 0;
         }
-        // Step t contracts block t - 1 (step 0: the last) out of stage t % 2 and
-        // loads block t into the other one.  The last step has none to load and
-        // loads the one before it again: no branch between the matrix
-        // instructions.
+        // Step t contracts block t - 1 (step 0: the last) and loads block t + BR
+        // - 2 of the other operand and t + AR - 2 of the P operand into the
+        // stages that step t - 1 read.  The last steps have none to load and load
+        // the last whole one again: no branch between the matrix instructions.
+        auto whole = [&](int blk) { return max(min(blk, last - 1), 0); };
+        unroll<AR - 2>([&](auto i) {
+            if constexpr (i < BR - 2) unroll<LOADS_B>([&](auto j) { load_b(j, whole(i), i + 1); });
+            unroll<LOADS_A>([&](auto j) { load_a(j, whole(i), i + 1); });
+        });
+        int ar = 0, br = 0;  // stages of step t
         for (int t = 0; t <= last; ++t) {
-            gmm_barrier<0>();
-            scales(t);
-            const int blk = max(min(t, last - 1), 0), to = ~t & 1;
-            contract(s_stage + (t & 1) * SC, [&](auto gi) {
-                // (in the earlier half of the groups: the later half covers the
-                // last loads' way)
-                constexpr int G = gi, OVER = NG < 2 ? NG : NG / 2;
+            // what may be on its way: all that was asked for behind this step's
+            gmm_barrier<(AR == BR ? (BR - 2) * LOADS : (BR - 2) * LOADS + LOADS_A)>();
+            const int blk_a = whole(t + AR - 2), blk_b = whole(t + BR - 2);
+            const int to_a = ar == 0 ? AR - 1 : ar - 1, to_b = br == 0 ? BR - 1 : br - 1;
+            contract(s_a + ar * TA::CHUNKS, s_b + br * TB::CHUNKS, s_s + br * SS, [&](auto gi) {
+                // (in the earlier half of the groups, the later half covers the
+                // last loads' way: gate + up at 8192 tokens 2.98 ms, spread over
+                // all groups 3.06; fp8, whose groups are twice as long, 2.36 / 2.30)
+                constexpr int G = gi, OVER = FP8 || NG < 2 ? NG : NG / 2;
                 if constexpr (G < OVER)
-                    unroll<(G + 1) * LOADS / OVER - G * LOADS / OVER>(
-                        [&](auto l) { load(std::integral_constant<int, G * LOADS / OVER + l>{}, blk, to); });
+                    unroll<(G + 1) * LOADS / OVER - G * LOADS / OVER>([&](auto l) {
+                        constexpr int L = G * LOADS / OVER + l;
+                        if constexpr (L < LOADS_B) load_b(std::integral_constant<int, L>{}, blk_b, to_b);
+                        else load_a(std::integral_constant<int, L - LOADS_B>{}, blk_a, to_a);
+                    });
             });
-            if (last > 0) look_up(min(t + 1, last - 1));
+            if (last > 0) look_up(whole(t + 1));
+            ar = ar == AR - 1 ? 0 : ar + 1;
+            br = br == BR - 1 ? 0 : br + 1;
         }
         gmm_barrier<0>();
     }
@@ -529,13 +553,11 @@ inline long long gmm_grid(const GmmArgs &a) {
 }
 
 // Launches it; a grid beyond the runtime's 2^32 threads is refused.
-// Stages: 4 of 64 bytes; 2 of 128 bytes where the fp8 instructions want them or
-// a stage of 64 has less than a chunk for every thread.
-template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, bool WIDE = false>
+template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int AR, int BR, bool WIDE = false>
 ts_status run_tiled(const char *name, const GmmArgs &a, hipStream_t st) {
     const long long grid = gmm_grid<MODE, BP, BQ>(a);
     if (grid * (64 * WP * WQ) >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
-    launch<GmmArgs>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, 128, WIDE>, dim3((unsigned)grid),
+    launch<GmmArgs>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, AR, BR, WIDE>, dim3((unsigned)grid),
                     dim3(64 * WP * WQ), st, a);
     return check_launch(name);
 }
