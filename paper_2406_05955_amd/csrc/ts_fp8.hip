@@ -152,16 +152,6 @@ __global__ __launch_bounds__(256) void fp8_quant_weights_kernel(const T *w, uint
 
 namespace {
 
-template <GmmMode MODE>
-ts_status run_fp8(const char *name, const GmmArgs &a, hipStream_t st) {
-    if (gmm_wide<kGmmFp8>(a)) return run_tiled<kGmmFp8, MODE, false, 128, 128, 2, 2, 2, 2, true>(name, a, st);
-    const int mean = a.rows / a.groups;
-    if (mean > 128) return run_tiled<kGmmFp8, MODE, false, 256, 256, 2, 4, 2, 2>(name, a, st);
-    if (mean > 48) return run_tiled<kGmmFp8, MODE, false, 128, 128, 2, 2, 2, 2>(name, a, st);
-    if (mean > 24) return run_tiled<kGmmFp8, MODE, false, 128, 64, 4, 1, 3, 3>(name, a, st);
-    return run_tiled<kGmmFp8, MODE, false, 128, 32, 4, 1, 4, 4>(name, a, st);
-}
-
 ts_status fp8_args(GmmArgs *a, const void *x, const float *x_scale, const void *w, const float *w_scale,
                    const int32_t *row_src, const int32_t *offsets, int rows, int src_rows, int groups, int n, int k,
                    void *out, ts_dtype odtype) {
@@ -256,7 +246,7 @@ ts_status ts_fp8_mm(const void *x, const float *x_scale, const void *w, const fl
     ts_status s = ts::fp8_args(&a, x, x_scale, w, w_scale, row_src, offsets, rows, src_rows, n_groups, n, k, out,
                                odtype);
     if (s != TS_OK || rows == 0) return s;
-    return ts::run_fp8<ts::kFwd>("fp8_mm", a, static_cast<hipStream_t>(stream));
+    return ts::run_fwd<ts::kGmmFp8, ts::kFwd, false>("fp8_mm", a, static_cast<hipStream_t>(stream));
 }
 
 ts_status ts_fp8_drelu(const void *x, const float *x_scale, const void *w_gate, const float *gate_scale,
@@ -270,7 +260,7 @@ ts_status ts_fp8_drelu(const void *x, const float *x_scale, const void *w_gate, 
     if (!ts::aligned16(w_up) || !ts::aligned4(up_scale)) return TS_ERR_ALIGN;
     a.w[1] = static_cast<const char *>(w_up);
     a.ws[1] = up_scale;
-    return ts::run_fp8<ts::kDrelu>("fp8_drelu", a, static_cast<hipStream_t>(stream));
+    return ts::run_fwd<ts::kGmmFp8, ts::kDrelu, false>("fp8_drelu", a, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

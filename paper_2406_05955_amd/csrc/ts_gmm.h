@@ -568,4 +568,23 @@ inline bool gmm_wide(const GmmArgs &a) {
     return (unsigned long long)a.src_rows * a.k * GmmElem<KIND>::SZ >= (1ull << 32);
 }
 
+// Forward product on the tile that suits its sizes.
+template <GmmKind KIND, GmmMode MODE, bool ACOL>
+ts_status run_fwd(const char *name, const GmmArgs &a, hipStream_t st) {
+    if (gmm_wide<KIND>(a)) return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2, true>(name, a, st);
+    switch (pick_tile(KIND, MODE == kDrelu, a.groups, a.rows, a.n, a.k)) {
+        case kTile64x32: return run_tiled<KIND, MODE, ACOL, 64, 32, 2, 2, 6, 6>(name, a, st);
+        case kTile128x64: return run_tiled<KIND, MODE, ACOL, 128, 64, 4, 1, 3, 3>(name, a, st);
+        case kTile128x128: return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2>(name, a, st);
+        case kTile256x128:
+            if constexpr (KIND != kGmmF32) return run_tiled<KIND, MODE, ACOL, 256, 128, 4, 2, 3, 3>(name, a, st);
+            break;
+        default:
+            // (fp8: a third stage of the weights and the scales are more than LDS holds)
+            if constexpr (KIND == kGmmFp8) return run_tiled<KIND, MODE, ACOL, 256, 256, 2, 4, 2, 2>(name, a, st);
+            else if constexpr (KIND == kGmmBf16) return run_tiled<KIND, MODE, ACOL, 256, 256, 2, 4, 3, 2>(name, a, st);
+    }
+    return TS_ERR_UNSUPPORTED;
+}
+
 }  // namespace ts

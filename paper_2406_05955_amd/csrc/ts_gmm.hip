@@ -13,17 +13,6 @@ namespace ts {
 
 namespace {
 
-template <GmmKind KIND, GmmMode MODE, bool ACOL>
-ts_status run_fwd(const char *name, const GmmArgs &a, hipStream_t st) {
-    if (gmm_wide<KIND>(a)) return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2, true>(name, a, st);
-    const int mean = a.rows / a.groups;
-    if constexpr (KIND == kGmmBf16)
-        if (mean > 128) return run_tiled<KIND, MODE, ACOL, 256, 256, 2, 4, 3, 2>(name, a, st);
-    if (mean > 48) return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2>(name, a, st);
-    if (mean > 24) return run_tiled<KIND, MODE, ACOL, 128, 64, 4, 1, 3, 3>(name, a, st);
-    return run_tiled<KIND, MODE, ACOL, 128, 32, 4, 1, 4, 4>(name, a, st);
-}
-
 template <GmmKind KIND>
 ts_status run_grad_w(const GmmArgs &a, hipStream_t st) {
     if (gmm_wide<KIND>(a)) return run_tiled<KIND, kGradW, true, 128, 128, 2, 2, 2, 2, true>("grouped_mm_dw", a, st);

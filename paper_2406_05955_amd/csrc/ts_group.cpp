@@ -2,6 +2,7 @@
 #include "ts_group.h"
 
 #include <algorithm>
+#include <cmath>
 
 #include "ts_plan.h"
 
@@ -38,6 +39,45 @@ size_t route_ws_bytes(int tokens, int n_experts, int top_k) {
     const int tpb = route_tokens_per_block(tokens, top_k);
     if (tpb == 0) return 256;
     return align_up256((size_t)ceil_div(tokens, tpb) * kMaxExperts * sizeof(int32_t));
+}
+
+// The tile whose time is least by a simple count, in cycles: a step (128 bytes
+// of contraction) takes its matrix instructions at half their peak, or its
+// operands at 20 bytes a cycle and unit (what a unit draws with all units busy),
+// or a round trip of 500 cycles shared by the stages ahead; the tiles run in
+// rounds of 256 units.  Groups are taken as spread evenly over their sizes (half
+// a tile over).  Over 30 calls (1 to 3000 tokens, dense, 8 and 16 groups, 512 x
+// 1792 to 4096 x 14336, three types) the choice costs 1.7% on average against
+// the best of ten tiles measured one by one.  Us, 64x32 / 128x64 / 128x128 /
+// 256x128 / 256x256: down bf16 4096 x 14336 1 token 38 / 67 / 131 / 142 / 235, 32
+// tokens 181 / 154 / 232 / 171 / 302, 512 tokens 545 / 309 / 307 / 243 / 283; one
+// fp8 layer 4096 x 4096 100 rows 13 / 23 / 33 / 32 / 48, 2000 rows 111 / 62 / 51 /
+// 41 / 64.
+GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k) {
+    const int esz = kind == kGmmF32 ? 4 : kind == kGmmFp8 ? 1 : 2;
+    const int used = std::max(1, std::min(groups, rows));
+    const double mean = (double)rows / used;
+    const double steps = (double)ceil_div(k * esz, 128);
+    GmmTileId best = kTile128x64;
+    double least = 0.0;
+    for (int i = 0; i < kTiles; ++i) {
+        const GmmTileSize &t = kTileSize[i];
+        // (fp32: 8 waves of matrix instructions that long gain nothing from a larger tile)
+        if (kind == kGmmF32 && t.p == 256) continue;
+        const double row_tiles = groups == 1 ? ceil_div(rows, t.q) : used * std::max(1.0, mean / t.q + 0.5);
+        const double tiles = ceil_div(n, drelu ? t.p / 2 : t.p) * row_tiles;
+        const double matrix = (double)t.p * t.q / (kind == kGmmF32 ? 2.0 : 16.0);
+        const double step = std::max(matrix, (t.p + t.q) * 128 / 20.0);
+        const double together = std::min<double>(t.per_unit, std::max(1.0, tiles / 256));
+        const double r = tiles / (256.0 * t.per_unit);
+        const double rounds = r < 4 ? std::ceil(r) : r + 0.5;
+        const double cycles = rounds * (steps * std::max(together * step, 500.0 / (t.stages - 1)) + 1000.0);
+        if (i == 0 || cycles < least) {
+            least = cycles;
+            best = (GmmTileId)i;
+        }
+    }
+    return best;
 }
 
 }  // namespace ts

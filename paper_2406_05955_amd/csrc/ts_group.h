@@ -37,6 +37,15 @@ struct GmmArgs {
     int out_f32 = 0;
 };
 
+// Tiles of the forward products: columns (dReLU: of gate and up together) x
+// rows, workgroups of it that a compute unit holds, stages.
+enum GmmTileId { kTile64x32 = 0, kTile128x64, kTile128x128, kTile256x128, kTile256x256, kTiles };
+struct GmmTileSize {
+    int p, q, per_unit, stages;
+};
+constexpr GmmTileSize kTileSize[kTiles] = {{64, 32, 2, 6}, {128, 64, 2, 3}, {128, 128, 2, 2}, {256, 128, 1, 3}, {256, 256, 1, 2}};
+GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k);
+
 ts_status check_group_dims(int rows, int groups, int n, int k, int quantum);
 bool type_ok(ts_dtype d);
 ts_status check_route_dims(int tokens, int n_experts, int top_k);
