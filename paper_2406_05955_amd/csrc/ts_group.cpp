@@ -72,7 +72,7 @@ GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k
         const double r = tiles / (256.0 * t.per_unit);
         const double rounds = r < 4 ? std::ceil(r) : r + 0.5;
         const double cycles = rounds * (steps * std::max(together * step, 500.0 / (t.stages - 1)) + 1000.0);
-        if (i == 0 || cycles < least) {
+        if (least == 0.0 || cycles < least) {
             least = cycles;
             best = (GmmTileId)i;
         }

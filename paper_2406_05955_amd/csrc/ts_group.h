@@ -39,11 +39,11 @@ struct GmmArgs {
 
 // Tiles of the forward products: columns (dReLU: of gate and up together) x
 // rows, workgroups of it that a compute unit holds, stages.
-enum GmmTileId { kTile64x32 = 0, kTile128x64, kTile128x128, kTile256x128, kTile256x256, kTiles };
+enum GmmTileId { kTile256x256 = 0, kTile128x128, kTile128x64, kTile64x32, kTile256x128, kTiles };  // equals: the first
 struct GmmTileSize {
     int p, q, per_unit, stages;
 };
-constexpr GmmTileSize kTileSize[kTiles] = {{64, 32, 2, 6}, {128, 64, 2, 3}, {128, 128, 2, 2}, {256, 128, 1, 3}, {256, 256, 1, 2}};
+constexpr GmmTileSize kTileSize[kTiles] = {{256, 256, 1, 2}, {128, 128, 2, 2}, {128, 64, 2, 3}, {64, 32, 2, 6}, {256, 128, 1, 3}};
 GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k);
 
 ts_status check_group_dims(int rows, int groups, int n, int k, int quantum);
