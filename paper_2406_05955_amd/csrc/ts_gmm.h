@@ -295,6 +295,8 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
     constexpr int JB = BCOL ? THREADS / TB::RC : 0;
     using Off = std::conditional_t<WIDE, size_t, uint32_t>;  // of a row of x
     const Off xrow = (Off)a.k * SZ;
+    [[maybe_unused]] const auto *row_src =
+        (const __attribute__((address_space(4))) int32_t *)(reinterpret_cast<uintptr_t>(a.row_src));
     auto source = [&](int r) {
         return a.row_src ? min(max(a.row_src[r], 0), a.src_rows - 1) : min(r, a.src_rows - 1);
     };
@@ -414,12 +416,40 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
             else
                 boff[j] = (Off)source(min(q0 + row, e - 1)) * xrow + ch * 16;
         }
-        // weight gradient: the offsets of block blk's rows of x
-        auto look_up = [&](int blk) {
-            if constexpr (MODE == kGradW)
+        // Weight gradient: the offsets of block blk's rows of x.  A wave's loads
+        // are of 64 / RC rows each, looked up with scalar loads (vector ones
+        // return in order with the stages and would be waited for with them),
+        // asked for at a step's start and taken at its end (one after another
+        // their round trips doubled the step).
+        constexpr int RPW = MODE == kGradW ? 64 / TA::RC : 1, NR = MODE == kGradW ? TA::NJ * RPW : 1;
+        static_assert(MODE != kGradW || RPW == 2 || RPW == 4, "rows of a wave's load");
+        int row[NR];
+        auto ask = [&](int blk) {
+            if constexpr (MODE == kGradW) {
+                const int r0 = b + blk * KS + wave * RPW;
 #pragma unroll
-                for (int j = 0; j < TA::NJ; ++j)
-                    rowoff[j] = (Off)source(b + min(blk * KS + ka + JA * j, C - 1)) * xrow;
+                for (int i = 0; i < NR; ++i) row[i] = min(r0 + JA * (i / RPW) + i % RPW, b + C - 1);
+                if (a.row_src) {
+                    int v[NR];
+#pragma unroll
+                    for (int i = 0; i < NR; ++i) v[i] = row_src[row[i]];
+#pragma unroll
+                    for (int i = 0; i < NR; ++i) row[i] = v[i];
+                }
+            }
+        };
+        auto take = [&] {
+            if constexpr (MODE == kGradW) {
+                unroll<TA::NJ>([&](auto j) {
+                    Off o[RPW];
+#pragma unroll
+                    for (int h = 0; h < RPW; ++h)
+                        o[h] = (Off)min(max(row[j * RPW + h], 0), a.src_rows - 1) * xrow;
+                    const int h = lane / TA::RC;
+                    if constexpr (RPW == 4) rowoff[j] = h & 2 ? (h & 1 ? o[3] : o[2]) : (h & 1 ? o[1] : o[0]);
+                    else rowoff[j] = h ? o[1] : o[0];
+                });
+            }
         };
         auto a_off = [&](auto j) {
             if constexpr (MODE == kGradW) return (Off)(rowoff[j] + aoff[j]);
@@ -450,7 +480,8 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
             else ld_lds16(bbase + blk * bstep, boff[j], lds_b + (uint32_t)(to * TB::CHUNKS + THREADS * j) * 16);
         };
 
-        look_up(last);
+        ask(last);
+        take();
         {
             const int left = C - last * KS;
             unroll<TB::NJ>([&](auto j) {
@@ -461,7 +492,6 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
                 ld_lds16(ka + JA * j < left ? abase + last * astep + a_off(j) : zero, lds_a + 16 * THREADS * j);
             });
         }
-        look_up(0);
         if (last == 0) {
             // no whole block to load: zeros
             abase = bbase = zero;
@@ -481,13 +511,22 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
         auto whole = [&](int blk) { return max(min(blk, last - 1), 0); };
         unroll<AR - 2>([&](auto i) {
             if constexpr (i < BR - 2) unroll<LOADS_B>([&](auto j) { load_b(j, whole(i), i + 1); });
+            if (last > 0) {
+                ask(whole(i));
+                take();
+            }
             unroll<LOADS_A>([&](auto j) { load_a(j, whole(i), i + 1); });
         });
+        if (last > 0) {
+            ask(whole(AR - 2));
+            take();
+        }
         int ar = 0, br = 0;  // stages of step t
         for (int t = 0; t <= last; ++t) {
             // what may be on its way: all that was asked for behind this step's
             gmm_barrier<(AR == BR ? (BR - 2) * LOADS : (BR - 2) * LOADS + LOADS_A)>();
             const int blk_a = whole(t + AR - 2), blk_b = whole(t + BR - 2);
+            ask(whole(t + AR - 1));
             const int to_a = ar == 0 ? AR - 1 : ar - 1, to_b = br == 0 ? BR - 1 : br - 1;
             contract(s_a + ar * TA::CHUNKS, s_b + br * TB::CHUNKS, s_s + br * SS, [&](auto gi) {
                 // (in the earlier half of the groups, the later half covers the
@@ -501,7 +540,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
                         else load_a(std::integral_constant<int, L - LOADS_B>{}, blk_a, to_a);
                     });
             });
-            if (last > 0) look_up(whole(t + 1));
+            if (last > 0) take();
             ar = ar == AR - 1 ? 0 : ar + 1;
             br = br == BR - 1 ? 0 : br + 1;
         }
