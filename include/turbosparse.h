@@ -296,7 +296,8 @@ ts_status ts_moe_dense(const float *x, const void *w_router, const void *w_gate,
  *     every run.  Outputs must not overlap inputs.
  */
 
-/* Workspace bytes of ts_moe_route / ts_moe_group (0 if out of range). */
+/* Workspace bytes of ts_moe_route / ts_moe_group (0: none is needed, or out of
+ * range). */
 size_t ts_moe_route_workspace_bytes(int tokens, int n_experts, int top_k);
 
 /*

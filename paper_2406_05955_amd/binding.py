@@ -467,6 +467,12 @@ def moe_route_workspace_bytes(tokens: int, n_experts: int, top_k: int) -> int:
     return int(lib.ts_moe_route_workspace_bytes(tokens, n_experts, top_k))
 
 
+def _route_ws(dev, ws, T, E, K):
+    """A workspace where the call needs one (small calls do not)."""
+    n = 0 if ws is not None else moe_route_workspace_bytes(T, E, K)
+    return torch.empty(n, dtype=torch.uint8, device=dev) if n else ws
+
+
 def _maps(T, E, K, dev):
     return (torch.empty(E + 1, dtype=_i32, device=dev), torch.empty(T * K, dtype=_i32, device=dev),
             torch.empty(T, K, dtype=_i32, device=dev))
@@ -485,7 +491,7 @@ def moe_route(logits, top_k: int, maps: bool = True, ws=None, stream=None):
     idx, w = torch.empty(T, K, dtype=_i32, device=dev), torch.empty(T, K, dtype=_f32, device=dev)
     m = _maps(T, E, K, dev) if maps else (None, None, None)
     if maps:
-        ws = _workspace(moe_route_workspace_bytes, dev, ws, T, E, K)
+        ws = _route_ws(dev, ws, T, E, K)
     code = lib.ts_moe_route(_ptr(logits), T, E, K, _ptr(idx), _ptr(w), _ptr(m[0]), _ptr(m[1]), _ptr(m[2]), _ptr(ws),
                             _nbytes(ws) if ws is not None else 0, st)
     if code:
@@ -503,8 +509,9 @@ def moe_group(topk_idx, n_experts: int, ws=None, stream=None):
     if E < 1:
         raise ValueError(f"n_experts must be positive, got {E}")
     m = _maps(T, E, K, topk_idx.device)
-    ws = _workspace(moe_route_workspace_bytes, topk_idx.device, ws, T, E, K)
-    code = lib.ts_moe_group(_ptr(topk_idx), T, E, K, _ptr(m[0]), _ptr(m[1]), _ptr(m[2]), _ptr(ws), _nbytes(ws), st)
+    ws = _route_ws(topk_idx.device, ws, T, E, K)
+    code = lib.ts_moe_group(_ptr(topk_idx), T, E, K, _ptr(m[0]), _ptr(m[1]), _ptr(m[2]), _ptr(ws),
+                            _nbytes(ws) if ws is not None else 0, st)
     if code:
         _check(code, "ts_moe_group")
     return m

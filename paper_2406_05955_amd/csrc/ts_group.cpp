@@ -27,17 +27,17 @@ ts_status check_route_dims(int tokens, int n_experts, int top_k) {
     return TS_OK;
 }
 
-// At most 256 workgroups, of at least 256 tokens: each adds up all their
-// counts (64 KB) for itself.
+// At most 256 workgroups, one per unit: each adds up all their counts (64 KB)
+// for itself.  At least 64 tokens, four a wave.
 int route_tokens_per_block(int tokens, int top_k) {
     if ((long long)tokens * top_k <= kRouteOneMax) return 0;
-    return std::max(256, ceil_div(ceil_div(tokens, 256), 64) * 64);
+    return std::max(64, ceil_div(ceil_div(tokens, 256), 16) * 16);
 }
 
 size_t route_ws_bytes(int tokens, int n_experts, int top_k) {
     if (check_route_dims(tokens, n_experts, top_k) != TS_OK) return 0;
     const int tpb = route_tokens_per_block(tokens, top_k);
-    if (tpb == 0) return 256;
+    if (tpb == 0) return 0;
     return align_up256((size_t)ceil_div(tokens, tpb) * kMaxExperts * sizeof(int32_t));
 }
 

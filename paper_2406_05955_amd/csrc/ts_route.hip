@@ -59,54 +59,39 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
     return max(max(a, b), max(c, d));
 }
 
-// One token by one wave, lane e holding expert e's logit: K times the largest
-// that is left (ties: the lowest lane), then their softmax.  A token with
-// nothing but -inf (or NaN) chooses the lowest experts, with weights of zero.
-// Lane k returns choice k and its weight.
-__device__ __forceinline__ void route_token(const RouteArgs &a, float logit, int lane, int &my_idx, float &my_w) {
-    uint32_t key = lane < a.E ? logit_key(logit) : 0u;
-    uint32_t my_key = 0x007fffffu;
-    float m = 0.f;
-    my_idx = 0;
-    for (int k = 0; k < a.K; ++k) {
-        const uint32_t top = wave_umax(key);
-        const int who = __ffsll((unsigned long long)__ballot(key == top)) - 1;
-        if (k == 0) m = key_logit(top);
-        if (lane == k) {
-            my_idx = who;
-            my_key = top;
-        }
-        if (lane == who) key = 0u;
+// U tokens by one wave, lane e holding expert e's logits: K times the largest
+// that is left (ties: the lowest lane), then their softmax; the tokens' chains
+// run side by side.  A token with nothing but -inf (or NaN) chooses the lowest
+// experts, with weights of zero.  Lane k returns choice k and its weight.
+template <int U>
+__device__ __forceinline__ void route_tokens(const RouteArgs &a, const float (&logit)[U], int lane, int (&my_idx)[U],
+                                             float (&my_w)[U]) {
+    uint32_t key[U], my_key[U];
+    float m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        key[u] = lane < a.E ? logit_key(logit[u]) : 0u;
+        my_key[u] = 0x007fffffu;
+        my_idx[u] = 0;
     }
-    const float l = key_logit(my_key);
-    // equal to the largest: 1 (inf - inf is no number)
-    float e = lane < a.K && m > -INFINITY ? (l == m ? 1.f : expf(l - m)) : 0.f;
-    const float sum = wave_sum(e);
-    my_w = sum > 0.f ? e / sum : 0.f;
-}
-
-// Routes tokens [t0, t1) of this workgroup.
-__device__ __forceinline__ void route_tokens(const RouteArgs &a, int t0, int t1, int wave, int lane) {
-    // (four tokens' logits in flight per wave)
-    for (int t = t0 + wave; t < t1; t += 4 * kRouteWaves) {
-        float l[4];
+    for (int k = 0; k < a.K; ++k) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int tt = t + u * kRouteWaves;
-            l[u] = tt < t1 && lane < a.E ? a.logits[(size_t)tt * a.E + lane] : 0.f;
+        for (int u = 0; u < U; ++u) {
+            const uint32_t top = wave_umax(key[u]);
+            const int who = __ffsll((unsigned long long)__ballot(key[u] == top)) - 1;
+            if (k == 0) m[u] = key_logit(top);
+            my_idx[u] = lane == k ? who : my_idx[u];
+            my_key[u] = lane == k ? top : my_key[u];
+            key[u] = lane == who ? 0u : key[u];
         }
+    }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int tt = t + u * kRouteWaves;
-            if (tt >= t1) break;
-            int i;
-            float w;
-            route_token(a, l[u], lane, i, w);
-            if (lane < a.K) {
-                a.idx[(size_t)tt * a.K + lane] = i;
-                a.w[(size_t)tt * a.K + lane] = w;
-            }
-        }
+    for (int u = 0; u < U; ++u) {
+        const float l = key_logit(my_key[u]);
+        // equal to the largest: 1 (inf - inf is no number)
+        const float e = lane < a.K && m[u] > -INFINITY ? (l == m[u] ? 1.f : expf(l - m[u])) : 0.f;
+        const float sum = wave_sum(e);
+        my_w[u] = sum > 0.f ? e / sum : 0.f;
     }
 }
 
@@ -158,13 +143,14 @@ __global__ __launch_bounds__(kRouteThreads) void route_one(RouteArgs a) {
     const int pairs = a.T * a.K;
     if (a.logits) {
         for (int t = wave; t < a.T; t += kRouteWaves) {
-            int i;
-            float w;
-            route_token(a, lane < a.E ? a.logits[(size_t)t * a.E + lane] : 0.f, lane, i, w);
+            const float l[1] = {lane < a.E ? a.logits[(size_t)t * a.E + lane] : 0.f};
+            int i[1];
+            float w[1];
+            route_tokens<1>(a, l, lane, i, w);
             if (lane < a.K) {
-                a.idx[t * a.K + lane] = i;
-                a.w[t * a.K + lane] = w;
-                s_idx[t * a.K + lane] = i;
+                a.idx[t * a.K + lane] = i[0];
+                a.w[t * a.K + lane] = w[0];
+                s_idx[t * a.K + lane] = i[0];
             }
         }
     } else {
@@ -192,14 +178,35 @@ __global__ __launch_bounds__(kRouteThreads) void route_count(RouteArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int t0 = min(blockIdx.x * a.tpb, (unsigned)a.T), t1 = min(t0 + a.tpb, a.T);
     if (tid < kMaxExperts) total[tid] = 0;
-    if (a.logits) route_tokens(a, t0, t1, wave, lane);
-    if (!a.offsets) return;
     __syncthreads();
-    const int32_t *idx = a.logits ? a.idx : a.idx_in;
-    for (int p = t0 * a.K + tid; p < t1 * a.K; p += kRouteThreads) {
-        const int e = idx[p];
-        if (e >= 0 && e < a.E) atomicAdd(&total[e], 1);
+    if (a.logits) {
+        constexpr int U = 4;
+        for (int t = t0 + wave; t < t1; t += U * kRouteWaves) {
+            float l[U], w[U];
+            int i[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int tt = t + u * kRouteWaves;
+                l[u] = tt < t1 && lane < a.E ? a.logits[(size_t)tt * a.E + lane] : 0.f;
+            }
+            route_tokens<U>(a, l, lane, i, w);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int tt = t + u * kRouteWaves;
+                if (tt < t1 && lane < a.K) {
+                    a.idx[(size_t)tt * a.K + lane] = i[u];
+                    a.w[(size_t)tt * a.K + lane] = w[u];
+                    atomicAdd(&total[i[u]], 1);  // (in LDS: the order does not matter)
+                }
+            }
+        }
+    } else {
+        for (int p = t0 * a.K + tid; p < t1 * a.K; p += kRouteThreads) {
+            const int e = a.idx_in[p];
+            if (e >= 0 && e < a.E) atomicAdd(&total[e], 1);
+        }
     }
+    if (!a.offsets) return;
     __syncthreads();
     if (tid < kMaxExperts) a.counts[blockIdx.x * kMaxExperts + tid] = total[tid];
 }
@@ -213,6 +220,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_place(RouteArgs a) {
     const int blk = blockIdx.x;
     const int t0 = min(blk * a.tpb, a.T), t1 = min(t0 + a.tpb, a.T);
     int n = 0, m = 0;
+#pragma unroll 8
     for (int b = wave; b < a.blocks; b += kRouteWaves) {
         const int c = a.counts[b * kMaxExperts + lane];
         n += c;
@@ -236,19 +244,33 @@ __global__ __launch_bounds__(kRouteThreads) void route_place(RouteArgs a) {
 }
 
 // d_logits[t] = w_k (d_w_k - sum_j w_j d_w_j) at the chosen experts, 0
-// elsewhere.  A lane writes one element; its token's K choices come from
-// cache.  An expert listed twice takes both terms.
+// elsewhere.  A lane writes V neighbouring elements; its token's K choices come
+// from cache, all of them at once.  An expert listed twice takes both terms.
+template <int V>
 __global__ __launch_bounds__(256) void route_grad_kernel(const int32_t *idx, const float *w, const float *dw,
                                                          float *dl, int T, int E, int K) {
-    const long long n = (long long)T * E, step = (long long)gridDim.x * 256;
+    const int per = E / V;
+    const long long n = (long long)T * per, step = (long long)gridDim.x * 256;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
-        const int t = (int)(i / E), e = (int)(i - (long long)t * E);
-        float dot = 0.f;
-        for (int k = 0; k < K; ++k) dot += w[(size_t)t * K + k] * dw[(size_t)t * K + k];
-        float v = 0.f;
-        for (int k = 0; k < K; ++k)
-            if (idx[(size_t)t * K + k] == e) v += w[(size_t)t * K + k] * (dw[(size_t)t * K + k] - dot);
-        dl[i] = v;
+        const int t = (int)(i / per), e = (int)(i - (long long)t * per) * V;
+        int c[kMaxTopK];
+        float p[kMaxTopK], d[kMaxTopK];
+#pragma unroll
+        for (int k = 0; k < kMaxTopK; ++k) {
+            const size_t at = (size_t)t * K + min(k, K - 1);
+            c[k] = k < K ? idx[at] : -1;
+            p[k] = k < K ? w[at] : 0.f;
+            d[k] = k < K ? dw[at] : 0.f;
+        }
+        float dot = 0.f, v[V] = {};
+#pragma unroll
+        for (int k = 0; k < kMaxTopK; ++k) dot += p[k] * d[k];
+#pragma unroll
+        for (int k = 0; k < kMaxTopK; ++k)
+#pragma unroll
+            for (int u = 0; u < V; ++u) v[u] += c[k] == e + u ? p[k] * (d[k] - dot) : 0.f;
+        if constexpr (V == 4) *reinterpret_cast<f32x4 *>(dl + (size_t)t * E + e) = f32x4{v[0], v[1], v[2], v[3]};
+        else dl[(size_t)t * E + e] = v[0];
     }
 }
 
@@ -439,11 +461,12 @@ ts_status ts_moe_route_grad(const int32_t *topk_idx, const float *topk_w, const 
     if (!topk_idx || !topk_w || !d_w || !d_logits) return TS_ERR_NULL;
     if (!ts::aligned4(topk_idx) || !ts::aligned4(topk_w) || !ts::aligned4(d_w) || !ts::aligned4(d_logits))
         return TS_ERR_ALIGN;
-    const long long n = (long long)tokens * n_experts;
+    const bool four = n_experts % 4 == 0 && ts::aligned16(d_logits);
+    const long long n = (long long)tokens * (four ? n_experts / 4 : n_experts);
     const unsigned grid = (unsigned)std::min<long long>((n + 255) / 256, 256 * 16);
     ts::launch<const int32_t *, const float *, const float *, float *, int, int, int>(
-        "moe_route_grad", ts::route_grad_kernel, dim3(grid), dim3(256), static_cast<hipStream_t>(stream), topk_idx,
-        topk_w, d_w, d_logits, tokens, n_experts, top_k);
+        "moe_route_grad", four ? ts::route_grad_kernel<4> : ts::route_grad_kernel<1>, dim3(grid), dim3(256),
+        static_cast<hipStream_t>(stream), topk_idx, topk_w, d_w, d_logits, tokens, n_experts, top_k);
     return ts::check_launch("moe_route_grad");
 }
 
