@@ -219,11 +219,15 @@ __device__ __forceinline__ void unroll(F f) {
 constexpr int kStrip = 8;
 
 // WP x WQ waves; a wave's tile is (BP / WP) x (BQ / WQ).  AR, BR: stages of the P
-// operand (weights) and of the other; AR may be one more.  WIDE: x is 4 GB or
+// operand (weights) and of the other; AR may be one more.  KW: groups of waves
+// that share the contraction's blocks, each with its own stages; their sums are
+// added at the end in a fixed order (few tiles with a long contraction: a step's
+// chain of barrier, operand reads and matrix instructions is what costs, and
+// KW of them run side by side).  WIDE: x is 4 GB or
 // more, its rows' offsets take 64 bits.
-template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int AR, int BR, bool WIDE>
-__global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
-    constexpr int THREADS = 64 * WP * WQ;
+template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int AR, int BR, int KW, bool WIDE>
+__global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
+    constexpr int THREADS = 64 * WP * WQ;  // of one contraction group
     constexpr bool BCOL = MODE == kGradW;
     using TA = GmmTile<KIND, ACOL, BP, THREADS>;
     using TB = GmmTile<KIND, BCOL, BQ, THREADS>;
@@ -240,11 +244,14 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
     constexpr int NX = BQ < 64 ? 1 : BQ / 64, SS = FP8 ? THREADS : 0;
     static_assert(!FP8 || THREADS / 64 >= NX + 2, "two waves for weight scales");
     constexpr int ALL = AR * TA::CHUNKS + BR * TB::CHUNKS + BR * SS / 4;
-    __shared__ u32x4 s_a[ALL];
+    static_assert(KW == 1 || MODE != kGradW, "the weight gradient's contraction is short");
+    __shared__ u32x4 s_all[KW * ALL];
+    const int kg = KW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
+    u32x4 *const s_a = s_all + kg * ALL;
     u32x4 *const s_b = s_a + AR * TA::CHUNKS;
     const float *const s_s = reinterpret_cast<const float *>(s_b + BR * TB::CHUNKS);
 
-    const int tid = threadIdx.x, lane = tid & 63, lm = lane & 15, lq = lane >> 4;
+    const int tid = threadIdx.x - kg * THREADS, lane = tid & 63, lm = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wp = wave / WQ, wq = wave % WQ;
 
@@ -480,9 +487,9 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
             else ld_lds16(bbase + blk * bstep, boff[j], lds_b + (uint32_t)(to * TB::CHUNKS + THREADS * j) * 16);
         };
 
-        ask(last);
-        take();
-        {
+        if (kg == 0) {
+            ask(last);
+            take();
             const int left = C - last * KS;
             unroll<TB::NJ>([&](auto j) {
                 ld_lds16(kb + JB * j < left ? bbase + last * bstep + boff[j] : zero, lds_b + 16 * THREADS * j);
@@ -504,47 +511,72 @@ __global__ __launch_bounds__(64 * WP * WQ) void gmm_tiled(GmmArgs a) {
 #pragma unroll
                 for (int j = 0; j < TA::NJ; ++j) rowoff[j] = 0;
         }
-        // Step t contracts block t - 1 (step 0: the last) and loads block t + BR
-        // - 2 of the other operand and t + AR - 2 of the P operand into the
-        // stages that step t - 1 read.  The last steps have none to load and load
-        // the last whole one again: no branch between the matrix instructions.
-        auto whole = [&](int blk) { return max(min(blk, last - 1), 0); };
+        // The blocks' order: the last, 0, 1, ...; step t of group kg contracts
+        // the (kg + t KW)th of them.  It loads those of steps t + BR - 1 (the
+        // other operand) and t + AR - 1 (the P operand) into the stages that
+        // step t - 1 read.  The last steps have none to load and load the last
+        // whole block again: no branch between the matrix instructions.
+        auto block = [&](int t) { return max(min(kg + t * KW - 1, last - 1), 0); };
+        if constexpr (KW > 1)
+            if (kg > 0) {
+                unroll<LOADS_B>([&](auto j) { load_b(j, block(0), 0); });
+                unroll<LOADS_A>([&](auto j) { load_a(j, block(0), 0); });
+            }
         unroll<AR - 2>([&](auto i) {
-            if constexpr (i < BR - 2) unroll<LOADS_B>([&](auto j) { load_b(j, whole(i), i + 1); });
+            if constexpr (i < BR - 2) unroll<LOADS_B>([&](auto j) { load_b(j, block(i + 1), i + 1); });
             if (last > 0) {
-                ask(whole(i));
+                ask(block(i + 1));
                 take();
             }
-            unroll<LOADS_A>([&](auto j) { load_a(j, whole(i), i + 1); });
+            unroll<LOADS_A>([&](auto j) { load_a(j, block(i + 1), i + 1); });
         });
         if (last > 0) {
-            ask(whole(AR - 2));
+            ask(block(AR - 1));
             take();
         }
         int ar = 0, br = 0;  // stages of step t
-        for (int t = 0; t <= last; ++t) {
+        for (int t = 0; t * KW <= last; ++t) {
             // what may be on its way: all that was asked for behind this step's
             gmm_barrier<(AR == BR ? (BR - 2) * LOADS : (BR - 2) * LOADS + LOADS_A)>();
-            const int blk_a = whole(t + AR - 2), blk_b = whole(t + BR - 2);
-            ask(whole(t + AR - 1));
+            const int blk_a = block(t + AR - 1), blk_b = block(t + BR - 1);
+            ask(block(t + AR));
             const int to_a = ar == 0 ? AR - 1 : ar - 1, to_b = br == 0 ? BR - 1 : br - 1;
-            contract(s_a + ar * TA::CHUNKS, s_b + br * TB::CHUNKS, s_s + br * SS, [&](auto gi) {
-                // (in the earlier half of the groups, the later half covers the
-                // last loads' way: gate + up at 8192 tokens 2.98 ms, spread over
-                // all groups 3.06; fp8, whose groups are twice as long, 2.36 / 2.30)
-                constexpr int G = gi, OVER = FP8 || NG < 2 ? NG : NG / 2;
-                if constexpr (G < OVER)
-                    unroll<(G + 1) * LOADS / OVER - G * LOADS / OVER>([&](auto l) {
-                        constexpr int L = G * LOADS / OVER + l;
-                        if constexpr (L < LOADS_B) load_b(std::integral_constant<int, L>{}, blk_b, to_b);
-                        else load_a(std::integral_constant<int, L - LOADS_B>{}, blk_a, to_a);
-                    });
-            });
+            if (KW == 1 || kg + t * KW <= last)
+                contract(s_a + ar * TA::CHUNKS, s_b + br * TB::CHUNKS, s_s + br * SS, [&](auto gi) {
+                    // (in the earlier half of the groups, the later half covers
+                    // the last loads' way: gate + up at 8192 tokens 2.98 ms,
+                    // spread over all groups 3.06; fp8, whose groups are twice as
+                    // long, 2.36 / 2.30)
+                    constexpr int G = gi, OVER = FP8 || NG < 2 ? NG : NG / 2;
+                    if constexpr (G < OVER)
+                        unroll<(G + 1) * LOADS / OVER - G * LOADS / OVER>([&](auto l) {
+                            constexpr int L = G * LOADS / OVER + l;
+                            if constexpr (L < LOADS_B) load_b(std::integral_constant<int, L>{}, blk_b, to_b);
+                            else load_a(std::integral_constant<int, L - LOADS_B>{}, blk_a, to_a);
+                        });
+                });
             if (last > 0) take();
             ar = ar == AR - 1 ? 0 : ar + 1;
             br = br == BR - 1 ? 0 : br + 1;
         }
         gmm_barrier<0>();
+    }
+    if constexpr (KW > 1) {
+        static_assert((KW - 1) * BP * BQ / 4 <= KW * ALL, "the groups' sums fit the stages");
+        f32x4 *red = reinterpret_cast<f32x4 *>(s_all);
+        if (kg > 0)
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < MJ; ++j) red[((kg - 1) * MI * MJ + i * MJ + j) * THREADS + tid] = acc[i][j];
+        __syncthreads();
+        if (kg > 0) return;
+#pragma unroll
+        for (int h = 0; h < KW - 1; ++h)
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < MJ; ++j) acc[i][j] += red[(h * MI * MJ + i * MJ + j) * THREADS + tid];
     }
 
     // lane (lm, lq) holds, of the 16 x 16 block (i, j), column lm (Q) and rows
@@ -592,12 +624,12 @@ inline long long gmm_grid(const GmmArgs &a) {
 }
 
 // Launches it; a grid beyond the runtime's 2^32 threads is refused.
-template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int AR, int BR, bool WIDE = false>
+template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int AR, int BR, int KW = 1, bool WIDE = false>
 ts_status run_tiled(const char *name, const GmmArgs &a, hipStream_t st) {
     const long long grid = gmm_grid<MODE, BP, BQ>(a);
-    if (grid * (64 * WP * WQ) >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
-    launch<GmmArgs>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, AR, BR, WIDE>, dim3((unsigned)grid),
-                    dim3(64 * WP * WQ), st, a);
+    if (grid * (64 * WP * WQ * KW) >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
+    launch<GmmArgs>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, AR, BR, KW, WIDE>, dim3((unsigned)grid),
+                    dim3(64 * WP * WQ * KW), st, a);
     return check_launch(name);
 }
 
@@ -610,9 +642,10 @@ inline bool gmm_wide(const GmmArgs &a) {
 // Forward product on the tile that suits its sizes.
 template <GmmKind KIND, GmmMode MODE, bool ACOL>
 ts_status run_fwd(const char *name, const GmmArgs &a, hipStream_t st) {
-    if (gmm_wide<KIND>(a)) return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2, true>(name, a, st);
+    if (gmm_wide<KIND>(a)) return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2, 1, true>(name, a, st);
     switch (pick_tile(KIND, MODE == kDrelu, a.groups, a.rows, a.n, a.k)) {
-        case kTile64x32: return run_tiled<KIND, MODE, ACOL, 64, 32, 2, 2, 6, 6>(name, a, st);
+        case kTile64x32: return run_tiled<KIND, MODE, ACOL, 64, 32, 2, 2, 3, 3, 2>(name, a, st);
+        case kTile64x64: return run_tiled<KIND, MODE, ACOL, 64, 64, 2, 2, 4, 4, 2>(name, a, st);
         case kTile128x64: return run_tiled<KIND, MODE, ACOL, 128, 64, 4, 1, 3, 3>(name, a, st);
         case kTile128x128: return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2>(name, a, st);
         case kTile256x128:

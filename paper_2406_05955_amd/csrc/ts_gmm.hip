@@ -15,7 +15,7 @@ namespace {
 
 template <GmmKind KIND>
 ts_status run_grad_w(const GmmArgs &a, hipStream_t st) {
-    if (gmm_wide<KIND>(a)) return run_tiled<KIND, kGradW, true, 128, 128, 2, 2, 2, 2, true>("grouped_mm_dw", a, st);
+    if (gmm_wide<KIND>(a)) return run_tiled<KIND, kGradW, true, 128, 128, 2, 2, 2, 2, 1, true>("grouped_mm_dw", a, st);
     if constexpr (KIND == kGmmBf16)
         if ((long long)a.n * a.k * a.groups >= 256LL * 65536)
             return run_tiled<KIND, kGradW, true, 256, 256, 2, 4, 3, 2>("grouped_mm_dw", a, st);

@@ -44,15 +44,16 @@ size_t route_ws_bytes(int tokens, int n_experts, int top_k) {
 // The tile whose time is least by a simple count, in cycles: a step (128 bytes
 // of contraction) takes its matrix instructions at half their peak, or its
 // operands at 20 bytes a cycle and unit (what a unit draws with all units busy),
-// or a round trip of 500 cycles shared by the stages ahead; the tiles run in
-// rounds of 256 units.  Groups are taken as spread evenly over their sizes (half
-// a tile over).  Over 30 calls (1 to 3000 tokens, dense, 8 and 16 groups, 512 x
-// 1792 to 4096 x 14336, three types) the choice costs 1.7% on average against
-// the best of ten tiles measured one by one.  Us, 64x32 / 128x64 / 128x128 /
-// 256x128 / 256x256: down bf16 4096 x 14336 1 token 38 / 67 / 131 / 142 / 235, 32
-// tokens 181 / 154 / 232 / 171 / 302, 512 tokens 545 / 309 / 307 / 243 / 283; one
-// fp8 layer 4096 x 4096 100 rows 13 / 23 / 33 / 32 / 48, 2000 rows 111 / 62 / 51 /
-// 41 / 64.
+// or a round trip of 2000 cycles shared by the stages ahead and the contraction
+// groups; the tiles run in rounds of 256 units.  Groups are taken as spread evenly
+// over their sizes (half a tile over).  Over 41 calls (1 to 3000 tokens, dense, 4
+// to 16 groups, 512 x 1792 to 4096 x 14336, three types) the choice costs 3.9% on
+// average against the best of eleven tiles measured one by one.  Us, 64x32 / 64x64
+// / 128x64 / 128x128 / 256x128 / 256x256: down bf16 4096 x 14336 1 token 39 / 41 /
+// 67 / 131 / 142 / 236, 32 tokens 181 / 172 / 153 / 232 / 192 / 322, 512 tokens 503
+// / 391 / 310 / 305 / 243 / 292; one fp8 layer 4096 x 4096 100 rows 9.5 / 11 / 24 /
+// 32 / 31 / 47, 2000 rows 97 / 80 / 61 / 52 / 42 / 66; 2048 x 8192 400 rows 26 / 19
+// / 41 / 68 / 58 / 106.
 GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k) {
     const int esz = kind == kGmmF32 ? 4 : kind == kGmmFp8 ? 1 : 2;
     const int used = std::max(1, std::min(groups, rows));
@@ -71,7 +72,7 @@ GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k
         const double together = std::min<double>(t.per_unit, std::max(1.0, tiles / 256));
         const double r = tiles / (256.0 * t.per_unit);
         const double rounds = r < 4 ? std::ceil(r) : r + 0.5;
-        const double cycles = rounds * (steps * std::max(together * step, 500.0 / (t.stages - 1)) + 1000.0);
+        const double cycles = rounds * (steps * std::max(together * step, 2000.0 / (t.stages - 1) / t.kw) + 250.0 * (t.kw + 1));
         if (least == 0.0 || cycles < least) {
             least = cycles;
             best = (GmmTileId)i;
