@@ -8,6 +8,8 @@
 // its own code NaN.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "ts_gmm.h"
 #include "ts_plan.h"
 #include "ts_runtime.h"
@@ -56,36 +58,40 @@ template <typename T>
 __global__ __launch_bounds__(256) void fp8_quant_kernel(const T *x, uint8_t *q, float *s, int rows, int cols) {
     const int kb = (cols + kScaleBlock - 1) / kScaleBlock;
     const int lane16 = threadIdx.x & 15;
-    const long long blk = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const bool in = blk < (long long)rows * kb;
-    const int row = in ? (int)(blk / kb) : 0, b = in ? (int)(blk % kb) : 0;
-    const int c0 = b * kScaleBlock + lane16 * 8;
-    const bool ok = in && c0 < cols;  // cols is a multiple of 16: all 8 or none
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (ok) {
-        const T *p = x + (size_t)row * cols + c0;
-        if constexpr (sizeof(T) == 4) {
-            unpack<float>(ld_cached(p), v);
-            unpack<float>(ld_cached(p + 4), v + 4);
-        } else {
-            unpack<uint16_t>(ld_cached(p), v);
+    const long long blocks = (long long)rows * kb, step = (long long)gridDim.x * 16;
+    // (whole waves stay in the loop: a block's lanes exchange their maxima)
+    for (long long b0 = (long long)blockIdx.x * 16; b0 < blocks; b0 += step) {
+        const long long blk = b0 + (threadIdx.x >> 4);
+        const bool in = blk < blocks;
+        const int row = in ? (int)(blk / kb) : 0, b = in ? (int)(blk % kb) : 0;
+        const int c0 = b * kScaleBlock + lane16 * 8;
+        const bool ok = in && c0 < cols;  // cols is a multiple of 16: all 8 or none
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (ok) {
+            const T *p = x + (size_t)row * cols + c0;
+            if constexpr (sizeof(T) == 4) {
+                unpack<float>(ld_cached(p), v);
+                unpack<float>(ld_cached(p + 4), v + 4);
+            } else {
+                unpack<uint16_t>(ld_cached(p), v);
+            }
         }
-    }
-    float amax = kAmaxMin;
+        float amax = kAmaxMin;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) amax = max_abs(amax, v[i]);
-    amax = fmaxf(amax, dpp_f32<0xB1>(amax));
-    amax = fmaxf(amax, dpp_f32<0x4E>(amax));
-    amax = fmaxf(amax, dpp_f32<0x124>(amax));
-    amax = fmaxf(amax, dpp_f32<0x128>(amax));
-    if (ok) {
-        const QuantDiv div(amax);
-        uint2 o;
-        o.x = codes4(div(v[0]), div(v[1]), div(v[2]), div(v[3]));
-        o.y = codes4(div(v[4]), div(v[5]), div(v[6]), div(v[7]));
-        *reinterpret_cast<uint2 *>(q + (size_t)row * cols + c0) = o;
+        for (int i = 0; i < 8; ++i) amax = max_abs(amax, v[i]);
+        amax = fmaxf(amax, dpp_f32<0xB1>(amax));
+        amax = fmaxf(amax, dpp_f32<0x4E>(amax));
+        amax = fmaxf(amax, dpp_f32<0x124>(amax));
+        amax = fmaxf(amax, dpp_f32<0x128>(amax));
+        if (ok) {
+            const QuantDiv div(amax);
+            uint2 o;
+            o.x = codes4(div(v[0]), div(v[1]), div(v[2]), div(v[3]));
+            o.y = codes4(div(v[4]), div(v[5]), div(v[6]), div(v[7]));
+            *reinterpret_cast<uint2 *>(q + (size_t)row * cols + c0) = o;
+        }
+        if (in && lane16 == 0) s[blk] = amax / kE4m3Max;
     }
-    if (in && lane16 == 0) s[blk] = amax / kE4m3Max;
 }
 
 // Weights: one 128 x 128 tile per workgroup; KN: the matrix is stored [k][n]
@@ -202,8 +208,7 @@ ts_status ts_fp8_quant(const void *x, ts_dtype dtype, int rows, int cols, void *
     ts_status s = ts::check_quant(x, dtype, q, scale);
     if (s != TS_OK) return s;
     const long long blocks = (long long)rows * ts::ceil_div(cols, ts::kScaleBlock);
-    const long long grid = (blocks + 15) / 16;
-    if (grid * 256 >= (1LL << 32)) return TS_ERR_SHAPE;
+    const long long grid = std::min<long long>((blocks + 15) / 16, 1 << 20);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (dtype == TS_F32)
         ts::launch<const float *, uint8_t *, float *, int, int>("fp8_quant", ts::fp8_quant_kernel<float>,
@@ -224,6 +229,7 @@ ts_status ts_fp8_quant_weights(const void *w, ts_dtype dtype, int w_kn, int n_gr
     s = ts::check_quant(w, dtype, q, scale);
     if (s != TS_OK) return s;
     const long long grid = (long long)n_groups * ts::ceil_div(n, 128) * ts::ceil_div(k, 128);
+    if (grid * 256 >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
     auto go = [&](auto kernel, auto *p) {
         ts::launch<decltype(p), uint8_t *, float *, int, int>("fp8_quant_weights", kernel, dim3((unsigned)grid),

@@ -52,28 +52,29 @@ enum GmmMode { kFwd = 0, kDrelu = 1, kGradW = 2 };
 __device__ __forceinline__ uint32_t lds_addr(const void *p) {
     return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p);
 }
-__device__ __forceinline__ void ld_lds16(const char *p, uint32_t l) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(l) : "memory", "m0");
-}
-__device__ __forceinline__ void ld_lds16(const char *base, uint32_t off, uint32_t l) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(l)
-                 : "memory", "m0");
-}
-__device__ __forceinline__ void ld_lds16(const char *base, size_t off, uint32_t l) { ld_lds16(base + off, l); }
 // A wave-uniform address in scalar registers.
 __device__ __forceinline__ const char *uniform(const void *p) {
     const uint64_t v = reinterpret_cast<uint64_t>(p);
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
     return reinterpret_cast<const char *>((uint64_t)hi << 32 | lo);
 }
+__device__ __forceinline__ void ld_lds16(const char *p, uint32_t l) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p),
+                 "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
+}
+__device__ __forceinline__ void ld_lds16(const char *base, uint32_t off, uint32_t l) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(uniform(base)),
+                 "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
+}
+__device__ __forceinline__ void ld_lds16(const char *base, size_t off, uint32_t l) { ld_lds16(base + off, l); }
 // 4 bytes a lane, at `l` + 4 x lane.
 __device__ __forceinline__ void ld_lds4(const char *base, uint32_t off, uint32_t l) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(l)
-                 : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(uniform(base)),
+                 "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
 }
 __device__ __forceinline__ void ld_lds4(const char *base, size_t off, uint32_t l) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(base + off), "s"(l)
-                 : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(base + off),
+                 "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
 }
 
 // Inclusive sums and maxima over the wave's lanes (maxima of values >= 0):
@@ -483,7 +484,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
         };
         auto load_b = [&](auto j, int blk, int to) {
             if constexpr (j == TB::NJ)
-                ld_lds4(uniform(sbase + blk), soff, lds_s + (uint32_t)(to * SS) * 4);
+                ld_lds4(reinterpret_cast<const char *>(sbase + blk), soff, lds_s + (uint32_t)(to * SS) * 4);
             else ld_lds16(bbase + blk * bstep, boff[j], lds_b + (uint32_t)(to * TB::CHUNKS + THREADS * j) * 16);
         };
 
@@ -645,7 +646,9 @@ ts_status run_fwd(const char *name, const GmmArgs &a, hipStream_t st) {
     if (gmm_wide<KIND>(a)) return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2, 1, true>(name, a, st);
     switch (pick_tile(KIND, MODE == kDrelu, a.groups, a.rows, a.n, a.k)) {
         case kTile64x32: return run_tiled<KIND, MODE, ACOL, 64, 32, 2, 2, 3, 3, 2>(name, a, st);
-        case kTile64x64: return run_tiled<KIND, MODE, ACOL, 64, 64, 2, 2, 4, 4, 2>(name, a, st);
+        case kTile64x64:
+            if constexpr (KIND != kGmmF32) return run_tiled<KIND, MODE, ACOL, 64, 64, 2, 2, 4, 4, 2>(name, a, st);
+            break;
         case kTile128x64: return run_tiled<KIND, MODE, ACOL, 128, 64, 4, 1, 3, 3>(name, a, st);
         case kTile128x128: return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2>(name, a, st);
         case kTile256x128:

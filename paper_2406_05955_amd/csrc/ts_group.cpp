@@ -63,8 +63,9 @@ GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k
     double least = 0.0;
     for (int i = 0; i < kTiles; ++i) {
         const GmmTileSize &t = kTileSize[i];
-        // (fp32: 8 waves of matrix instructions that long gain nothing from a larger tile)
-        if (kind == kGmmF32 && t.p == 256) continue;
+        // (fp32: matrix instructions are all of the time, larger tiles gain nothing;
+        // 64 x 64 had no call where it was the best)
+        if (kind == kGmmF32 && (t.p == 256 || i == kTile64x64)) continue;
         const double row_tiles = groups == 1 ? ceil_div(rows, t.q) : used * std::max(1.0, mean / t.q + 0.5);
         const double tiles = ceil_div(n, drelu ? t.p / 2 : t.p) * row_tiles;
         const double matrix = (double)t.p * t.q / (kind == kGmmF32 ? 2.0 : 16.0);

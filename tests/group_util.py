@@ -1,5 +1,5 @@
 """Plain 64-bit forms of the grouped operators, and what their results may be
-off by (CPU tensors in, CPU tensors out)."""
+off by (results on the inputs' device)."""
 import torch
 
 F32, BF16, D = torch.float32, torch.bfloat16, torch.float64
@@ -25,11 +25,19 @@ def ragged(rows, groups, gen, lead=0, tail=0):
     return (o + lead).to(torch.int32)
 
 
+# (rows, groups, n) that between them take every tile of every kind and mode at
+# these contractions: several whole blocks (the stages' rings wrap) and a partial one
+TILE_SHAPES = [(41, 1, 144), (41, 1, 6160), (41, 1, 8208), (41, 5, 4112), (41, 5, 8208), (100, 5, 6160), (300, 5, 4112),
+               (300, 5, 6160), (300, 5, 8208), (700, 5, 4112), (700, 5, 6160), (700, 5, 8208), (1000, 1, 2064),
+               (2500, 1, 1552), (4000, 1, 144)]
+TILE_K = {"bf16": 336, "f32": 336, "fp8": 720}
+
+
 def mm(x, w, offsets, row_src=None, w_kn=False):
     """(y, sum of |products|) in 64 bits; NaN where no group has the row."""
     x = x.double() if row_src is None else x.double()[row_src.long()]
     w = w.double() if w_kn else w.double().transpose(1, 2)
-    y = torch.full((x.shape[0], w.shape[2]), float("nan"), dtype=D)
+    y = torch.full((x.shape[0], w.shape[2]), float("nan"), dtype=D, device=x.device)
     mag = y.clone()
     for g, a, b in spans(offsets):
         y[a:b] = x[a:b] @ w[g]
@@ -41,7 +49,7 @@ def dw(d_y, x, offsets, row_src=None):
     x = x.double() if row_src is None else x.double()[row_src.long()]
     d_y = d_y.double()
     G = len(offsets) - 1
-    y = torch.zeros(G, d_y.shape[1], x.shape[1], dtype=D)
+    y = torch.zeros(G, d_y.shape[1], x.shape[1], dtype=D, device=x.device)
     mag = y.clone()
     for g, a, b in spans(offsets):
         y[g] = d_y[a:b].t() @ x[a:b]
@@ -63,10 +71,10 @@ def fp8_bound(x, w, offsets, row_src=None):
     than 2^-13 of the group's largest product."""
     x = x.double() if row_src is None else x.double()[row_src.long()]
     w, x = w.double().abs(), x.abs()
-    out = torch.zeros(x.shape[0], w.shape[1], dtype=D)
+    out = torch.zeros(x.shape[0], w.shape[1], dtype=D, device=x.device)
     for g, a, b in spans(offsets):
         for k in range(0, x.shape[1], 8):
-            top = torch.zeros(b - a, w.shape[1], dtype=D)
+            top = torch.zeros(b - a, w.shape[1], dtype=D, device=x.device)
             for i in range(k, k + 8):
                 top = torch.maximum(top, x[a:b, i, None] * w[g, None, :, i])
             out[a:b] += 7 * 2.0 ** -13 * top

@@ -29,7 +29,7 @@ def dev(*ts_):
 
 
 def within(got, want, bound, what=""):
-    got = got.detach().cpu().double()
+    got = got.detach().to(want.device).double()
     assert got.shape == want.shape, (got.shape, want.shape)
     bad = ~((got - want).abs() <= bound)
     assert not bad.any(), (what, int(bad.sum()), float((got - want).abs().max()), bad.nonzero()[:4].tolist())
@@ -404,6 +404,147 @@ def test_combine_and_gradients(ydt, odt, T, K, H):
     within(d_y, want, ref.rounded(2.0 ** -24 * want.abs(), want, ydt))
     dd = d_out.double()[:, None]
     within(d_w, (dd * rows).sum(2), ref.sum_bound((dd.abs() * rows.abs()).sum(2), H))
+
+
+# --- every tile, long offsets, bad maps ---------------------------------------------
+
+def big(rows, G, n, k, kind, w_kn=False):
+    """Inputs on the device (drawn there), ragged groups that leave rows out at
+    both ends, gathered rows."""
+    g = gen(70, rows, G, n, k)
+    gd = torch.Generator(device=DEV).manual_seed(rows * 7 + n)
+    offsets = ref.ragged(rows, G, g, lead=2, tail=3) if G > 1 else torch.tensor([2, rows - 3], dtype=torch.int32)
+    src = torch.randint(0, rows // 2, (rows,), generator=g, dtype=torch.int32)
+    dt = F32 if kind == "f32" else BF16
+    x = torch.randn(rows // 2, k, generator=gd, device=DEV).to(dt)
+    ws = [(torch.randn(G, *((k, n) if w_kn else (n, k)), generator=gd, device=DEV) * k ** -0.5).to(dt) for _ in range(2)]
+    return x, ws, offsets, dev(src), dev(offsets)
+
+
+@pytest.mark.parametrize("rows,G,n", ref.TILE_SHAPES)
+@pytest.mark.parametrize("kind", ["bf16", "f32", "fp8"])
+def test_every_tile(rows, G, n, kind):
+    k = ref.TILE_K[kind]
+    x, (wg, wu), offsets, src, off = big(rows, G, n, k, kind)
+    mid = slice(2, rows - 3)
+
+    def same_rows(got, want, bound, dt):
+        assert got.dtype == dt
+        within(got[mid], want[mid], ref.rounded(bound, want, dt)[mid])
+        untouched(got, mid, 7.0)
+    out = lambda dt: torch.full((rows, n), 7.0, dtype=dt, device=DEV)  # noqa: E731
+    if kind == "fp8":
+        (xq, xs), qg, qu = ts.fp8_quant(x), ts.fp8_quant_weights(wg), ts.fp8_quant_weights(wu)
+        (gt, eg), (up, eu) = (fp8_want(xq, xs, *q, offsets, src) for q in (qg, qu))
+        same_rows(ts.fp8_mm(xq, xs, *qg, off, row_src=src, out=out(F32)), gt, eg, F32)
+        c = ts.fp8_drelu(xq, xs, *qg, *qu, off, row_src=src, out=out(BF16))
+    else:
+        (gt, mg), (up, mu) = ref.mm(x, wg, offsets, src), ref.mm(x, wu, offsets, src)
+        eg, eu = ref.sum_bound(mg, k), ref.sum_bound(mu, k)
+        same_rows(ts.grouped_mm(x, wg, off, row_src=src, out=out(F32)), gt, eg, F32)
+        same_rows(ts.grouped_mm(x, wg.transpose(1, 2).contiguous(), off, row_src=src, w_kn=True, out=out(BF16)), gt, eg,
+                  BF16)
+        x2 = torch.randn_like(x.float()).to(x.dtype)
+        y2, m2 = ref.mm(x2, wu, offsets, src)
+        same_rows(ts.grouped_mm(x, wg, off, row_src=src, x2=x2, w2=wu, out=out(F32)), gt + y2,
+                  ref.sum_bound(mg + m2, 2 * k), F32)
+        c = ts.grouped_drelu(x, wg, wu, off, row_src=src, out=out(F32))
+    want = ref.drelu(gt, up)
+    same_rows(c, want, ref.drelu_bound(gt, up, eg, eu) + 2.0 ** -23 * want.abs(), c.dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,G,n,k", [(700, 5, 2064, 1736), (300, 3, 2576, 2312)])
+def test_dw_large_tiles(dtype, rows, G, n, k):
+    x, _, offsets, src, off = big(rows, G, 8, k, "f32" if dtype is F32 else "bf16")
+    d_y = torch.randn(rows, n, device=DEV, generator=torch.Generator(device=DEV).manual_seed(5)).to(dtype)
+    for s in (src, None):
+        xx = x if s is not None else torch.cat([x, x, x[:rows % 2]])
+        y, mag = ref.dw(d_y, xx, offsets, s)
+        within(ts.grouped_mm_dw(d_y, xx, off, row_src=s), y, ref.sum_bound(mag, rows))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "fp8"])
+def test_rows_of_x_past_4_gb(kind):
+    """x of more than 4 GB: gathered rows on both sides of that offset."""
+    k, n, rows, G = 8192, 144, 90, 3
+    esz = {"bf16": 2, "f32": 4, "fp8": 1}[kind]
+    S = (1 << 32) // (k * esz) + 70
+    g = gen(80)
+    src = torch.cat([torch.randint(0, 50, (rows // 2,), generator=g),
+                     S - 1 - torch.randint(0, 60, (rows - rows // 2,), generator=g)])
+    src = src[torch.randperm(rows, generator=g)].to(torch.int32)
+    offsets = ref.ragged(rows, G, g)
+    dt = F32 if kind == "f32" else BF16
+    few, back = src.long().unique(return_inverse=True)
+    xf = randn(g, len(few), k, dtype=dt)
+    w = randn(g, G, n, k, dtype=dt, scale=k ** -0.5)
+    small = back.to(torch.int32)
+    if kind == "fp8":
+        q, s = ref.quant_rows(xf)
+        x = torch.empty(S, k, dtype=torch.uint8, device=DEV)
+        xs = torch.empty(S, k // 128, device=DEV)
+        x[few.to(DEV)], xs[few.to(DEV)] = dev(q.view(torch.uint8)), dev(s)
+        wq = ts.fp8_quant_weights(dev(w))
+        for f, more in ((ts.fp8_mm, ()), (ts.fp8_drelu, wq)):
+            a = f(x.view(torch.float8_e4m3fn), xs, *wq, *more, dev(offsets), row_src=dev(src), out_dtype=F32)
+            b = f(dev(q), dev(s), *wq, *more, dev(offsets), row_src=dev(small), out_dtype=F32)
+            assert (a - b).norm() <= 1e-5 * b.norm()  # (another tile: another order of the same sums)
+        return
+    x = torch.empty(S, k, dtype=dt, device=DEV)
+    x[few.to(DEV)] = dev(xf)
+    y, mag = ref.mm(xf, w, offsets, small)
+    wd, od, sd = dev(w, offsets, src)
+    within(ts.grouped_mm(x, wd, od, row_src=sd, out_dtype=F32), y, ref.sum_bound(mag, k))
+    kn = wd.transpose(1, 2).contiguous()
+    within(ts.grouped_mm(x, kn, od, row_src=sd, w_kn=True, out_dtype=F32), y, ref.sum_bound(mag, k))
+    e = ref.sum_bound(mag, k)
+    c = ref.drelu(y, y)
+    within(ts.grouped_drelu(x, wd, wd, od, row_src=sd, out_dtype=F32), c,
+           ref.drelu_bound(y, y, e, e) + 2.0 ** -23 * c.abs())
+    d_y = randn(g, rows, n, dtype=dt)
+    y, mag = ref.dw(d_y, xf, offsets, small)
+    within(ts.grouped_mm_dw(dev(d_y), x, od, row_src=sd), y, ref.sum_bound(mag, rows))
+
+
+def test_outputs_past_2_31_elements():
+    rows, n, k = 140000, 16384, 8
+    g = gen(81)
+    x, w = randn(g, rows, k, dtype=BF16), randn(g, 1, n, k, dtype=BF16)
+    out = ts.grouped_mm(*dev(x, w))
+    for r in (0, 65535, 131071, 131072, 131073, rows - 1):
+        want = x[r].double() @ w[0].double().t()
+        mag = x[r].double().abs() @ w[0].double().abs().t()
+        within(out[r], want, ref.rounded(ref.sum_bound(mag, k), want, BF16))
+    gate = torch.ones_like(out)
+    dg, du = ts.drelu_grad(gate, gate, out)
+    assert torch.equal(dg[-1], out[-1]) and torch.equal(du[131073], out[131073])
+    del dg, du, gate
+    q, s = ts.fp8_quant(out)
+    rq, rs = ref.quant_rows(out[-2:].cpu())
+    assert torch.equal(q[-2:].cpu().view(torch.uint8), rq.view(torch.uint8)) and torch.equal(s[-2:].cpu(), rs)
+    pair = torch.tensor([[rows - 1, 131073]], dtype=torch.int32, device=DEV)
+    got = ts.moe_combine(out, pair, out_dtype=F32)
+    assert torch.equal(got[0], out[rows - 1].float() + out[131073].float())
+
+
+def test_maps_out_of_range_stay_in_bounds():
+    """Offsets out of order or range, sources out of range: clamped as stated
+    (rows that no clamped group holds stay)."""
+    rows, G, n, k = 60, 5, 72, 136
+    g = gen(82)
+    x, w = randn(g, 20, k, dtype=BF16), randn(g, G, n, k, dtype=BF16)
+    bad = torch.tensor([-7, 10, 4, 33, 1 << 30, 12], dtype=torch.int32)
+    src = torch.randint(-40, 60, (rows,), generator=g, dtype=torch.int32)
+    src[0], src[1] = -(1 << 31), (1 << 31) - 1
+    good = bad.clamp(0, rows).cummax(0).values
+    y, mag = ref.mm(x, w, good, src.clamp(0, 19))
+    out = torch.full((rows, n), 7.0, device=DEV)
+    ts.grouped_mm(*dev(x, w, bad), row_src=dev(src), out=out)
+    within(out, y, ref.sum_bound(mag, k))
+    d_y = randn(g, rows, n, dtype=BF16)
+    y, mag = ref.dw(d_y, x, good, src.clamp(0, 19))
+    within(ts.grouped_mm_dw(*dev(d_y, x, bad), row_src=dev(src)), y, ref.sum_bound(mag, rows))
 
 
 # --- together ---------------------------------------------------------------------

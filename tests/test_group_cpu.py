@@ -2,6 +2,8 @@
 codes (nothing is enqueued) and the binding's own checks.  The plain 64-bit
 forms that the GPU tests compare with are held against one another here."""
 import itertools
+import os
+import subprocess
 
 import pytest
 import torch
@@ -197,3 +199,32 @@ def test_plain_quantiser():
     q, s = ref.quant_rows(x)
     assert torch.equal(ref.row_values(q, s).float(), x)
     assert s.tolist()[0][:2] == [1.0, 1.0]
+
+
+# --- the host side's choices ---------------------------------------------------------
+
+def build_check(tmp_path, *flags):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    csrc = os.path.join(root, "paper_2406_05955_amd", "csrc")
+    exe = tmp_path / "group_check"
+    subprocess.run(["g++", "-std=c++17", "-Wall", *flags, "-I", os.path.join(root, "include"), "-I", csrc,
+                    os.path.join(root, "tests", "native", "group_check.cpp"), os.path.join(csrc, "ts_group.cpp"),
+                    os.path.join(csrc, "ts_plan.cpp"), "-o", str(exe)], check=True)
+    return exe
+
+
+def test_host_side_under_sanitizers(tmp_path):
+    exe = build_check(tmp_path, "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all")
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
+def test_the_gpu_tests_reach_every_tile(tmp_path):
+    """The shapes that the GPU tests take run every tile that the rule can
+    choose, forward and with dReLU (fp32: three of the six)."""
+    exe = build_check(tmp_path, "-O2")
+    for kind, name in enumerate(("bf16", "f32", "fp8")):
+        for drelu in (0, 1):
+            lines = "\n".join(f"{kind} {drelu} {G} {rows} {n} {ref.TILE_K[name]}" for rows, G, n in ref.TILE_SHAPES)
+            r = subprocess.run([str(exe), "-"], input=lines, capture_output=True, text=True, check=True)
+            assert set(map(int, r.stdout.split())) == ({1, 2, 3} if name == "f32" else set(range(6))), (name, drelu)
