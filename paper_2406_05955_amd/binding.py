@@ -429,10 +429,17 @@ _i32, _e4m3 = torch.int32, torch.float8_e4m3fn
 
 
 def _need(t, name, dtype, shape):
-    """Raises unless t has this dtype and shape (None: any extent)."""
+    """Raises unless t has this dtype (or one of them) and shape (None: any
+    extent; a number: so many dimensions)."""
+    dt = t.dtype
+    if dt is dtype or (type(dtype) is tuple and dt in dtype):
+        if (t.dim() == shape) if type(shape) is int else (t.shape == shape):
+            return
     dts = dtype if isinstance(dtype, tuple) else (dtype,)
-    if t.dtype not in dts:
-        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dts)}, got {t.dtype}")
+    if dt not in dts:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dts)}, got {dt}")
+    if isinstance(shape, int):
+        shape = (None,) * shape
     if len(t.shape) != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
         want = "".join(f"[{'*' if w is None else w}]" for w in shape)
         raise ValueError(f"{name} must be {want}, got {tuple(t.shape)}")
@@ -443,6 +450,8 @@ def _here(stream, *ts):
     d = _cur_device() if _cur_device is not None and torch.cuda.is_initialized() else None
     for t in ts:
         if t is None:
+            continue
+        if t.get_device() == d and t.is_contiguous():  # (d is None or >= 0, -1 is the host)
             continue
         if not t.is_cuda or not t.is_contiguous():
             raise ValueError("tensors must be contiguous device tensors")
@@ -481,7 +490,7 @@ def _maps(T, E, K, dev):
 def moe_route(logits, top_k: int, maps: bool = True, ws=None, stream=None):
     """ts_moe_route.  logits [T][E] f32.  Returns topk_idx, topk_w [T][K] and,
     with maps, offsets [E + 1], row_token [T K], pair_row [T][K]."""
-    _need(logits, "logits", _f32, (None, None))
+    _need(logits, "logits", _f32, 2)
     st = _here(stream, logits, ws)
     T, E = logits.shape
     K = int(top_k)
@@ -502,7 +511,7 @@ def moe_route(logits, top_k: int, maps: bool = True, ws=None, stream=None):
 def moe_group(topk_idx, n_experts: int, ws=None, stream=None):
     """ts_moe_group.  topk_idx [T][K] int32.  Returns offsets [E + 1],
     row_token [T K] (entries from offsets[E] on unspecified), pair_row [T][K]."""
-    _need(topk_idx, "topk_idx", _i32, (None, None))
+    _need(topk_idx, "topk_idx", _i32, 2)
     st = _here(stream, topk_idx, ws)
     T, K = topk_idx.shape
     E = int(n_experts)
@@ -519,7 +528,7 @@ def moe_group(topk_idx, n_experts: int, ws=None, stream=None):
 
 def moe_route_grad(topk_idx, topk_w, d_w, n_experts: int, out=None, stream=None):
     """ts_moe_route_grad: d_logits [T][E] from d_w [T][K] (the gradient of topk_w)."""
-    _need(topk_idx, "topk_idx", _i32, (None, None))
+    _need(topk_idx, "topk_idx", _i32, 2)
     T, K = topk_idx.shape
     E = int(n_experts)
     if E < 1:
@@ -541,7 +550,7 @@ def _rows_of(x, offsets, row_src, G):
     elif G != 1:
         raise ValueError(f"{G} groups need offsets")
     if row_src is not None:
-        _need(row_src, "row_src", _i32, (None,))
+        _need(row_src, "row_src", _i32, 1)
         if x.shape[0] == 0 and row_src.shape[0] > 0:
             raise ValueError("row_src names rows of an empty x")
         return row_src.shape[0]
@@ -567,9 +576,9 @@ def grouped_mm(x, w, offsets=None, row_src=None, x2=None, w2=None, w_kn: bool = 
     f32, one dtype; x2, w2: a second product added to the first.  Returns out
     [rows][n] (out_dtype: x's unless given), rows = len(row_src) or S; rows
     outside the groups are not written."""
-    _need(x, "x", (_f32, _bf16), (None, None))
+    _need(x, "x", (_f32, _bf16), 2)
     S, k = x.shape
-    _need(w, "w", x.dtype, (None, None, None))
+    _need(w, "w", x.dtype, 3)
     G, n = w.shape[0], w.shape[2] if w_kn else w.shape[1]
     _need(w, "w", x.dtype, (None, k, n) if w_kn else (None, n, k))
     if (x2 is None) != (w2 is None):
@@ -592,7 +601,7 @@ def grouped_drelu(x, w_gate, w_up, offsets=None, row_src=None, keep: bool = Fals
                   stream=None):
     """ts_grouped_drelu.  x [S][k]; w_gate, w_up [G][n][k].  Returns c
     [rows][n], or (c, gate, up) with keep."""
-    _need(x, "x", (_f32, _bf16), (None, None))
+    _need(x, "x", (_f32, _bf16), 2)
     S, k = x.shape
     _need(w_gate, "w_gate", x.dtype, (None, None, k))
     _need(w_up, "w_up", x.dtype, tuple(w_gate.shape))
@@ -611,7 +620,7 @@ def grouped_drelu(x, w_gate, w_up, offsets=None, row_src=None, keep: bool = Fals
 
 def drelu_grad(gate, up, d_c, stream=None):
     """ts_drelu_grad: (d_gate, d_up) of c = max(0, gate) * max(0, up)."""
-    _need(gate, "gate", (_f32, _bf16), (None, None))
+    _need(gate, "gate", (_f32, _bf16), 2)
     _need(up, "up", gate.dtype, tuple(gate.shape))
     _need(d_c, "d_c", gate.dtype, tuple(gate.shape))
     st = _here(stream, gate, up, d_c)
@@ -626,11 +635,13 @@ def drelu_grad(gate, up, d_c, stream=None):
 def grouped_mm_dw(d_y, x, offsets=None, row_src=None, out=None, out_dtype=None, stream=None):
     """ts_grouped_mm_dw.  d_y [rows][n], x [S][k] -> d_w [G][n][k] (f32 unless
     out_dtype or out says otherwise), G = len(offsets) - 1."""
-    _need(x, "x", (_f32, _bf16), (None, None))
-    _need(d_y, "d_y", x.dtype, (None, None))
+    _need(x, "x", (_f32, _bf16), 2)
+    _need(d_y, "d_y", x.dtype, 2)
     if offsets is not None:
-        _need(offsets, "offsets", _i32, (None,))
+        _need(offsets, "offsets", _i32, 1)
     G = 1 if offsets is None else offsets.shape[0] - 1
+    if G < 1:
+        raise ValueError("offsets must hold n_groups + 1 entries, at least two")
     R = _rows_of(x, offsets, row_src, G)
     if d_y.shape[0] != R:
         raise ValueError(f"d_y has {d_y.shape[0]} rows, the product {R}")
@@ -652,7 +663,7 @@ def _nblk(n):
 def fp8_quant(x, stream=None):
     """ts_fp8_quant.  x [rows][cols] bf16 / f32 -> (codes float8_e4m3fn
     [rows][cols], scale f32 [rows][ceil(cols / 128)])."""
-    _need(x, "x", (_f32, _bf16), (None, None))
+    _need(x, "x", (_f32, _bf16), 2)
     st = _here(stream, x)
     R, C = x.shape
     q = torch.empty(R, C, dtype=_e4m3, device=x.device)
@@ -666,7 +677,7 @@ def fp8_quant(x, stream=None):
 def fp8_quant_weights(w, w_kn: bool = False, stream=None):
     """ts_fp8_quant_weights.  w [G][n][k], or [G][k][n] with w_kn -> (codes
     [G][n][k], scale [G][ceil(n / 128)][ceil(k / 128)])."""
-    _need(w, "w", (_f32, _bf16), (None, None, None))
+    _need(w, "w", (_f32, _bf16), 3)
     st = _here(stream, w)
     G, n, k = (w.shape[0], w.shape[2], w.shape[1]) if w_kn else w.shape
     q = torch.empty(G, n, k, dtype=_e4m3, device=w.device)
@@ -678,7 +689,7 @@ def fp8_quant_weights(w, w_kn: bool = False, stream=None):
 
 
 def _fp8_shapes(x, x_scale, ws):
-    _need(x, "x", _e4m3, (None, None))
+    _need(x, "x", _e4m3, 2)
     S, k = x.shape
     _need(x_scale, "x_scale", _f32, (S, _nblk(k)))
     G, n = None, None
@@ -722,8 +733,8 @@ def fp8_drelu(x, x_scale, w_gate, gate_scale, w_up, up_scale, offsets=None, row_
 def moe_combine(y, pair_row, w=None, out=None, out_dtype=None, stream=None):
     """ts_moe_combine.  y [rows][H] bf16 / f32, pair_row [T][K] int32, w [T][K]
     f32 or None (weights of one).  Returns out [T][H] (y's dtype unless given)."""
-    _need(y, "y", (_f32, _bf16), (None, None))
-    _need(pair_row, "pair_row", _i32, (None, None))
+    _need(y, "y", (_f32, _bf16), 2)
+    _need(pair_row, "pair_row", _i32, 2)
     T, K = pair_row.shape
     if w is not None:
         _need(w, "w", _f32, (T, K))
@@ -740,8 +751,8 @@ def moe_combine(y, pair_row, w=None, out=None, out_dtype=None, stream=None):
 def moe_combine_grad(d_out, y, pair_row, w, d_y=None, stream=None):
     """ts_moe_combine_grad.  Returns d_y [rows][H] (y's dtype; rows that no
     pair names are not written) and d_w [T][K]."""
-    _need(y, "y", (_f32, _bf16), (None, None))
-    _need(pair_row, "pair_row", _i32, (None, None))
+    _need(y, "y", (_f32, _bf16), 2)
+    _need(pair_row, "pair_row", _i32, 2)
     (R, H), (T, K) = y.shape, pair_row.shape
     _need(d_out, "d_out", (_f32, _bf16), (T, H))
     _need(w, "w", _f32, (T, K))

@@ -21,6 +21,19 @@
 // 2^-13 of it: with values drawn evenly over the codes 5e-5 of the result's
 // 2-norm, far under the codes' own 2^-4; everything behind is fp32.
 //
+// What bounds it: few rows, the weights' bytes (gate + up 4096 x 14336 bf16, 1
+// token 80 us = 5.9 TB/s; down, 32 tokens 156 us = 6.0 TB/s; fp8 gate + up, 4
+// tokens 98 us = 6.5 TB/s); many, the matrix cores and the power they draw
+// (gate + up, 8192 tokens, 8 experts 3.0 ms = 1.28 PFLOP/s, matrix cores busy in
+// 77% of the cycles at the 1.4 to 1.8 GHz that the load leaves; the same loop
+// without its loads 2.55 ms, a library product of that size 2.52), fp8 2.2 ms = 1.75 PFLOP/s (busy 44%: four
+// multiply-adds per matrix instruction for the scales run beside it).  Waves of
+// 128 x 64 out of 256 x 256: LDS reads take 0.8k of a step's 2k matrix cycles.
+// Tried and no better: four stages of 64 bytes (each 128-byte line asked for
+// twice, 3.77 ms), all loads of a stage at once (3.45), other starting blocks per
+// workgroup (3.02 to 3.12), persistent workgroups that load the next tile's first
+// stages ahead of the present one's stores (gate + up the same, weight gradients 3%).
+//
 // Chunks past the contraction's end come from a block of zeros (both operands:
 // 0 x 0, whatever lies behind), rows past a group's end repeat its last row
 // and are not stored.
@@ -312,9 +325,9 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
 
     const int last = blocks - 1;
     // Contracts the stages A, B.  Groups of MJ matrix instructions (one block
-    // of 16 P rows, one sub-step); operand reads run a group or two (where the registers allow) ahead, and
-    // between(group) issues the next stages' loads spread over the groups: all
-    // at once they hold up the waves that issue them.
+    // of 16 P rows, one sub-step); operand reads run a group or two (where the
+    // registers allow) ahead, and between(group) issues the next stages' loads
+    // spread over the groups: all at once they hold up the waves that issue them.
     constexpr int NS = KIND == kGmmFp8 ? 1 : RB / 64, NG = NS * MI;
     auto contract = [&](const u32x4 *A, const u32x4 *B, [[maybe_unused]] const float *scale, auto between) {
         using Frag = std::conditional_t<KIND == kGmmFp8, i32x8, u32x4>;
