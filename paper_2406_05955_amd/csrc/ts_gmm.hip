@@ -14,9 +14,9 @@ namespace ts {
 namespace {
 
 // Weight gradients: short contractions (a group's rows) over a large output, 1.9
-// GB in fp32 at 8 x 14336 x 4096.  6002 rows of 8 groups 1.21 ms (0.58 PFLOP/s),
-// of it 0.29 the stores (6.5 TB/s) and 0.16 the tiles' starts; 128 x 128 tiles
-// 1.76, 256 x 128 1.43 to 1.50.  Large outputs take the large tile (bf16, from one
+// GB in fp32 at 8 x 14336 x 4096.  6002 rows of 8 groups 0.95 ms (0.74 PFLOP/s),
+// of it 0.29 the stores (6.5 TB/s) and 0.16 the tiles' starts; groups of 6144 rows
+// 1.2 PFLOP/s.  128 x 128 tiles take half as long again, 256 x 128 a fifth more.  Large outputs take the large tile (bf16, from one
 // for each of 256 units on).
 template <GmmKind KIND>
 ts_status run_grad_w(const GmmArgs &a, hipStream_t st) {
