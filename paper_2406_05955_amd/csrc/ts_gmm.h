@@ -61,7 +61,11 @@ enum GmmMode { kFwd = 0, kDrelu = 1, kGradW = 2 };
 // lanes active).  Written out, with no register to return to: the compiler
 // follows its own loads into LDS and waits for all of them before any read of
 // LDS that it cannot tell apart, which empties the pipeline at every step.
-// The waits are the kernel's: gmm_barrier.
+// The waits are the kernel's: gmm_barrier.  Nor does it see what the text
+// reads: a vector load may take a base from scalar registers only five issue
+// slots after a vector instruction (readfirstlane, readlane) wrote them, a
+// scalar move at once.  So the load reads a scalar copy, whose move also fills
+// the slot that a load into LDS needs behind m0.
 __device__ __forceinline__ uint32_t lds_addr(const void *p) {
     return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p);
 }
@@ -76,14 +80,16 @@ __device__ __forceinline__ void ld_lds16(const char *p, uint32_t l) {
                  "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
 }
 __device__ __forceinline__ void ld_lds16(const char *base, uint32_t off, uint32_t l) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(uniform(base)),
-                 "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
+    uint64_t at;
+    asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0"
+                 : "=&s"(at) : "v"(off), "s"(uniform(base)), "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
 }
 __device__ __forceinline__ void ld_lds16(const char *base, size_t off, uint32_t l) { ld_lds16(base + off, l); }
 // 4 bytes a lane, at `l` + 4 x lane.
 __device__ __forceinline__ void ld_lds4(const char *base, uint32_t off, uint32_t l) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(uniform(base)),
-                 "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
+    uint64_t at;
+    asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dword %1, %0"
+                 : "=&s"(at) : "v"(off), "s"(uniform(base)), "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
 }
 __device__ __forceinline__ void ld_lds4(const char *base, size_t off, uint32_t l) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(base + off),

@@ -3,6 +3,7 @@ codes (nothing is enqueued) and the binding's own checks.  The plain 64-bit
 forms that the GPU tests compare with are held against one another here."""
 import itertools
 import os
+import re
 import subprocess
 
 import pytest
@@ -228,3 +229,25 @@ def test_the_gpu_tests_reach_every_tile(tmp_path):
             lines = "\n".join(f"{kind} {drelu} {G} {rows} {n} {ref.TILE_K[name]}" for rows, G, n in ref.TILE_SHAPES)
             r = subprocess.run([str(exe), "-"], input=lines, capture_output=True, text=True, check=True)
             assert set(map(int, r.stdout.split())) == ({1, 2, 3} if name == "f32" else set(range(6))), (name, drelu)
+
+
+def test_loads_written_out_read_scalar_copies():
+    """A vector load written in assembler is invisible to the compiler's waits:
+    it may read scalar registers only that its own text wrote with a scalar
+    instruction (a vector instruction's take five issue slots until then), and
+    m0 only one instruction after its write."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    csrc = os.path.join(root, "paper_2406_05955_amd", "csrc")
+    found = 0
+    for name in sorted(os.listdir(csrc)):
+        if not name.endswith((".h", ".hip")):
+            continue
+        with open(os.path.join(csrc, name)) as f:
+            text = f.read()
+        for m in re.finditer(r'asm volatile\(\s*"([^"]*global_load_lds[^"]*)"', text):
+            ops = m.group(1).split("\\n\\t")
+            assert ops[0].startswith("s_mov_b32 m0") and len(ops) == 3, (name, ops)
+            base = ops[-1].split()[-1]
+            assert base == "off" or ops[1].startswith(f"s_mov_b64 {base},"), (name, ops)
+            found += 1
+    assert found >= 4
