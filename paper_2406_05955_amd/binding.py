@@ -423,7 +423,10 @@ def moe_dense(x, w_router, w_gate, w_up, w_down_t, top_k: int, out=None, ws=None
 
 
 # ---------------------------------------------------------------------------
-# The MoE layer on any number of tokens, its gradients, its 8-bit form.
+# The MoE layer on any number of tokens, its gradients, its 8-bit form.  With
+# `stream`, a call runs there and what it makes is that stream's memory, as
+# under torch.cuda.stream(stream): memory that other streams freed may still be
+# in use there, and a workspace is freed as the call returns.
 
 _i32, _e4m3 = torch.int32, torch.float8_e4m3fn
 
@@ -445,8 +448,15 @@ def _need(t, name, dtype, shape):
         raise ValueError(f"{name} must be {want}, got {tuple(t.shape)}")
 
 
-def _here(stream, *ts):
-    """All tensors contiguous on the current device; the stream to launch on."""
+def _run_on(stream, f, *args):
+    if stream.device.index != torch.cuda.current_device():
+        raise ValueError(f"stream on {stream.device}, current device cuda:{torch.cuda.current_device()}")
+    with torch.cuda.stream(stream):
+        return f(*args)
+
+
+def _here(*ts):
+    """All tensors contiguous on the current device; the current stream."""
     d = _cur_device() if _cur_device is not None and torch.cuda.is_initialized() else None
     for t in ts:
         if t is None:
@@ -459,9 +469,7 @@ def _here(stream, *ts):
             d = torch.cuda.current_device()
         if t.get_device() != d:
             raise ValueError(f"tensor on {t.device}, current device cuda:{d}")
-    if stream is not None and stream.device.index != d:
-        raise ValueError(f"stream on {stream.device}, current device cuda:{d}")
-    return _stream(stream)
+    return _stream(None)
 
 
 def _new(out, name, shape, dtype, device):
@@ -490,8 +498,10 @@ def _maps(T, E, K, dev):
 def moe_route(logits, top_k: int, maps: bool = True, ws=None, stream=None):
     """ts_moe_route.  logits [T][E] f32.  Returns topk_idx, topk_w [T][K] and,
     with maps, offsets [E + 1], row_token [T K], pair_row [T][K]."""
+    if stream is not None:
+        return _run_on(stream, moe_route, logits, top_k, maps, ws)
     _need(logits, "logits", _f32, 2)
-    st = _here(stream, logits, ws)
+    st = _here(logits, ws)
     T, E = logits.shape
     K = int(top_k)
     if not 1 <= K <= E:
@@ -511,8 +521,10 @@ def moe_route(logits, top_k: int, maps: bool = True, ws=None, stream=None):
 def moe_group(topk_idx, n_experts: int, ws=None, stream=None):
     """ts_moe_group.  topk_idx [T][K] int32.  Returns offsets [E + 1],
     row_token [T K] (entries from offsets[E] on unspecified), pair_row [T][K]."""
+    if stream is not None:
+        return _run_on(stream, moe_group, topk_idx, n_experts, ws)
     _need(topk_idx, "topk_idx", _i32, 2)
-    st = _here(stream, topk_idx, ws)
+    st = _here(topk_idx, ws)
     T, K = topk_idx.shape
     E = int(n_experts)
     if E < 1:
@@ -528,6 +540,8 @@ def moe_group(topk_idx, n_experts: int, ws=None, stream=None):
 
 def moe_route_grad(topk_idx, topk_w, d_w, n_experts: int, out=None, stream=None):
     """ts_moe_route_grad: d_logits [T][E] from d_w [T][K] (the gradient of topk_w)."""
+    if stream is not None:
+        return _run_on(stream, moe_route_grad, topk_idx, topk_w, d_w, n_experts, out)
     _need(topk_idx, "topk_idx", _i32, 2)
     T, K = topk_idx.shape
     E = int(n_experts)
@@ -535,7 +549,7 @@ def moe_route_grad(topk_idx, topk_w, d_w, n_experts: int, out=None, stream=None)
         raise ValueError(f"n_experts must be positive, got {E}")
     _need(topk_w, "topk_w", _f32, (T, K))
     _need(d_w, "d_w", _f32, (T, K))
-    st = _here(stream, topk_idx, topk_w, d_w, out)
+    st = _here(topk_idx, topk_w, d_w, out)
     out = _new(out, "out", (T, E), _f32, topk_idx.device)
     code = lib.ts_moe_route_grad(_ptr(topk_idx), _ptr(topk_w), _ptr(d_w), T, E, K, _ptr(out), st)
     if code:
@@ -576,6 +590,8 @@ def grouped_mm(x, w, offsets=None, row_src=None, x2=None, w2=None, w_kn: bool = 
     f32, one dtype; x2, w2: a second product added to the first.  Returns out
     [rows][n] (out_dtype: x's unless given), rows = len(row_src) or S; rows
     outside the groups are not written."""
+    if stream is not None:
+        return _run_on(stream, grouped_mm, x, w, offsets, row_src, x2, w2, w_kn, out, out_dtype)
     _need(x, "x", (_f32, _bf16), 2)
     S, k = x.shape
     _need(w, "w", x.dtype, 3)
@@ -588,7 +604,7 @@ def grouped_mm(x, w, offsets=None, row_src=None, x2=None, w2=None, w_kn: bool = 
         _need(w2, "w2", x.dtype, tuple(w.shape))
     R = _rows_of(x, offsets, row_src, G)
     odt, od = _odtype(out, out_dtype, x.dtype)
-    st = _here(stream, x, w, x2, w2, offsets, row_src, out)
+    st = _here(x, w, x2, w2, offsets, row_src, out)
     out = _new(out, "out", (R, n), odt, x.device)
     code = lib.ts_grouped_mm(_ptr(x), _ptr(w), _ptr(x2), _ptr(w2), wdtype_of_rows(x.dtype), int(bool(w_kn)),
                              _ptr(row_src), _ptr(offsets), R, S, G, n, k, _ptr(out), od, st)
@@ -601,6 +617,8 @@ def grouped_drelu(x, w_gate, w_up, offsets=None, row_src=None, keep: bool = Fals
                   stream=None):
     """ts_grouped_drelu.  x [S][k]; w_gate, w_up [G][n][k].  Returns c
     [rows][n], or (c, gate, up) with keep."""
+    if stream is not None:
+        return _run_on(stream, grouped_drelu, x, w_gate, w_up, offsets, row_src, keep, out, out_dtype)
     _need(x, "x", (_f32, _bf16), 2)
     S, k = x.shape
     _need(w_gate, "w_gate", x.dtype, (None, None, k))
@@ -608,7 +626,7 @@ def grouped_drelu(x, w_gate, w_up, offsets=None, row_src=None, keep: bool = Fals
     G, n = w_gate.shape[:2]
     R = _rows_of(x, offsets, row_src, G)
     odt, od = _odtype(out, out_dtype, x.dtype)
-    st = _here(stream, x, w_gate, w_up, offsets, row_src, out)
+    st = _here(x, w_gate, w_up, offsets, row_src, out)
     out = _new(out, "out", (R, n), odt, x.device)
     gate, up = (torch.empty_like(out), torch.empty_like(out)) if keep else (None, None)
     code = lib.ts_grouped_drelu(_ptr(x), _ptr(w_gate), _ptr(w_up), wdtype_of_rows(x.dtype), _ptr(row_src),
@@ -620,10 +638,12 @@ def grouped_drelu(x, w_gate, w_up, offsets=None, row_src=None, keep: bool = Fals
 
 def drelu_grad(gate, up, d_c, stream=None):
     """ts_drelu_grad: (d_gate, d_up) of c = max(0, gate) * max(0, up)."""
+    if stream is not None:
+        return _run_on(stream, drelu_grad, gate, up, d_c)
     _need(gate, "gate", (_f32, _bf16), 2)
     _need(up, "up", gate.dtype, tuple(gate.shape))
     _need(d_c, "d_c", gate.dtype, tuple(gate.shape))
-    st = _here(stream, gate, up, d_c)
+    st = _here(gate, up, d_c)
     dg, du = torch.empty_like(gate), torch.empty_like(gate)
     code = lib.ts_drelu_grad(_ptr(gate), _ptr(up), _ptr(d_c), wdtype_of_rows(gate.dtype), gate.shape[0],
                              gate.shape[1], _ptr(dg), _ptr(du), st)
@@ -635,6 +655,8 @@ def drelu_grad(gate, up, d_c, stream=None):
 def grouped_mm_dw(d_y, x, offsets=None, row_src=None, out=None, out_dtype=None, stream=None):
     """ts_grouped_mm_dw.  d_y [rows][n], x [S][k] -> d_w [G][n][k] (f32 unless
     out_dtype or out says otherwise), G = len(offsets) - 1."""
+    if stream is not None:
+        return _run_on(stream, grouped_mm_dw, d_y, x, offsets, row_src, out, out_dtype)
     _need(x, "x", (_f32, _bf16), 2)
     _need(d_y, "d_y", x.dtype, 2)
     if offsets is not None:
@@ -647,7 +669,7 @@ def grouped_mm_dw(d_y, x, offsets=None, row_src=None, out=None, out_dtype=None, 
         raise ValueError(f"d_y has {d_y.shape[0]} rows, the product {R}")
     (S, k), n = x.shape, d_y.shape[1]
     odt, od = _odtype(out, out_dtype, _f32)
-    st = _here(stream, d_y, x, offsets, row_src, out)
+    st = _here(d_y, x, offsets, row_src, out)
     out = _new(out, "out", (G, n, k), odt, x.device)
     code = lib.ts_grouped_mm_dw(_ptr(d_y), _ptr(x), wdtype_of_rows(x.dtype), _ptr(row_src), _ptr(offsets), R, S, G,
                                 n, k, _ptr(out), od, st)
@@ -663,8 +685,10 @@ def _nblk(n):
 def fp8_quant(x, stream=None):
     """ts_fp8_quant.  x [rows][cols] bf16 / f32 -> (codes float8_e4m3fn
     [rows][cols], scale f32 [rows][ceil(cols / 128)])."""
+    if stream is not None:
+        return _run_on(stream, fp8_quant, x)
     _need(x, "x", (_f32, _bf16), 2)
-    st = _here(stream, x)
+    st = _here(x)
     R, C = x.shape
     q = torch.empty(R, C, dtype=_e4m3, device=x.device)
     s = torch.empty(R, _nblk(C), dtype=_f32, device=x.device)
@@ -677,8 +701,10 @@ def fp8_quant(x, stream=None):
 def fp8_quant_weights(w, w_kn: bool = False, stream=None):
     """ts_fp8_quant_weights.  w [G][n][k], or [G][k][n] with w_kn -> (codes
     [G][n][k], scale [G][ceil(n / 128)][ceil(k / 128)])."""
+    if stream is not None:
+        return _run_on(stream, fp8_quant_weights, w, w_kn)
     _need(w, "w", (_f32, _bf16), 3)
-    st = _here(stream, w)
+    st = _here(w)
     G, n, k = (w.shape[0], w.shape[2], w.shape[1]) if w_kn else w.shape
     q = torch.empty(G, n, k, dtype=_e4m3, device=w.device)
     s = torch.empty(G, _nblk(n), _nblk(k), dtype=_f32, device=w.device)
@@ -703,10 +729,12 @@ def _fp8_shapes(x, x_scale, ws):
 def fp8_mm(x, x_scale, w, w_scale, offsets=None, row_src=None, out=None, out_dtype=None, stream=None):
     """ts_fp8_mm on the codes and scales of fp8_quant and fp8_quant_weights.
     Returns out [rows][n] (bf16 unless out_dtype or out says otherwise)."""
+    if stream is not None:
+        return _run_on(stream, fp8_mm, x, x_scale, w, w_scale, offsets, row_src, out, out_dtype)
     S, k, G, n = _fp8_shapes(x, x_scale, (("w", w, w_scale),))
     R = _rows_of(x, offsets, row_src, G)
     odt, od = _odtype(out, out_dtype, _bf16)
-    st = _here(stream, x, x_scale, w, w_scale, offsets, row_src, out)
+    st = _here(x, x_scale, w, w_scale, offsets, row_src, out)
     out = _new(out, "out", (R, n), odt, x.device)
     code = lib.ts_fp8_mm(_ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(row_src), _ptr(offsets), R, S, G, n, k,
                          _ptr(out), od, st)
@@ -718,10 +746,13 @@ def fp8_mm(x, x_scale, w, w_scale, offsets=None, row_src=None, out=None, out_dty
 def fp8_drelu(x, x_scale, w_gate, gate_scale, w_up, up_scale, offsets=None, row_src=None, out=None, out_dtype=None,
               stream=None):
     """ts_fp8_drelu: grouped_drelu on quantised rows and weights."""
+    if stream is not None:
+        return _run_on(stream, fp8_drelu, x, x_scale, w_gate, gate_scale, w_up, up_scale, offsets, row_src, out,
+                       out_dtype)
     S, k, G, n = _fp8_shapes(x, x_scale, (("w_gate", w_gate, gate_scale), ("w_up", w_up, up_scale)))
     R = _rows_of(x, offsets, row_src, G)
     odt, od = _odtype(out, out_dtype, _bf16)
-    st = _here(stream, x, x_scale, w_gate, gate_scale, w_up, up_scale, offsets, row_src, out)
+    st = _here(x, x_scale, w_gate, gate_scale, w_up, up_scale, offsets, row_src, out)
     out = _new(out, "out", (R, n), odt, x.device)
     code = lib.ts_fp8_drelu(_ptr(x), _ptr(x_scale), _ptr(w_gate), _ptr(gate_scale), _ptr(w_up), _ptr(up_scale),
                             _ptr(row_src), _ptr(offsets), R, S, G, n, k, _ptr(out), od, st)
@@ -733,13 +764,15 @@ def fp8_drelu(x, x_scale, w_gate, gate_scale, w_up, up_scale, offsets=None, row_
 def moe_combine(y, pair_row, w=None, out=None, out_dtype=None, stream=None):
     """ts_moe_combine.  y [rows][H] bf16 / f32, pair_row [T][K] int32, w [T][K]
     f32 or None (weights of one).  Returns out [T][H] (y's dtype unless given)."""
+    if stream is not None:
+        return _run_on(stream, moe_combine, y, pair_row, w, out, out_dtype)
     _need(y, "y", (_f32, _bf16), 2)
     _need(pair_row, "pair_row", _i32, 2)
     T, K = pair_row.shape
     if w is not None:
         _need(w, "w", _f32, (T, K))
     odt, od = _odtype(out, out_dtype, y.dtype)
-    st = _here(stream, y, pair_row, w, out)
+    st = _here(y, pair_row, w, out)
     R, H = y.shape
     out = _new(out, "out", (T, H), odt, y.device)
     code = lib.ts_moe_combine(_ptr(y), wdtype_of_rows(y.dtype), _ptr(pair_row), _ptr(w), T, K, H, R, _ptr(out), od, st)
@@ -751,12 +784,14 @@ def moe_combine(y, pair_row, w=None, out=None, out_dtype=None, stream=None):
 def moe_combine_grad(d_out, y, pair_row, w, d_y=None, stream=None):
     """ts_moe_combine_grad.  Returns d_y [rows][H] (y's dtype; rows that no
     pair names are not written) and d_w [T][K]."""
+    if stream is not None:
+        return _run_on(stream, moe_combine_grad, d_out, y, pair_row, w, d_y)
     _need(y, "y", (_f32, _bf16), 2)
     _need(pair_row, "pair_row", _i32, 2)
     (R, H), (T, K) = y.shape, pair_row.shape
     _need(d_out, "d_out", (_f32, _bf16), (T, H))
     _need(w, "w", _f32, (T, K))
-    st = _here(stream, d_out, y, pair_row, w, d_y)
+    st = _here(d_out, y, pair_row, w, d_y)
     d_y = _new(d_y, "d_y", (R, H), y.dtype, y.device)
     d_w = torch.empty(T, K, dtype=_f32, device=y.device)
     code = lib.ts_moe_combine_grad(_ptr(d_out), wdtype_of_rows(d_out.dtype), _ptr(y), wdtype_of_rows(y.dtype),

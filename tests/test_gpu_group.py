@@ -670,6 +670,47 @@ def test_repeats_and_streams_give_the_same_bits():
         assert same(a, b)
 
 
+def test_a_given_stream_owns_what_the_call_makes(monkeypatch):
+    """Outputs and workspaces come from the memory of the stream that the call
+    runs on: from the current stream's, blocks whose last readers still run there
+    could be handed out, and a workspace handed on while the call runs."""
+    x, (wr, wg, wu, wd), K, d = small_layer(1500, 3)  # (two launches and a workspace to route)
+
+    def run(stream):
+        kw = {} if stream is None else {"stream": stream}
+        logits = ts.grouped_mm(x, wr[None], out_dtype=F32, **kw)
+        idx, w, off, tok, pair = ts.moe_route(logits, K, **kw)
+        off2, tok2, pair2 = ts.moe_group(idx, 8, **kw)
+        c, gate, up = ts.grouped_drelu(x, wg, wu, off, row_src=tok, keep=True, **kw)
+        y = ts.grouped_mm(c, wd, off, w_kn=True, **kw)
+        out = ts.moe_combine(y, pair, w, **kw)
+        d_y, d_w = ts.moe_combine_grad(d, y, pair, w, **kw)
+        d_l = ts.moe_route_grad(idx, w, d_w, 8, **kw)
+        d_g, d_u = ts.drelu_grad(gate, up, ts.grouped_mm(d_y, wd, off, **kw), **kw)
+        d_wg = ts.grouped_mm_dw(d_g, x, off, row_src=tok, **kw)
+        qx, qg = ts.fp8_quant(x, **kw), ts.fp8_quant_weights(wg, **kw)
+        qu, qd = ts.fp8_quant_weights(wu, **kw), ts.fp8_quant_weights(wd, w_kn=True, **kw)
+        c8 = ts.fp8_drelu(*qx, *qg, *qu, off, row_src=tok, **kw)
+        y8 = ts.fp8_mm(*ts.fp8_quant(c8, **kw), *qd, off, **kw)
+        return out, w, off2, tok2, pair2, d_y, d_l, d_u, d_wg, y8
+
+    want = run(None)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    made, empty = [], torch.empty
+
+    def watched(*args, **kw):
+        made.append(torch.cuda.current_stream())
+        return empty(*args, **kw)
+
+    monkeypatch.setattr(torch, "empty", watched)
+    got = run(s)
+    monkeypatch.undo()
+    s.synchronize()
+    assert len(made) > 20 and all(m == s for m in made)
+    assert same(got, want)
+
+
 @pytest.mark.parametrize("T", [1, 600])
 def test_graph_replays(T):
     """Forward and backward captured into one graph: replays with new inputs,
