@@ -380,7 +380,9 @@ ts_status ts_fp8_quant_weights(const void *w, ts_dtype dtype, int w_kn, int n_gr
 
 /* ts_grouped_mm and ts_grouped_drelu on quantised rows and weights
  * ([n_groups][n][k]): out[r][j] = sum over blocks b of x_scale[src(r)][b]
- * w_scale[g][j / 128][b] sum over i in b of x[src(r)][i] w[g][j][i]. */
+ * w_scale[g][j / 128][b] sum over i in b of x[src(r)][i] w[g][j][i].  The two
+ * scales are multiplied first, in fp32: both are representable apart and must
+ * be so together. */
 ts_status ts_fp8_mm(const void *x, const float *x_scale, const void *w, const float *w_scale, const int32_t *row_src,
                     const int32_t *offsets, int rows, int src_rows, int n_groups, int n, int k, void *out,
                     ts_dtype odtype, void *stream);

@@ -429,6 +429,13 @@ def moe_dense(x, w_router, w_gate, w_up, w_down_t, top_k: int, out=None, ws=None
 # in use there, and a workspace is freed as the call returns.
 
 _i32, _e4m3 = torch.int32, torch.float8_e4m3fn
+_int_max = 0x7fffffff
+
+
+def _need_int(name, ns):
+    """The library's sizes are C ints, to which larger numbers would wrap."""
+    if max(ns) > _int_max:
+        raise ValueError(f"{name}: extents must be below 2^31, got {tuple(ns)}")
 
 
 def _need(t, name, dtype, shape):
@@ -437,6 +444,8 @@ def _need(t, name, dtype, shape):
     dt = t.dtype
     if dt is dtype or (type(dtype) is tuple and dt in dtype):
         if (t.dim() == shape) if type(shape) is int else (t.shape == shape):
+            if t.numel() > _int_max:
+                _need_int(name, t.shape)
             return
     dts = dtype if isinstance(dtype, tuple) else (dtype,)
     if dt not in dts:
@@ -446,6 +455,7 @@ def _need(t, name, dtype, shape):
     if len(t.shape) != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
         want = "".join(f"[{'*' if w is None else w}]" for w in shape)
         raise ValueError(f"{name} must be {want}, got {tuple(t.shape)}")
+    _need_int(name, t.shape)
 
 
 def _run_on(stream, f, *args):
@@ -524,11 +534,11 @@ def moe_group(topk_idx, n_experts: int, ws=None, stream=None):
     if stream is not None:
         return _run_on(stream, moe_group, topk_idx, n_experts, ws)
     _need(topk_idx, "topk_idx", _i32, 2)
-    st = _here(topk_idx, ws)
     T, K = topk_idx.shape
     E = int(n_experts)
-    if E < 1:
-        raise ValueError(f"n_experts must be positive, got {E}")
+    if not 1 <= E <= _int_max:
+        raise ValueError(f"n_experts must be in 1..2^31 - 1, got {E}")
+    st = _here(topk_idx, ws)
     m = _maps(T, E, K, topk_idx.device)
     ws = _route_ws(topk_idx.device, ws, T, E, K)
     code = lib.ts_moe_group(_ptr(topk_idx), T, E, K, _ptr(m[0]), _ptr(m[1]), _ptr(m[2]), _ptr(ws),
@@ -545,8 +555,8 @@ def moe_route_grad(topk_idx, topk_w, d_w, n_experts: int, out=None, stream=None)
     _need(topk_idx, "topk_idx", _i32, 2)
     T, K = topk_idx.shape
     E = int(n_experts)
-    if E < 1:
-        raise ValueError(f"n_experts must be positive, got {E}")
+    if not 1 <= E <= _int_max:
+        raise ValueError(f"n_experts must be in 1..2^31 - 1, got {E}")
     _need(topk_w, "topk_w", _f32, (T, K))
     _need(d_w, "d_w", _f32, (T, K))
     st = _here(topk_idx, topk_w, d_w, out)

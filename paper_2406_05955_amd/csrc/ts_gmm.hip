@@ -157,7 +157,7 @@ ts_status ts_grouped_mm_dw(const void *d_y, const void *x, ts_dtype dtype, const
     ts_status s = check_fwd(x, d_y, dtype, odtype, row_src, offsets, rows, src_rows, n_groups, n, k, d_w, &empty);
     if (s != TS_OK) return s;
     if (!d_w) return TS_ERR_NULL;
-    if (!ts::aligned16(d_w)) return TS_ERR_ALIGN;
+    if (!ts::aligned16(d_w) || !ts::aligned4(offsets)) return TS_ERR_ALIGN;  // (read without rows, too)
     ts::GmmArgs a;
     a.w[0] = static_cast<const char *>(x);
     a.x[0] = static_cast<const char *>(d_y);

@@ -161,6 +161,30 @@ def test_binding_checks():
             call()
 
 
+def test_binding_refuses_extents_that_wrap():
+    """The library's sizes are C ints: 2^32 + 8 rows would count as 8."""
+    n, i32, f32 = 2 ** 32 + 8, torch.int32, torch.float32
+
+    def wide(cols, dtype=torch.bfloat16):
+        return torch.zeros(1, cols, dtype=dtype).expand(n, cols)  # (no memory)
+
+    w, off = z(2, 24, 16), z(3, dtype=i32)
+    for call in (lambda: ts.grouped_mm(wide(16), w, off), lambda: ts.grouped_drelu(wide(16), w, w, off),
+                 lambda: ts.grouped_mm(z(8, 16), w, off, row_src=z(1, dtype=i32).expand(n)),
+                 lambda: ts.grouped_mm_dw(wide(24), z(8, 16), off), lambda: ts.drelu_grad(wide(16), wide(16), wide(16)),
+                 lambda: ts.fp8_quant(wide(16)), lambda: ts.fp8_quant_weights(z(1, 1, 16).expand(2, n, 16)),
+                 lambda: ts.moe_route(wide(8, f32), 2), lambda: ts.moe_group(wide(2, i32), 8),
+                 lambda: ts.moe_group(z(8, 2, dtype=i32), n), lambda: ts.moe_combine(z(8, 16), wide(2, i32)),
+                 lambda: ts.moe_combine(wide(16), z(8, 2, dtype=i32)),
+                 lambda: ts.moe_route_grad(z(8, 2, dtype=i32), z(8, 2, dtype=f32), z(8, 2, dtype=f32), n)):
+        with pytest.raises(ValueError, match=r"2\^31"):
+            call()
+
+
+def test_weight_gradient_without_rows_still_checks_its_offsets():
+    assert dw(rows=0, x=None, w=None, off=A + 2) == ALIGN
+
+
 # --- the plain forms ---------------------------------------------------------------
 
 def test_plain_products_against_loops():
