@@ -507,40 +507,6 @@ def test_rows_of_x_past_4_gb(kind):
     within(ts.grouped_mm_dw(dev(d_y), x, od, row_src=sd), y, ref.sum_bound(mag, rows))
 
 
-@pytest.mark.parametrize("kind", ["bf16", "f32", "fp8"])
-def test_operands_between_2_and_4_gb(kind):
-    """The largest weight matrices, and rows of x, whose offsets need all of 32
-    bits."""
-    size = {"bf16": 2, "f32": 4, "fp8": 1}[kind]
-    n = 131072 if size > 1 else 131056
-    k = ((1 << 32) - 1) // (n * size) // 16 * 16 if size > 1 else 32752
-    assert 2 ** 32 - 2 ** 22 * size < n * k * size < 2 ** 32
-    dt = F32 if kind == "f32" else BF16
-    rows, g = 5, gen(83)
-    gd = torch.Generator(device=DEV).manual_seed(83)
-    cols = torch.tensor([0, 1, n // 2 - 1, n // 2, 3 * n // 4, n - 17, n - 1], device=DEV)
-    long = torch.randn(n, k, generator=gd, device=DEV, dtype=dt)
-    few = randn(g, rows, k, dtype=dt).to(DEV)
-    if kind == "fp8":
-        ql, qf = ts.fp8_quant_weights(long[None]), ts.fp8_quant(few)
-        rl = ql[0][0].float()[cols].double() * ql[1][0][cols // 128].repeat_interleave(128, 1)[:, :k].double()
-        rf = qf[0].double() * qf[1].repeat_interleave(128, 1)[:, :k].double()
-        out = ts.fp8_mm(*qf, *ql, out_dtype=F32)
-        # the matrix instruction's own cut at 2^-13 of groups of 8, the sums' roundings
-        bound = (2.0 ** -13 * 8 + k * 2.0 ** -24) * (rf.abs() @ rl.abs().t())
-        within(out[:, cols], rf @ rl.t(), bound)
-        return
-    want, mag = few.double() @ long[cols].double().t(), few.double().abs() @ long[cols].double().abs().t()
-    within(ts.grouped_mm(few, long[None], out_dtype=F32)[:, cols], want, ref.sum_bound(mag, k))
-    # the same memory as x: gathered, and in a weight gradient
-    src = cols.to(torch.int32)
-    within(ts.grouped_mm(long, few[None], row_src=src, out_dtype=F32), want.t(), ref.sum_bound(mag.t(), k))
-    d_y = randn(g, len(cols), 16, dtype=dt).to(DEV)
-    got = ts.grouped_mm_dw(d_y, long, row_src=src)[0]
-    want = d_y.double().t() @ long[cols].double()
-    within(got, want, ref.sum_bound(d_y.double().abs().t() @ long[cols].double().abs(), len(cols)))
-
-
 @pytest.mark.parametrize("kind,n,k", [("bf16", 131072, 16368), ("f32", 131072, 8176), ("fp8", 131056, 32752)])
 def test_operands_just_below_4_gb(kind, n, k):
     """The largest weight matrix, and as many rows of x: their offsets need all
