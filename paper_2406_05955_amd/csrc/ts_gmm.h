@@ -26,8 +26,9 @@
 // tokens 98 us = 6.5 TB/s); many, the matrix cores and the power they draw
 // (gate + up, 8192 tokens, 8 experts 3.0 ms = 1.28 PFLOP/s, matrix cores busy in
 // 77% of the cycles at the 1.4 to 1.8 GHz that the load leaves; the same loop
-// without its loads 2.55 ms, a library product of that size 2.52), fp8 2.2 ms = 1.75 PFLOP/s (busy 44%: four
-// multiply-adds per matrix instruction for the scales run beside it).  Waves of
+// without its loads 2.55 ms, a library product of that size 2.52), fp8 1.92 ms = 2.0
+// PFLOP/s (busy 51%: four multiply-adds per matrix instruction for the scales run beside
+// it; without them, and without the scales' loads, 1.58 ms).  Waves of
 // 128 x 64 out of 256 x 256: LDS reads take 0.8k of a step's 2k matrix cycles.
 // Tried and no better: four stages of 64 bytes (each 128-byte line asked for
 // twice, 3.77 ms), all loads of a stage at once (3.45), other starting blocks per
@@ -53,7 +54,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4g __attribute__((ext_vector_type(4)));
 
-static __device__ const u32x4 g_zero_chunk = {0u, 0u, 0u, 0u};
+static __device__ const u32x4 g_zero_chunk[8] = {};  // (a step's 128 bytes of a row)
 
 enum GmmMode { kFwd = 0, kDrelu = 1, kGradW = 2 };
 
@@ -203,14 +204,19 @@ struct GmmTile {
     }
 };
 
+// The workgroup's barrier for LDS.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // Until at most N of this wave's loads are on their way, then the workgroup's
 // barrier for LDS (its other loads stay in flight).
 template <int N>
 __device__ __forceinline__ void gmm_barrier() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    lds_barrier();
 }
 
 // 4 consecutive outputs.
@@ -239,7 +245,9 @@ __device__ __forceinline__ void unroll(F f) {
 constexpr int kStrip = 8;
 
 // WP x WQ waves; a wave's tile is (BP / WP) x (BQ / WQ).  AR, BR: stages of the P
-// operand (weights) and of the other; AR may be one more.  KW: groups of waves
+// operand (weights) and of the other; AR may be one more.  BR = 1 (fp8, whose
+// operands of a step are one read): one stage, which is loaded again behind a
+// second barrier once every wave has read it, and leaves room for AR = 3.  KW: groups of waves
 // that share the contraction's blocks, each with its own stages; their sums are
 // added at the end in a fixed order (few tiles with a long contraction: a step's
 // chain of barrier, operand reads and matrix instructions is what costs, and
@@ -257,13 +265,18 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
     static_assert(MODE != kGradW || ACOL, "the weight gradient contracts over rows");
     static_assert(MODE != kDrelu || (!ACOL && MI % 2 == 0), "gate and up in pairs of 16 rows");
 
-    static_assert(BR >= 2 && (AR == BR || AR == BR + 1), "P stages");
+    constexpr int LB = BR == 1 ? 2 : BR;  // steps that the other operand is loaded ahead, and one
+    static_assert(AR == LB || AR == LB + 1, "P stages");
     // fp8: a step's scales: NX waves fetch those of the rows, the others those
-    // of the tile's weight blocks
-    constexpr bool FP8 = KIND == kGmmFp8;
+    // of the tile's weight blocks.  BR = 1: the rows' for 8 blocks, a part in
+    // each step, into one of two halves (a lane for each row of one block asks
+    // for 64 lines at once: 2.20 ms of gate + up at 8192 tokens, 2.06 without);
+    // the weights' are scalar loads.
+    constexpr bool FP8 = KIND == kGmmFp8, AHEAD8 = FP8 && BR == 1;
     constexpr int NX = BQ < 64 ? 1 : BQ / 64, SS = FP8 ? THREADS : 0;
     static_assert(!FP8 || THREADS / 64 >= NX + 2, "two waves for weight scales");
-    constexpr int ALL = AR * TA::CHUNKS + BR * TB::CHUNKS + BR * SS / 4;
+    static_assert(BR > 1 || (FP8 && KW == 1 && !WIDE && BQ == THREADS / 2), "4 loads a wave for 8 blocks of scales");
+    constexpr int ALL = AR * TA::CHUNKS + BR * TB::CHUNKS + (AHEAD8 ? 2 * BQ * 8 / 4 : BR * SS / 4);
     static_assert(KW == 1 || MODE != kGradW, "the weight gradient's contraction is short");
     __shared__ u32x4 s_all[KW * ALL];
     const int kg = KW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
@@ -341,7 +354,13 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
     // registers allow) ahead, and between(group) issues the next stages' loads
     // spread over the groups: all at once they hold up the waves that issue them.
     constexpr int NS = KIND == kGmmFp8 ? 1 : RB / 64, NG = NS * MI;
-    auto contract = [&](const u32x4 *A, const u32x4 *B, [[maybe_unused]] const float *scale, auto between) {
+    // (fp8 dReLU: the gate's blocks, then the up projection's: one set of factors)
+    constexpr auto order = [](int G) constexpr {
+        return FP8 && MODE == kDrelu ? G % (MI / 2) * 2 + G / (MI / 2) : G % MI;
+    };
+    [[maybe_unused]] int slot8 = 0;  // the step's among 8 scales
+    auto contract = [&](const u32x4 *A, const u32x4 *B, [[maybe_unused]] const float *scale,
+                        [[maybe_unused]] const float (&wscale)[2], auto between) {
         using Frag = std::conditional_t<KIND == kGmmFp8, i32x8, u32x4>;
         auto read = [&](auto tile, const u32x4 *t, int blk, int s) -> Frag {
             using T = decltype(tile);
@@ -357,38 +376,47 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
 #pragma unroll
         for (int j = 0; j < MJ; ++j) bf[0][j] = read(TB{}, B, wq * MJ + j, 0);
         unroll<AHEAD>([&](auto gi) {
-            if constexpr (gi < NG) af[gi] = read(TA{}, A, wp * MI + gi % MI, gi / MI);
+            if constexpr (gi < NG) af[gi] = read(TA{}, A, wp * MI + order(gi), gi / MI);
         });
-        // the factors of this lane's columns (dReLU: for gate and for up)
-        [[maybe_unused]] float f[2][MJ];
-        if constexpr (FP8) {
-            const int sel = MODE == kDrelu ? 0 : wp * (BP / WP) / kScaleBlock;
-            const float w0 = scale[(NX + sel) * 64 + lane], w1 = MODE == kDrelu ? scale[(NX + 1) * 64 + lane] : w0;
+        // the factors of this lane's columns
+        [[maybe_unused]] float f[MJ];
+        [[maybe_unused]] f32x4 d[2][MJ];
+        [[maybe_unused]] auto factors = [&](auto up) {
+            const int sel = MODE == kDrelu ? (int)up : wp * (BP / WP) / kScaleBlock;
+            const float w = AHEAD8 ? wscale[up] : scale[(NX + sel) * 64 + lane];
+            constexpr int ROW = AHEAD8 ? 8 : 1;
+            const float *x = scale + (wq * MJ * 16 + lm) * ROW + (AHEAD8 ? slot8 ^ lm >> 2 : 0);
 #pragma unroll
-            for (int j = 0; j < MJ; ++j) {
-                const float x = scale[(wq * MJ + j) * 16 + lm];
-                f[0][j] = x * w0;
-                f[1][j] = x * w1;
-            }
-        }
+            for (int j = 0; j < MJ; ++j) f[j] = x[j * 16 * ROW] * w;
+        };
         unroll<NG>([&](auto gi) {
-            constexpr int G = gi, s = G / MI, i = G % MI;
+            constexpr int G = gi, s = G / MI, i = order(G);
             constexpr int NX = G + AHEAD;
-            if constexpr (NX < NG) af[NX % (AHEAD + 1)] = read(TA{}, A, wp * MI + NX % MI, NX / MI);
+            if constexpr (NX < NG) af[NX % (AHEAD + 1)] = read(TA{}, A, wp * MI + order(NX), NX / MI);
             if constexpr (s + 1 < NS) {
                 // the next sub-step's Q operands, over this one's groups
 #pragma unroll
                 for (int j = i * MJ / MI; j < (i + 1) * MJ / MI; ++j) bf[s + 1][j] = read(TB{}, B, wq * MJ + j, s + 1);
             }
             const Frag a_ = af[G % (AHEAD + 1)];
-            if constexpr (KIND == kGmmFp8) {
+            if constexpr (FP8) {
+                // this group's products, the factors times the last one's (its own
+                // would be waited for: with the order below 2.17 -> 1.99 ms of gate +
+                // up at 8192 tokens, the third weight stage included)
+                if constexpr (G == 0) factors(std::integral_constant<int, 0>{});
 #pragma unroll
                 for (int j = 0; j < MJ; ++j) {
                     // both formats e4m3; block exponents 127: factors of one
-                    const f32x4 d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                    d[G & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
                         a_, bf[0][j], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
-                    acc[i][j] += d * f[i & 1][j];
+                    if constexpr (G > 0) acc[order(G - 1)][j] += d[(G - 1) & 1][j] * f[j];
                 }
+                if constexpr (MODE == kDrelu && G == MI / 2) factors(std::integral_constant<int, 1>{});
+                // (in this order: the scheduler puts the sums first, which wait)
+                if constexpr (G > 0) unroll<MJ>([&](auto) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+                });
             } else if constexpr (KIND == kGmmBf16) {
 #pragma unroll
                 for (int j = 0; j < MJ; ++j)
@@ -405,11 +433,15 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
             between(gi);
             __builtin_amdgcn_sched_barrier(0);
         });
+        if constexpr (FP8)
+#pragma unroll
+            for (int j = 0; j < MJ; ++j) acc[order(NG - 1)][j] += d[(NG - 1) & 1][j] * f[j];
     };
 
     // The last block, the only one that may be partial, is contracted first;
     // the loads of the others check nothing.
-    for (int pair = 0; blocks > 0 && pair < a.pairs; ++pair) {
+    const int pairs = MODE == kFwd && !FP8 ? a.pairs : 1;
+    for (int pair = 0; blocks > 0 && pair < pairs; ++pair) {
         // dReLU: a wave's chunks are of 64 / CR consecutive rows (and of those
         // 32 or more further on), so all of w_gate or all of w_up
         const bool second = MODE == kDrelu ? ((wave * (64 / TA::CR)) >> 4) & 1 : pair == 1;
@@ -422,6 +454,9 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
         // (weight gradient: aoff in a row of x; the rows are looked up block by
         // block); the contraction index of its first chunk.
         std::conditional_t<MODE == kGradW, Off, uint32_t> aoff[TA::NJ];
+        // (BR = 1, short of registers: rows, whose offsets in x and in the scales
+        // follow from them, and the first chunk's column)
+        [[maybe_unused]] u32x4 rows4;
         std::conditional_t<MODE == kGradW, uint32_t, Off> boff[TB::NJ];
         Off rowoff[MODE == kGradW ? TA::NJ : 1];
         int ka, kb;
@@ -436,7 +471,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
                 aoff[j] = (uint32_t)row * (uint32_t)(a.n * SZ) + (uint32_t)min(p0 * SZ + ch * 16, a.n * SZ - 16);
             } else {
                 const int n = MODE == kDrelu ? p0 + (row >> 5) * 16 + (row & 15) : p0 + row;
-                aoff[j] = (uint32_t)min(n, a.n - 1) * (uint32_t)(a.k * SZ) + ch * 16;
+                aoff[j] = AHEAD8 ? n : (uint32_t)min(n, a.n - 1) * (uint32_t)(a.k * SZ) + ch * 16;
             }
         }
 #pragma unroll
@@ -446,6 +481,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
             if (j == 0) kb = BCOL ? row : ch * (16 / SZ);
             if constexpr (MODE == kGradW)
                 boff[j] = (uint32_t)row * (uint32_t)(a.n * SZ) + (uint32_t)min(q0 * SZ + ch * 16, a.n * SZ - 16);
+            else if constexpr (AHEAD8) rows4[j] = source(min(q0 + row, e - 1));
             else
                 boff[j] = (Off)source(min(q0 + row, e - 1)) * xrow + ch * 16;
         }
@@ -484,18 +520,33 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
                 });
             }
         };
+        uint32_t krow = a.k;  // (BR = 1)
         auto a_off = [&](auto j) {
             if constexpr (MODE == kGradW) return (Off)(rowoff[j] + aoff[j]);
+            else if constexpr (AHEAD8)
+                return (uint32_t)min((int)aoff[0] + j * (MODE == kDrelu ? 32 : 64), a.n - 1) * krow + ka;
             else return aoff[j];
+        };
+        auto b_off = [&](auto j) {
+            if constexpr (AHEAD8) return rows4[(int)j] * krow + kb;
+            else return boff[j];
         };
         const uint32_t lds_a = lds_addr(s_a) + wave * 1024, lds_b = lds_a + AR * TA::CHUNKS * 16;
         [[maybe_unused]] const uint32_t lds_s = lds_addr(s_s) + wave * 256;
         // this wave's scales: a row's (or a weight block's) are one after another
         const float *sbase = a.xs;
         Off soff = 0;
+        typedef const __attribute__((address_space(4))) float cfloat;
+        [[maybe_unused]] cfloat *wsbase[2];
+        float wscale[2] = {};
         if constexpr (FP8) {
             const int kbn = (a.k + kScaleBlock - 1) / kScaleBlock, nbn = (a.n + kScaleBlock - 1) / kScaleBlock;
-            if (wave < NX) {
+            if constexpr (AHEAD8) {
+                const int nb = min(p0 / kScaleBlock + (MODE == kDrelu ? 0 : wp * (BP / WP) / kScaleBlock), nbn - 1);
+                const size_t at = ((size_t)g * nbn + nb) * kbn;
+                wsbase[0] = (cfloat *)reinterpret_cast<uintptr_t>(a.ws[0] + at);
+                wsbase[1] = MODE == kDrelu ? (cfloat *)reinterpret_cast<uintptr_t>(a.ws[1] + at) : wsbase[0];
+            } else if (wave < NX) {
                 soff = (Off)source(min(q0 + wave * 64 + lane, e - 1)) * (Off)(4 * kbn);
             } else {
                 const int sel = (wave - NX) & 1;
@@ -507,10 +558,26 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
         auto load_a = [&](auto j, int blk, int to) {
             ld_lds16(abase + blk * astep, a_off(j), lds_a + (uint32_t)(to * TA::CHUNKS + THREADS * j) * 16);
         };
+        // the scales of the rows' 8 blocks 8 c ... (-1: the last block), a fourth
+        // of this wave's
+        auto load_s8 = [&](int i, int c) {
+            // (masks: a branch on i would let the matrix instructions sink past it)
+            const uint32_t m1 = -(i & 1), m2 = -(i >> 1 & 1);
+            const uint32_t lo = rows4.x ^ ((rows4.x ^ rows4.y) & m1), hi = rows4.z ^ ((rows4.z ^ rows4.w) & m1);
+            const uint32_t row = lo ^ ((lo ^ hi) & m2);
+            // (a row's 8 permuted by the row: reads of 16 rows cover 16 banks)
+            const int blk = c < 0 ? last : min(c * 8 + ((lane & 7) ^ (wave << 1 & 2) ^ lane >> 5), last);
+            ld_lds4(reinterpret_cast<const char *>(a.xs), 4 * (row * (uint32_t)blocks + blk),
+                    lds_s + (uint32_t)((c & 1) * BQ * 32 + i * 2048));
+        };
         auto load_b = [&](auto j, int blk, int to) {
-            if constexpr (j == TB::NJ)
+            if constexpr (j == TB::NJ && AHEAD8)
+                load_s8(to & 3, to >> 2);  // (part and blocks, see below)
+            else if constexpr (j == TB::NJ)
                 ld_lds4(reinterpret_cast<const char *>(sbase + blk), soff, lds_s + (uint32_t)(to * SS) * 4);
-            else ld_lds16(bbase + blk * bstep, boff[j], lds_b + (uint32_t)(to * TB::CHUNKS + THREADS * j) * 16);
+            else
+                ld_lds16(bbase + blk * bstep, b_off(j),
+                         lds_b + (uint32_t)((BR == 1 ? 0 : to) * TB::CHUNKS + THREADS * j) * 16);
         };
 
         if (kg == 0) {
@@ -518,9 +585,18 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
             take();
             const int left = C - last * KS;
             unroll<TB::NJ>([&](auto j) {
-                ld_lds16(kb + JB * j < left ? bbase + last * bstep + boff[j] : zero, lds_b + 16 * THREADS * j);
+                ld_lds16(kb + JB * j < left ? bbase + last * bstep + b_off(j) : zero, lds_b + 16 * THREADS * j);
             });
-            if constexpr (FP8) load_b(std::integral_constant<int, TB::NJ>{}, last, 0);
+            if constexpr (AHEAD8) {
+                unroll<4>([&](auto i) {
+                    load_s8(i, -1);
+                    load_s8(i, 0);
+                });
+                wscale[0] = wsbase[0][last];
+                wscale[1] = wsbase[1][last];
+            } else if constexpr (FP8) {
+                load_b(std::integral_constant<int, TB::NJ>{}, last, 0);
+            }
             unroll<TA::NJ>([&](auto j) {
                 ld_lds16(ka + JA * j < left ? abase + last * astep + a_off(j) : zero, lds_a + 16 * THREADS * j);
             });
@@ -529,10 +605,13 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
             // no whole block to load: zeros
             abase = bbase = zero;
             astep = bstep = 0;
+            krow = 0;
+            if constexpr (!AHEAD8) {
 #pragma unroll
-            for (int j = 0; j < TA::NJ; ++j) aoff[j] = 0;
+                for (int j = 0; j < TA::NJ; ++j) aoff[j] = 0;
 #pragma unroll
-            for (int j = 0; j < TB::NJ; ++j) boff[j] = 0;
+                for (int j = 0; j < TB::NJ; ++j) boff[j] = 0;
+            }
             if constexpr (MODE == kGradW)
 #pragma unroll
                 for (int j = 0; j < TA::NJ; ++j) rowoff[j] = 0;
@@ -549,7 +628,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
                 unroll<LOADS_A>([&](auto j) { load_a(j, block(0), 0); });
             }
         unroll<AR - 2>([&](auto i) {
-            if constexpr (i < BR - 2) unroll<LOADS_B>([&](auto j) { load_b(j, block(i + 1), i + 1); });
+            if constexpr (i < LB - 2) unroll<LOADS_B>([&](auto j) { load_b(j, block(i + 1), i + 1); });
             if (last > 0) {
                 ask(block(i + 1));
                 take();
@@ -563,17 +642,32 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
         int ar = 0, br = 0;  // stages of step t
         for (int t = 0; t * KW <= last; ++t) {
             // what may be on its way: all that was asked for behind this step's
-            gmm_barrier<(AR == BR ? (BR - 2) * LOADS : (BR - 2) * LOADS + LOADS_A)>();
-            const int blk_a = block(t + AR - 1), blk_b = block(t + BR - 1);
+            gmm_barrier<(AR == LB ? (LB - 2) * LOADS : (LB - 2) * LOADS + LOADS_A)>();
+            const int blk_a = block(t + AR - 1), blk_b = block(t + LB - 1);
             ask(block(t + AR));
-            const int to_a = ar == 0 ? AR - 1 : ar - 1, to_b = br == 0 ? BR - 1 : br - 1;
+            // (computed again in every step: held over the loop, the offsets spill)
+            if constexpr (AHEAD8) asm volatile("" : "+v"(aoff[0]), "+v"(kb));
+            // (BR = 1: which of 8 scales are this step's, and which part of the
+            // next 8 blocks' is loaded)
+            const int u = t - 1;
+            slot8 = u & 7;
+            const int to_a = ar == 0 ? AR - 1 : ar - 1;
+            const int to_b = AHEAD8 ? ((u >> 3) + 1) * 4 + (u & 3) : br == 0 ? BR - 1 : br - 1;
+            [[maybe_unused]] float wnext[2];
+            if constexpr (AHEAD8) {
+                wnext[0] = wsbase[0][block(t + 1)];
+                wnext[1] = wsbase[1][block(t + 1)];
+            }
             if (KW == 1 || kg + t * KW <= last)
-                contract(s_a + ar * TA::CHUNKS, s_b + br * TB::CHUNKS, s_s + br * SS, [&](auto gi) {
+                contract(s_a + ar * TA::CHUNKS, s_b + br * TB::CHUNKS,
+                         s_s + (AHEAD8 ? (u >> 3 & 1) * BQ * 8 : br * SS), wscale, [&](auto gi) {
                     // (in the earlier half of the groups, the later half covers
                     // the last loads' way: gate + up at 8192 tokens 2.98 ms,
-                    // spread over all groups 3.06; fp8, whose groups are twice as
-                    // long, 2.36 / 2.30)
-                    constexpr int G = gi, OVER = FP8 || NG < 2 ? NG : NG / 2;
+                    // spread over all groups 3.06; fp8 1.99 / 2.07)
+                    constexpr int G = gi, OVER = NG < 2 ? NG : NG / 2;
+                    // (every wave's operands of the first group are in its
+                    // registers: all of the Q operand's)
+                    if constexpr (BR == 1 && G == 0) lds_barrier();
                     if constexpr (G < OVER)
                         unroll<(G + 1) * LOADS / OVER - G * LOADS / OVER>([&](auto l) {
                             constexpr int L = G * LOADS / OVER + l;
@@ -582,8 +676,12 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
                         });
                 });
             if (last > 0) take();
+            if constexpr (AHEAD8) {
+                wscale[0] = wnext[0];
+                wscale[1] = wnext[1];
+            }
             ar = ar == AR - 1 ? 0 : ar + 1;
-            br = br == BR - 1 ? 0 : br + 1;
+            br = BR == 1 || br == BR - 1 ? 0 : br + 1;
         }
         gmm_barrier<0>();
     }
@@ -680,8 +778,9 @@ ts_status run_fwd(const char *name, const GmmArgs &a, hipStream_t st) {
             if constexpr (KIND != kGmmF32) return run_tiled<KIND, MODE, ACOL, 256, 128, 4, 2, 3, 3>(name, a, st);
             break;
         default:
-            // (fp8: a third stage of the weights and the scales are more than LDS holds)
-            if constexpr (KIND == kGmmFp8) return run_tiled<KIND, MODE, ACOL, 256, 256, 2, 4, 2, 2>(name, a, st);
+            // (fp8: a third stage of the weights, two of the rows and the scales are
+            // more than LDS holds)
+            if constexpr (KIND == kGmmFp8) return run_tiled<KIND, MODE, ACOL, 256, 256, 2, 4, 3, 1>(name, a, st);
             else if constexpr (KIND == kGmmBf16) return run_tiled<KIND, MODE, ACOL, 256, 256, 2, 4, 3, 2>(name, a, st);
     }
     return TS_ERR_UNSUPPORTED;

@@ -31,6 +31,9 @@ TILE_SHAPES = [(41, 1, 144), (41, 1, 6160), (41, 1, 8208), (41, 5, 4112), (41, 5
                (300, 5, 6160), (300, 5, 8208), (700, 5, 4112), (700, 5, 6160), (700, 5, 8208), (1000, 1, 2064),
                (2500, 1, 1552), (4000, 1, 144)]
 TILE_K = {"bf16": 336, "f32": 336, "fp8": 720}
+# the fp8 tile that fetches the rows' scales of 8 blocks at a time: 9 to 23 blocks
+EIGHTS = (1500, 3, 8208)
+EIGHTS_K = (1152, 1168, 2176, 2832)
 
 
 def mm(x, w, offsets, row_src=None, w_kn=False):

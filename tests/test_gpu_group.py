@@ -377,6 +377,30 @@ def test_fp8_block_exponents():
     within(ts.fp8_mm(q, s, wq, wsc, out_dtype=F32), y, bound)
 
 
+@pytest.mark.parametrize("k", ref.EIGHTS_K)
+def test_fp8_many_scale_blocks(k):
+    """Each block of 128 its own powers of two, rows and weights: a scale of
+    another block would show."""
+    rows, G, n = ref.EIGHTS
+    g = gen(34, k)
+    nb = -(-k // 128)
+    blocks = lambda *s: 2.0 ** torch.randint(-6, 7, (*s, nb), generator=g).float().repeat_interleave(128, len(s))[..., :k]  # noqa: E731
+    gd = torch.Generator(device=DEV).manual_seed(k)
+    x = torch.randn(rows // 2, k, generator=gd, device=DEV) * dev(blocks(rows // 2))
+    wg, wu = (torch.randn(G, n, k, generator=gd, device=DEV) * dev(blocks(G, 1)) * k ** -0.5 for _ in range(2))
+    offsets = ref.ragged(rows, G, g, lead=2, tail=3)
+    src = torch.randint(0, rows // 2, (rows,), generator=g, dtype=torch.int32)
+    off, sd = dev(offsets, src)
+    (xq, xs), qg, qu = ts.fp8_quant(x), ts.fp8_quant_weights(wg), ts.fp8_quant_weights(wu)
+    (gt, eg), (up, eu) = (fp8_want(xq, xs, *q, offsets, sd) for q in (qg, qu))
+    mid = slice(2, rows - 3)
+    within(ts.fp8_mm(xq, xs, *qg, off, row_src=sd, out_dtype=F32)[mid], gt[mid], eg[mid])
+    c = ref.drelu(gt, up)
+    bound = ref.drelu_bound(gt, up, eg, eu) + 2.0 ** -23 * c.abs()
+    got = ts.fp8_drelu(xq, xs, *qg, *qu, off, row_src=sd, out_dtype=F32)
+    within(got[mid], c[mid], bound[mid])
+
+
 # --- combine ---------------------------------------------------------------------
 
 @pytest.mark.parametrize("ydt,odt", [(BF16, BF16), (F32, F32), (BF16, F32), (F32, BF16)])

@@ -255,6 +255,14 @@ def test_the_gpu_tests_reach_every_tile(tmp_path):
             assert set(map(int, r.stdout.split())) == ({1, 2, 3} if name == "f32" else set(range(6))), (name, drelu)
 
 
+def test_the_gpu_tests_of_many_scale_blocks_take_the_large_tile(tmp_path):
+    exe = build_check(tmp_path, "-O2")
+    rows, G, n = ref.EIGHTS
+    lines = "\n".join(f"2 {drelu} {G} {rows} {n} {k}" for drelu in (0, 1) for k in ref.EIGHTS_K)
+    r = subprocess.run([str(exe), "-"], input=lines, capture_output=True, text=True, check=True)
+    assert set(map(int, r.stdout.split())) == {0}, r.stdout
+
+
 def test_loads_written_out_read_scalar_copies():
     """A vector load written in assembler is invisible to the compiler's waits:
     it may read scalar registers only that its own text wrote with a scalar
