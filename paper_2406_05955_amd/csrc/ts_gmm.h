@@ -772,6 +772,9 @@ ts_status run_fwd(const char *name, const GmmArgs &a, hipStream_t st) {
         case kTile64x64:
             if constexpr (KIND != kGmmF32) return run_tiled<KIND, MODE, ACOL, 64, 64, 2, 2, 4, 4, 2>(name, a, st);
             break;
+        case kTile32x32:
+            if constexpr (MODE != kDrelu) return run_tiled<KIND, MODE, ACOL, 32, 32, 2, 2, 3, 3, 3>(name, a, st);
+            break;
         case kTile128x64: return run_tiled<KIND, MODE, ACOL, 128, 64, 4, 1, 3, 3>(name, a, st);
         case kTile128x128: return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2>(name, a, st);
         case kTile256x128:

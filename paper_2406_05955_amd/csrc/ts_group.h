@@ -40,12 +40,13 @@ struct GmmArgs {
 // Tiles of the forward products: columns (dReLU: of gate and up together) x
 // rows, workgroups of it that a compute unit holds, stages, contraction groups.
 // (equal costs: the first)
-enum GmmTileId { kTile256x256 = 0, kTile128x128, kTile128x64, kTile64x32, kTile256x128, kTile64x64, kTiles };
+enum GmmTileId { kTile256x256 = 0, kTile128x128, kTile128x64, kTile64x32, kTile256x128, kTile64x64, kTile32x32, kTiles };
 struct GmmTileSize {
     int p, q, per_unit, stages, kw;
 };
 constexpr GmmTileSize kTileSize[kTiles] = {{256, 256, 1, 2, 1}, {128, 128, 2, 2, 1}, {128, 64, 2, 3, 1},
-                                           {64, 32, 2, 3, 2},   {256, 128, 1, 3, 1}, {64, 64, 1, 4, 2}};
+                                           {64, 32, 2, 3, 2},   {256, 128, 1, 3, 1}, {64, 64, 1, 4, 2},
+                                           {32, 32, 2, 3, 3}};
 GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k);
 
 ts_status check_group_dims(int rows, int groups, int n, int k, int quantum);

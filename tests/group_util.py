@@ -29,7 +29,7 @@ def ragged(rows, groups, gen, lead=0, tail=0):
 # these contractions: several whole blocks (the stages' rings wrap) and a partial one
 TILE_SHAPES = [(41, 1, 144), (41, 1, 6160), (41, 1, 8208), (41, 5, 4112), (41, 5, 8208), (100, 5, 6160), (300, 5, 4112),
                (300, 5, 6160), (300, 5, 8208), (700, 5, 4112), (700, 5, 6160), (700, 5, 8208), (1000, 1, 2064),
-               (2500, 1, 1552), (4000, 1, 144)]
+               (2500, 1, 1552), (4000, 1, 144), (300, 5, 2064), (700, 5, 2064), (2300, 1, 1552)]
 TILE_K = {"bf16": 336, "f32": 336, "fp8": 720}
 # the fp8 tile that fetches the rows' scales of 8 blocks at a time: 9 to 23 blocks
 EIGHTS = (1500, 3, 8208)

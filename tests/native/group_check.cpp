@@ -36,6 +36,8 @@ int main(int argc, char **) {
                             CHECK(t >= 0 && t < kTiles);
                             // fp32 has no tile of 256 and no 64 x 64
                             CHECK(kind != kGmmF32 || (kTileSize[t].p < 256 && t != kTile64x64));
+                            // 32 x 32 is too narrow for gate and up side by side
+                            CHECK(!drelu || t != kTile32x32);
                         }
     for (int k = 1; k <= kMaxTopK; ++k)
         for (int t : {0, 1, 2, 127, 128, 129, 512, 1024, 1025, 5000, 65536, 1000000, kMaxRows / 8}) {

@@ -246,13 +246,14 @@ def test_host_side_under_sanitizers(tmp_path):
 
 def test_the_gpu_tests_reach_every_tile(tmp_path):
     """The shapes that the GPU tests take run every tile that the rule can
-    choose, forward and with dReLU (fp32: three of the six)."""
+    choose: seven forward, six with dReLU (fp32: three of those)."""
     exe = build_check(tmp_path, "-O2")
     for kind, name in enumerate(("bf16", "f32", "fp8")):
         for drelu in (0, 1):
             lines = "\n".join(f"{kind} {drelu} {G} {rows} {n} {ref.TILE_K[name]}" for rows, G, n in ref.TILE_SHAPES)
             r = subprocess.run([str(exe), "-"], input=lines, capture_output=True, text=True, check=True)
-            assert set(map(int, r.stdout.split())) == ({1, 2, 3} if name == "f32" else set(range(6))), (name, drelu)
+            want = ({1, 2, 3} if name == "f32" else set(range(6))) | (set() if drelu else {6})
+            assert set(map(int, r.stdout.split())) == want, (name, drelu)
 
 
 def test_the_gpu_tests_of_many_scale_blocks_take_the_large_tile(tmp_path):
