@@ -22,7 +22,7 @@
 // 2-norm, far under the codes' own 2^-4; everything behind is fp32.
 //
 // What bounds it: few rows, the weights' bytes (gate + up 4096 x 14336 bf16, 1
-// token 80 us = 5.9 TB/s; down, 32 tokens 156 us = 6.0 TB/s; fp8 gate + up, 4
+// token 80 to 88 us = 5.9 to 5.3 TB/s; down, 32 tokens 156 to 170 us; fp8 gate + up, 4
 // tokens 98 us = 6.5 TB/s); many, the matrix cores and the power they draw
 // (gate + up, 8192 tokens, 8 experts 3.0 ms = 1.28 PFLOP/s, matrix cores busy in
 // 77% of the cycles at the 1.4 to 1.8 GHz that the load leaves; the same loop
