@@ -66,7 +66,8 @@ enum GmmMode { kFwd = 0, kDrelu = 1, kGradW = 2 };
 // reads: a vector load may take a base from scalar registers only five issue
 // slots after a vector instruction (readfirstlane, readlane) wrote them, a
 // scalar move at once.  So the load reads a scalar copy, whose move also fills
-// the slot that a load into LDS needs behind m0.
+// the slot that a load into LDS needs behind m0.  m0 is an output of the text:
+// named as a clobber the compiler is free to overlook it (a reserved register).
 __device__ __forceinline__ uint32_t lds_addr(const void *p) {
     return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p);
 }
@@ -77,24 +78,30 @@ __device__ __forceinline__ const char *uniform(const void *p) {
     return reinterpret_cast<const char *>((uint64_t)hi << 32 | lo);
 }
 __device__ __forceinline__ void ld_lds16(const char *p, uint32_t l) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p),
-                 "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
+    uint32_t m0;
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 : "={m0}"(m0) : "v"(p), "s"(__builtin_amdgcn_readfirstlane(l)) : "memory");
 }
 __device__ __forceinline__ void ld_lds16(const char *base, uint32_t off, uint32_t l) {
     uint64_t at;
-    asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0"
-                 : "=&s"(at) : "v"(off), "s"(uniform(base)), "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
+    uint32_t m0;
+    asm volatile("s_mov_b32 m0, %4\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0"
+                 : "=&s"(at), "={m0}"(m0)
+                 : "v"(off), "s"(uniform(base)), "s"(__builtin_amdgcn_readfirstlane(l)) : "memory");
 }
 __device__ __forceinline__ void ld_lds16(const char *base, size_t off, uint32_t l) { ld_lds16(base + off, l); }
 // 4 bytes a lane, at `l` + 4 x lane.
 __device__ __forceinline__ void ld_lds4(const char *base, uint32_t off, uint32_t l) {
     uint64_t at;
-    asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dword %1, %0"
-                 : "=&s"(at) : "v"(off), "s"(uniform(base)), "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
+    uint32_t m0;
+    asm volatile("s_mov_b32 m0, %4\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dword %2, %0"
+                 : "=&s"(at), "={m0}"(m0)
+                 : "v"(off), "s"(uniform(base)), "s"(__builtin_amdgcn_readfirstlane(l)) : "memory");
 }
 __device__ __forceinline__ void ld_lds4(const char *base, size_t off, uint32_t l) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(base + off),
-                 "s"(__builtin_amdgcn_readfirstlane(l)) : "memory", "m0");
+    uint32_t m0;
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                 : "={m0}"(m0) : "v"(base + off), "s"(__builtin_amdgcn_readfirstlane(l)) : "memory");
 }
 
 // Inclusive sums and maxima over the wave's lanes (maxima of values >= 0):

@@ -4,6 +4,7 @@ forms that the GPU tests compare with are held against one another here."""
 import itertools
 import os
 import re
+import shutil
 import subprocess
 
 import pytest
@@ -284,3 +285,54 @@ def test_loads_written_out_read_scalar_copies():
             assert base == "off" or ops[1].startswith(f"s_mov_b64 {base},"), (name, ops)
             found += 1
     assert found >= 4
+
+
+M0_KERNEL = """
+#include "ts_gmm.h"
+// the compiler's own loads into LDS, one before and one behind each written-out form
+__global__ void probe(const char *p, float *o, uint32_t n) {
+    __shared__ float s[4096];
+    typedef __attribute__((address_space(3))) void lds;
+    typedef const __attribute__((address_space(1))) void global;
+    const auto own = [&] { __builtin_amdgcn_global_load_lds((global *)(p + threadIdx.x * 16), (lds *)s, 16, 0, 0); };
+    for (uint32_t i = 0; i < n; ++i) {
+        own();
+        ts::ld_lds16(p + threadIdx.x * 16, 1024u);
+        own();
+        ts::ld_lds16(p, threadIdx.x * 16, 2048u);
+        own();
+        ts::ld_lds4(p, threadIdx.x * 4, 3072u);
+        own();
+        ts::ld_lds4(p, (size_t)threadIdx.x * 4, 4096u);
+        own();
+        __syncthreads();
+    }
+    o[threadIdx.x] = s[threadIdx.x] + s[threadIdx.x + 1024];
+}
+"""
+
+
+@pytest.mark.skipif(shutil.which("hipcc") is None, reason="needs the device compiler")
+def test_loads_written_out_declare_m0(tmp_path):
+    """A written-out load sets m0: the compiler is told (as a clobber it takes no
+    note of a reserved register, and says so), and sets its own value again
+    before its next use."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "m0.hip"
+    src.write_text(M0_KERNEL)
+    r = subprocess.run(["hipcc", "-O3", "-std=c++17", "--offload-arch=gfx950", "--offload-device-only", "-S", "-x", "hip",
+                        "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+                        "-I", os.path.join(root, "include"), "-I", os.path.join(root, "paper_2406_05955_amd", "csrc"),
+                        str(src), "-o", str(tmp_path / "m0.s")], capture_output=True, text=True, check=True, timeout=300)
+    assert "reserved register" not in r.stderr, r.stderr
+    stale, inside, own, written = True, False, 0, 0
+    for line in (tmp_path / "m0.s").read_text().splitlines():
+        inside = (inside or "#ASMSTART" in line) and "#ASMEND" not in line
+        if line.startswith(".LBB"):
+            stale = True  # (a loop's start: what its end left)
+        if "s_mov_b32 m0" in line:
+            stale = inside
+        if "global_load_lds" in line:
+            assert inside or not stale, line
+            written, own = written + inside, own + (not inside)
+    assert written == 4 and own == 5
