@@ -251,6 +251,15 @@ __device__ __forceinline__ void unroll(F f) {
 
 constexpr int kStrip = 8;
 
+// LDS of one contraction group of gmm_tiled in 16-byte chunks: the stages of
+// both operands and (fp8) of the scales.
+template <GmmKind KIND, int BP, int BQ, int WP, int WQ, int AR, int BR>
+constexpr int gmm_chunks() {
+    constexpr int THREADS = 64 * WP * WQ, R = 128 / 16;
+    constexpr int scales = KIND != kGmmFp8 ? 0 : BR == 1 ? 2 * BQ * 8 / 4 : BR * THREADS / 4;
+    return AR * BP * R + BR * BQ * R + scales;
+}
+
 // WP x WQ waves; a wave's tile is (BP / WP) x (BQ / WQ).  AR, BR: stages of the P
 // operand (weights) and of the other; AR may be one more.  BR = 1 (fp8, whose
 // operands of a step are one read): one stage, which is loaded again behind a
@@ -283,7 +292,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
     constexpr int NX = BQ < 64 ? 1 : BQ / 64, SS = FP8 ? THREADS : 0;
     static_assert(!FP8 || THREADS / 64 >= NX + 2, "two waves for weight scales");
     static_assert(BR > 1 || (FP8 && KW == 1 && !WIDE && BQ == THREADS / 2), "4 loads a wave for 8 blocks of scales");
-    constexpr int ALL = AR * TA::CHUNKS + BR * TB::CHUNKS + (AHEAD8 ? 2 * BQ * 8 / 4 : BR * SS / 4);
+    constexpr int ALL = gmm_chunks<KIND, BP, BQ, WP, WQ, AR, BR>();
     static_assert(KW == 1 || MODE != kGradW, "the weight gradient's contraction is short");
     __shared__ u32x4 s_all[KW * ALL];
     const int kg = KW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
@@ -754,9 +763,22 @@ inline long long gmm_grid(const GmmArgs &a) {
     return (npt * nqt + 7) / 8 * 8;
 }
 
+// Whether the rule's table (kTileSize) says of a forward tile what its kernel
+// is: stages, contraction groups, and no more workgroups a unit than the 160 KB
+// of LDS hold.
+template <GmmKind KIND, int BP, int BQ, int WP, int WQ, int AR, int BR, int KW>
+constexpr bool gmm_in_table() {
+    for (int t = 0; t < kTiles; ++t)
+        if (kTileSize[t].p == BP && kTileSize[t].q == BQ)
+            return kTileSize[t].stages == (BR == 1 ? 2 : BR) && kTileSize[t].kw == KW &&
+                   tiles_per_unit(KIND, t) * KW * gmm_chunks<KIND, BP, BQ, WP, WQ, AR, BR>() * 16 <= 160 * 1024;
+    return false;
+}
+
 // Launches it; a grid beyond the runtime's 2^32 threads is refused.
 template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int AR, int BR, int KW = 1, bool WIDE = false>
 ts_status run_tiled(const char *name, const GmmArgs &a, hipStream_t st) {
+    static_assert(MODE == kGradW || WIDE || gmm_in_table<KIND, BP, BQ, WP, WQ, AR, BR, KW>(), "the tile's line in kTileSize");
     const long long grid = gmm_grid<MODE, BP, BQ>(a);
     if (grid * (64 * WP * WQ * KW) >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
     launch<GmmArgs>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, AR, BR, KW, WIDE>, dim3((unsigned)grid),

@@ -77,20 +77,21 @@ GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k
         const double matrix = (double)t.p * t.q / (kind == kGmmF32 ? 2.0 : 16.0);
         const double step = std::max(matrix, (t.p + t.q) * 128 / 20.0);
         const double trip = 2000.0 / (t.stages - 1) / t.kw, start = 250.0 * (t.kw + 1);
+        const int per_unit = tiles_per_unit(kind, i);
         double cycles;
         if (kind == kGmmF32) {
             // a unit's matrix cores take its tiles one after another; a step's
             // barrier and first reads are another 100 cycles of theirs (many tiles of
             // 32 x 32, 64 x 32, 128 x 64: 986, 896, 880 us at 2048 x 4096, 6000 rows)
             const double each = tiles / 256 < 8 ? std::ceil(tiles / 256) : tiles / 256 + 0.5;
-            const double together = std::min<double>(t.per_unit, each);
+            const double together = std::min<double>(per_unit, each);
             cycles = each * (steps * std::max(step + 100, trip / together) + start / together);
         } else {
-            const double together = std::min<double>(t.per_unit, std::max(1.0, tiles / 256));
-            const double r = tiles / (256.0 * t.per_unit);
+            const double together = std::min<double>(per_unit, std::max(1.0, tiles / 256));
+            const double r = tiles / (256.0 * per_unit);
             const double rounds = r < 4 ? std::ceil(r) : r + 0.5;
             cycles = rounds * (steps * std::max(together * step, trip) + start);
-            // (with two a unit its operands, twice those of 64 x 32, are what it waits for:
+            // (from the second a unit on its operands, twice those of 64 x 32, are what it waits for:
             // bf16 688 x 5456, 300 rows of 8 groups 32 us, 64 x 32 21)
             if (i == kTile32x32 && tiles > 256) continue;
         }

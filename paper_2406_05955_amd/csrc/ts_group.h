@@ -47,6 +47,10 @@ struct GmmTileSize {
 constexpr GmmTileSize kTileSize[kTiles] = {{256, 256, 1, 2, 1}, {128, 128, 2, 2, 1}, {128, 64, 2, 3, 1},
                                            {64, 32, 2, 3, 2},   {256, 128, 1, 3, 1}, {64, 64, 1, 4, 2},
                                            {32, 32, 2, 3, 3}};
+// (fp8 32 x 32: with its scales more than half of LDS)
+constexpr int tiles_per_unit(GmmKind kind, int t) {
+    return kind == kGmmFp8 && t == kTile32x32 ? 1 : kTileSize[t].per_unit;
+}
 GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k);
 
 ts_status check_group_dims(int rows, int groups, int n, int k, int quantum);

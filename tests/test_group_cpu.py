@@ -265,6 +265,16 @@ def test_the_gpu_tests_of_many_scale_blocks_take_the_large_tile(tmp_path):
     assert set(map(int, r.stdout.split())) == {0}, r.stdout
 
 
+def test_the_tile_table_fits_lds(tmp_path):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = tmp_path / "tile_units_check"
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-I", os.path.join(root, "include"),
+                    "-I", os.path.join(root, "paper_2406_05955_amd", "csrc"),
+                    os.path.join(root, "tests", "native", "tile_units_check.cpp"), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout
+
+
 def test_loads_written_out_read_scalar_copies():
     """A vector load written in assembler is invisible to the compiler's waits:
     it may read scalar registers only that its own text wrote with a scalar
