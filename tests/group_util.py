@@ -151,3 +151,40 @@ def group(idx, E):
     pair_row = torch.full((T * K,), -1, dtype=torch.int32)
     pair_row[order[:n]] = torch.arange(n, dtype=torch.int32)
     return offsets, (order[:n] // K).to(torch.int32), pair_row.view(T, K)
+
+
+def fp8_layer(x, gate, up, down, logits, K, c):
+    """The 8-bit layer from its own codes: Combined and the output in 64 bits and
+    what bf16 results may be off by.  gate, up, down: (codes, scales) of the
+    weights, [E][n][k] each; c: the Combined that the down product was given."""
+    idx, w, off, tok, pair = route(logits, K)
+
+    def product(v, q, src=None):
+        wv = tile_values(*q)
+        y, mag = mm(v, wv, off, src)
+        # (a block's two scales are multiplied first, and the sum by them)
+        return y, sum_bound(mag, v.shape[1] + 4) + fp8_bound(v, wv, off, src)
+
+    xv = row_values(*quant_rows(x))
+    (g, eg), (u, eu) = product(xv, gate, tok), product(xv, up, tok)
+    comb = drelu(g, u)
+    comb_bound = rounded(drelu_bound(g, u, eg, eu) + 2.0 ** -23 * comb, comb, BF16)
+    y, ey = product(row_values(*quant_rows(c)), down)
+    ey = rounded(ey, y, BF16)
+    # weights: exp of a difference rounded once, K of them added, one quotient
+    ew = (12 + K + float(logits.abs().max())) * 2.0 ** -23
+    y, ey, w = y[pair.long()], ey[pair.long()], w[:, :, None]
+    out, mag = (w * y).sum(1), (w * (y.abs() + ey)).sum(1)
+    bound = (w * ey).sum(1) + ew * (y.abs() + ey).sum(1) + sum_bound(mag, K)
+    return comb, comb_bound, out, rounded(bound, out, BF16)
+
+
+# tokens, experts, top k, hidden, inter: two and four blocks of 128, one of them partial
+FP8_LAYERS = [(1, 4, 2, 144, 272), (90, 8, 2, 256, 400), (700, 4, 3, 400, 256)]
+
+
+def fp8_layer_inputs(T, E, H, I, gen):
+    """x, router, gate, up, down_t as the layer's weights are laid out."""
+    x = torch.randn(T, H, generator=gen).to(BF16)
+    return x, *((torch.randn(*s, generator=gen) * H ** -0.5).to(BF16)
+                for s in ((E, H), (E, I, H), (E, I, H), (E, I, H)))

@@ -691,6 +691,25 @@ def test_layer_fp8_forward():
     assert (out.cpu().double() - want).norm() / want.norm() <= 6 * 2.0 ** -4
 
 
+@pytest.mark.parametrize("T,E,K,H,I", ref.FP8_LAYERS)
+def test_layer_fp8_forward_from_its_codes(T, E, K, H, I):
+    """The 8-bit layer, each element against the 64-bit layer on the same codes
+    and scales: every block's scale, expert and weight in its place."""
+    x, wr, wg, wu, wd = ref.fp8_layer_inputs(T, E, H, I, gen(52, T))
+    xd, wrd, wgd, wud, wdd = dev(x, wr, wg, wu, wd)
+    logits = ts.grouped_mm(xd, torch.nn.functional.pad(wrd, (0, 0, 0, -E % 8))[None], out_dtype=F32)[:, :E].contiguous()
+    want = x.double() @ wr.double().t()
+    within(logits, want, ref.sum_bound(x.double().abs() @ wr.double().abs().t(), H))
+    qg, qu, qd = ts.fp8_quant_weights(wgd), ts.fp8_quant_weights(wud), ts.fp8_quant_weights(wdd, w_kn=True)
+    idx, w, off, tok, pair = ts.moe_route(logits, K)
+    c = ts.fp8_drelu(*ts.fp8_quant(xd), *qg, *qu, off, row_src=tok)
+    out = ts.moe_combine(ts.fp8_mm(*ts.fp8_quant(c), *qd, off), pair, w)
+    codes = [ref.quant_tiles(m) for m in (wg, wu, wd.transpose(1, 2))]
+    comb, comb_bound, want, bound = ref.fp8_layer(x, *codes, logits.cpu(), K, c.cpu())
+    within(c, comb, comb_bound)
+    within(out, want, bound)
+
+
 # --- streams, graphs, determinism ---------------------------------------------------
 
 def everything(x, wr, wg, wu, wd, K, d_out):

@@ -227,6 +227,46 @@ def test_plain_quantiser():
     assert s.tolist()[0][:2] == [1.0, 1.0]
 
 
+@pytest.mark.parametrize("T,E,K,H,I", ref.FP8_LAYERS)
+def test_plain_fp8_layer_tells_mistakes(T, E, K, H, I):
+    """The bounds of the 8-bit layer take the layer itself, with Combined, the
+    down product and the output rounded as they are passed on, and no layer
+    with a scale, an expert, a column or a weight in the wrong place."""
+    x, wr, wg, wu, wd = ref.fp8_layer_inputs(T, E, H, I, torch.Generator().manual_seed(T))
+    logits = x.float() @ wr.float().t()
+    gate, up, down = (ref.quant_tiles(m) for m in (wg, wu, wd.transpose(1, 2)))
+    idx, w, off, tok, pair = ref.route(logits, K)
+    xv = ref.row_values(*ref.quant_rows(x))
+    g, u = (ref.mm(xv, ref.tile_values(*q), off, tok)[0] for q in (gate, up))
+    c = ref.drelu(g, u).to(ref.BF16)
+    y = ref.mm(ref.row_values(*ref.quant_rows(c)), ref.tile_values(*down), off)[0].to(ref.BF16)
+    out = (w[:, :, None] * y.double()[pair.long()]).sum(1).to(ref.BF16)
+
+    def holds(gate=gate, up=up, down=down, logits=logits, c_in=c, x=x):
+        comb, comb_bound, want, bound = ref.fp8_layer(x, gate, up, down, logits, K, c_in)
+        return bool(((c.double() - comb).abs() <= comb_bound).all() and ((out.double() - want).abs() <= bound).all())
+
+    def scales(q, s):
+        return q[0], s.contiguous()
+
+    assert holds()
+    cut = c.clone()
+    cut[:, -16:] = 0
+    for name, wrong in {
+            "up: the first contraction block's scales": dict(up=scales(up, up[1][:, :, :1].expand_as(up[1]))),
+            "gate: the first column block's scales": dict(gate=scales(gate, gate[1][:, :1].expand_as(gate[1]))),
+            "down: the first column block's scales": dict(down=scales(down, down[1][:, :1].expand_as(down[1]))),
+            "down: the first contraction block's scales": dict(down=scales(down, down[1][:, :, :1].expand_as(down[1]))),
+            "up: another expert's scales": dict(up=scales(up, up[1].roll(1, 0))),
+            "down: another expert's scales": dict(down=scales(down, down[1].roll(1, 0))),
+            "the columns of Combined in another order": dict(c_in=c.flip(1)),
+            "the last 16 columns of Combined left out": dict(c_in=cut),
+            "x's neighbouring token": dict(x=x.roll(1, 0) if T > 1 else -x),
+            "weights of 1 / K": dict(logits=logits.scatter(1, idx.long(), 9.0)),
+    }.items():
+        assert not holds(**wrong), name
+
+
 # --- the host side's choices ---------------------------------------------------------
 
 def build_check(tmp_path, *flags):
