@@ -228,7 +228,8 @@ size_t ts_moe_workspace_bytes(int batch, int hidden, int inter, int n_experts, i
  * per group).  Above 64 tokens they do so, in groups of 64 with x and Combined
  * in three bf16 parts (all 24 bits), where the weight readings saved pay for
  * it and the groups fit the workspace (few tokens beside many experts do
- * not); otherwise the single-token kernel runs per routed pair.
+ * not); otherwise the single-token kernel runs per routed pair.  More than 256
+ * tokens: the layer's parts, ts_moe_route and those behind it.
  */
 ts_status ts_moe_sparse(const float *x, const void *w_router, const void *w_gate, const void *w_up,
                         const void *w_down_t, ts_dtype wdtype, int batch, int hidden, int inter,
@@ -277,12 +278,16 @@ ts_status ts_moe_dense(const float *x, const void *w_router, const void *w_gate,
  * and each has its gradients; ts_fp8_* are the products with 8-bit operands.
  * The conventions above hold, but for these:
  *   - Row types: activations are TS_BF16 or TS_F32, as stated per argument;
- *     products accumulate in fp32 and round once.
+ *     bf16 and fp32 products accumulate in fp32 and round once (the fp8
+ *     products' own sums are shorter, see there).  A product's operands are of
+ *     one type: where ts_moe_sparse keeps x and Combined in fp32 next to bf16
+ *     weights, a layer made of these calls rounds both to bf16.
  *   - Limits: tokens, rows and pairs <= 2^23, each may be 0 (nothing is
  *     enqueued and device pointers may be NULL, except that gradients of
  *     weights and offsets are written); n_experts, n_groups <= 64; n, k and
  *     hidden <= 131072, multiples of 8 (TS_BF16), 4 (TS_F32) or 16 (fp8); one
- *     group's weight matrix below 4 GB.
+ *     group's weight matrix below 4 GB.  A call that would need 2^32 threads or
+ *     more (outputs of about 2^37 elements) returns TS_ERR_UNSUPPORTED.
  *   - `offsets` is device int32 [n_groups + 1], ascending, within [0, rows];
  *     NULL with n_groups == 1: the group holds all rows.  Values out of range
  *     or order are clamped (no access leaves the arrays; which rows are
@@ -382,7 +387,13 @@ ts_status ts_fp8_quant_weights(const void *w, ts_dtype dtype, int w_kn, int n_gr
  * ([n_groups][n][k]): out[r][j] = sum over blocks b of x_scale[src(r)][b]
  * w_scale[g][j / 128][b] sum over i in b of x[src(r)][i] w[g][j][i].  The two
  * scales are multiplied first, in fp32: both are representable apart and must
- * be so together. */
+ * be so together.
+ * The sum over i is the matrix instructions': they add products in groups of 8
+ * consecutive i (the first a multiple of 8) aligned to the group's largest, and
+ * drop what lies below 2^-13 of it, from each of the others.  So a result, in
+ * fp32 too, is off by up to 7 x 2^-13 of every group's largest product (times
+ * the scales) on top of fp32 rounding: 5e-5 of the result's 2-norm with codes
+ * drawn evenly, and more of a result whose products cancel. */
 ts_status ts_fp8_mm(const void *x, const float *x_scale, const void *w, const float *w_scale, const int32_t *row_src,
                     const int32_t *offsets, int rows, int src_rows, int n_groups, int n, int k, void *out,
                     ts_dtype odtype, void *stream);

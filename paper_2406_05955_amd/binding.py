@@ -738,7 +738,9 @@ def _fp8_shapes(x, x_scale, ws):
 
 def fp8_mm(x, x_scale, w, w_scale, offsets=None, row_src=None, out=None, out_dtype=None, stream=None):
     """ts_fp8_mm on the codes and scales of fp8_quant and fp8_quant_weights.
-    Returns out [rows][n] (bf16 unless out_dtype or out says otherwise)."""
+    Returns out [rows][n] (bf16 unless out_dtype or out says otherwise).  A
+    block's sums come from the matrix instructions, which keep fewer bits than
+    fp32 (5e-5 of the result's 2-norm; more of one whose products cancel)."""
     if stream is not None:
         return _run_on(stream, fp8_mm, x, x_scale, w, w_scale, offsets, row_src, out, out_dtype)
     S, k, G, n = _fp8_shapes(x, x_scale, (("w", w, w_scale),))
@@ -755,7 +757,8 @@ def fp8_mm(x, x_scale, w, w_scale, offsets=None, row_src=None, out=None, out_dty
 
 def fp8_drelu(x, x_scale, w_gate, gate_scale, w_up, up_scale, offsets=None, row_src=None, out=None, out_dtype=None,
               stream=None):
-    """ts_fp8_drelu: grouped_drelu on quantised rows and weights."""
+    """ts_fp8_drelu: grouped_drelu on quantised rows and weights (sums as in
+    fp8_mm)."""
     if stream is not None:
         return _run_on(stream, fp8_drelu, x, x_scale, w_gate, gate_scale, w_up, up_scale, offsets, row_src, out,
                        out_dtype)

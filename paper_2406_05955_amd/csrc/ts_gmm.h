@@ -19,7 +19,8 @@
 // The fp8 matrix instructions (all forms alike) add products in groups of 8
 // consecutive indices aligned to the group's largest and cut what is below
 // 2^-13 of it: with values drawn evenly over the codes 5e-5 of the result's
-// 2-norm, far under the codes' own 2^-4; everything behind is fp32.
+// 2-norm, far under the codes' own 2^-4; everything behind is fp32.  (Codes
+// widened to bf16 would be summed in fp32, at half the matrix rate.)
 //
 // What bounds it: few rows, the weights' bytes (gate + up 4096 x 14336 bf16, 1
 // token 80 to 88 us = 5.9 to 5.3 TB/s; down, 32 tokens 156 to 170 us; fp8 gate + up, 4

@@ -401,6 +401,27 @@ def test_fp8_many_scale_blocks(k):
     within(got[mid], c[mid], bound[mid])
 
 
+def test_fp8_products_that_cancel():
+    """Large products that cancel across groups of 8, small ones beside them: the
+    error is the stated share of the groups' largest products, whatever is left
+    of the result."""
+    rows, n, k = 70, 144, 512
+    g = gen(35)
+    half = k // 2
+    x, w = randn(g, rows, half), randn(g, 1, n, half)
+    at = torch.randperm(half, generator=g) + half  # (where the products come again, with the other sign)
+    xx, ww = torch.empty(rows, k), torch.empty(1, n, k)
+    xx[:, :half], ww[:, :, :half] = x, w
+    xx[:, at], ww[:, :, at] = x, -w
+    small = torch.rand(k, generator=g) < 0.3
+    xx[:, small] *= 2.0 ** -8
+    (xq, xs), (wq, wsc) = ref.quant_rows(xx), ref.quant_tiles(ww)
+    y, bound = fp8_want(xq, xs, wq, wsc, [0, rows])
+    for odt in (F32, BF16):
+        got = ts.fp8_mm(*dev(xq, xs, wq, wsc), out_dtype=odt)
+        within(got, y, ref.rounded(bound, y, odt))
+
+
 # --- combine ---------------------------------------------------------------------
 
 @pytest.mark.parametrize("ydt,odt", [(BF16, BF16), (F32, F32), (BF16, F32), (F32, BF16)])
