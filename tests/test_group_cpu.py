@@ -351,9 +351,9 @@ __global__ void probe(const char *p, float *o, uint32_t n) {
         own();
         ts::ld_lds16(p, threadIdx.x * 16, 2048u);
         own();
-        ts::ld_lds4(p, threadIdx.x * 4, 3072u);
+        ts::ld_lds4(p, threadIdx.x * 4, 5120u);
         own();
-        ts::ld_lds4(p, (size_t)threadIdx.x * 4, 4096u);
+        ts::ld_lds4(p, (size_t)threadIdx.x * 4, 6144u);
         own();
         __syncthreads();
     }
