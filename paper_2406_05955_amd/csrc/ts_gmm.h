@@ -294,7 +294,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
     static_assert(!FP8 || THREADS / 64 >= NX + 2, "two waves for weight scales");
     static_assert(BR > 1 || (FP8 && KW == 1 && !WIDE && BQ == THREADS / 2), "4 loads a wave for 8 blocks of scales");
     constexpr int ALL = gmm_chunks<KIND, BP, BQ, WP, WQ, AR, BR>();
-    static_assert(KW == 1 || MODE != kGradW, "the weight gradient's contraction is short");
+    static_assert(KW == 1 || MODE != kGradW, "the weight gradient's rows are looked up for one contraction group");
     __shared__ u32x4 s_all[KW * ALL];
     const int kg = KW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
     u32x4 *const s_a = s_all + kg * ALL;
@@ -793,7 +793,9 @@ inline bool gmm_wide(const GmmArgs &a) {
     return (unsigned long long)a.src_rows * a.k * GmmElem<KIND>::SZ >= (1ull << 32);
 }
 
-// Forward product on the tile that suits its sizes.
+// Forward product on the tile that suits its sizes; with 64-bit row offsets there is one
+// tile (bf16 4096 x 14336, rows gathered from x of 4 GB and, for comparison, of 8 MB:
+// 1 row 62 / 26 us, 512 rows 82 / 66).
 template <GmmKind KIND, GmmMode MODE, bool ACOL>
 ts_status run_fwd(const char *name, const GmmArgs &a, hipStream_t st) {
     if (gmm_wide<KIND>(a)) return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2, 1, true>(name, a, st);

@@ -46,11 +46,8 @@ size_t route_ws_bytes(int tokens, int n_experts, int top_k) {
 // operands at 20 bytes a cycle and unit (what a unit draws with all units busy),
 // or a round trip of 2000 cycles shared by the stages ahead and the contraction
 // groups; the tiles run in rounds of 256 units.  Groups are taken as spread evenly
-// over their sizes (half a tile over).  Over 41 calls (1 to 3000 tokens, dense, 4
-// to 16 groups, 512 x 1792 to 4096 x 14336, three types) the choice costs 3.9% on
-// average against the best of eleven tiles measured one by one; over 113 smaller ones
-// against four tiles 0.4% (fp32 1.2%).  Us, 64x32 / 64x64
-// / 128x64 / 128x128 / 256x128 / 256x256: down bf16 4096 x 14336 1 token 39 / 41 /
+// over their sizes (half a tile over); a second pair's steps are not counted.
+// Us, 64x32 / 64x64 / 128x64 / 128x128 / 256x128 / 256x256: down bf16 4096 x 14336 1 token 39 / 41 /
 // 67 / 131 / 142 / 236, 32 tokens 181 / 172 / 153 / 232 / 192 / 322, 512 tokens 503
 // / 391 / 310 / 305 / 243 / 292; one fp8 layer 4096 x 4096 100 rows 9.5 / 11 / 24 /
 // 32 / 31 / 47, 2000 rows 97 / 80 / 61 / 52 / 42 / 66; 2048 x 8192 400 rows 26 / 19
