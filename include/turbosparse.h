@@ -359,6 +359,36 @@ ts_status ts_drelu_grad(const void *gate, const void *up, const void *d_c, ts_dt
                         void *d_gate, void *d_up, void *stream);
 
 /*
+ * The same layer in training with gate and up kept in 8 bits instead of 2 x 2
+ * (or 4) bytes and Combined not at all.  max(0, gate) and max(0, up) are all that
+ * the gradient needs.  Each has a code of 4 bits of exponent and 4 of mantissa, no
+ * sign, 0 for "not positive" (NaN too), so which neurons pass the gradient is
+ * exact; 16 consecutive columns of a row share a byte E0.  With t(v) = the fp32
+ * bits of v rounded to 4 bits of mantissa (to nearest even, a finite v to a finite
+ * value) >> 19: E0 = max(15, largest t >> 4), code = max(1, t - 16 E0 + 240), and a
+ * code's value has the bits (code + 16 E0 - 240) << 19: within 2^-5 of v where v is
+ * above 33/32 x 2^-15 of its block's power of two, 17/16 x 2^-15 of that below.  A block
+ * with +inf keeps the infinity, its other values come out as 2^113 or more.
+ *   codes [rows][n][2] bytes (gate's, up's; 16-byte aligned), exps [rows][ceil(n
+ *   / 16)][2] bytes (alike; 2-byte aligned).
+ * ts_grouped_drelu_pack: c as ts_grouped_drelu, and the codes.
+ * ts_grouped_drelu_grad: d_c[r] = sum_i d_y[src(r)][i] w[g][j][i] (w [n_groups][n][k]:
+ *   w_down_t), then d_gate = d_c up, d_up = d_c gate where both codes are not 0,
+ *   otherwise 0, and (unless NULL) c = gate up, all [rows][n] `odtype`, from the codes'
+ *   values and the unrounded d_c.
+ * ts_drelu_unpack: the values, bf16 [rows][n] (exact), of every row.
+ * Rows outside the groups are not written (codes neither).
+ */
+ts_status ts_grouped_drelu_pack(const void *x, const void *w_gate, const void *w_up, ts_dtype dtype,
+                                const int32_t *row_src, const int32_t *offsets, int rows, int src_rows, int n_groups,
+                                int n, int k, void *c, void *codes, void *exps, ts_dtype odtype, void *stream);
+ts_status ts_grouped_drelu_grad(const void *d_y, const void *w, ts_dtype dtype, const int32_t *row_src,
+                                const int32_t *offsets, int rows, int src_rows, int n_groups, int n, int k,
+                                const void *codes, const void *exps, void *d_gate, void *d_up, void *c,
+                                ts_dtype odtype, void *stream);
+ts_status ts_drelu_unpack(const void *codes, const void *exps, int rows, int n, void *gate, void *up, void *stream);
+
+/*
  * Gradient of a grouped product's weights: d_w[g][j][i] = sum over the rows r
  * of group g of d_y[r][j] x[src(r)][i], zeros for a group without rows.
  *   d_y [rows][n], x [src_rows][k] `dtype`; d_w [n_groups][n][k] `odtype`.
@@ -436,7 +466,8 @@ const char *ts_version(void);
  * `kernel` ("ffn_main", "ffn_reduce", "ffn_gate_up", "ffn_down",
  * "ffn_topk_select", "ffn_topk_down", "ffn_given", "given_counts", "ffn_stats", "ffn_union",
  * "moe_router", "moe_route", "moe_place", "moe_route_grad", "grouped_mm",
- * "grouped_drelu", "drelu_grad", "grouped_mm_dw", "fp8_quant",
+ * "grouped_drelu", "drelu_grad", "grouped_drelu_pack", "grouped_drelu_grad",
+ * "drelu_unpack", "grouped_mm_dw", "fp8_quant",
  * "fp8_quant_weights", "fp8_mm", "fp8_drelu", "moe_combine",
  * "moe_combine_grad", "batch_prep", "batch_gate_up", "batch_down",
  * "batch_reduce", "batch_stats", "batch_union", "probe_read",

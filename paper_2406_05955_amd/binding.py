@@ -26,7 +26,8 @@ EXPORTED = ["ts_ffn_workspace_bytes", "ts_ffn_sparse", "ts_ffn_sparse_act", "ts_
             "ts_moe_dense", "ts_status_str", "ts_last_error", "ts_version", "ts_prof_enable", "ts_prof_reset",
             "ts_prof_read", "ts_probe_read", "ts_probe_copy", "ts_tune_set",
             "ts_moe_route_workspace_bytes", "ts_moe_route", "ts_moe_group", "ts_moe_route_grad", "ts_grouped_mm",
-            "ts_grouped_drelu", "ts_drelu_grad", "ts_grouped_mm_dw", "ts_fp8_quant", "ts_fp8_quant_weights",
+            "ts_grouped_drelu", "ts_drelu_grad",
+            "ts_grouped_drelu_pack", "ts_grouped_drelu_grad", "ts_drelu_unpack", "ts_grouped_mm_dw", "ts_fp8_quant", "ts_fp8_quant_weights",
             "ts_fp8_mm", "ts_fp8_drelu", "ts_moe_combine", "ts_moe_combine_grad"]
 
 
@@ -79,6 +80,9 @@ def _load() -> ctypes.CDLL:
             ("ts_grouped_mm", [vp, vp, vp, vp, i, i, vp, vp, i, i, i, i, i, vp, i, vp]),
             ("ts_grouped_drelu", [vp, vp, vp, i, vp, vp, i, i, i, i, i, vp, vp, vp, i, vp]),
             ("ts_drelu_grad", [vp, vp, vp, i, i, i, vp, vp, vp]),
+            ("ts_grouped_drelu_pack", [vp, vp, vp, i, vp, vp, i, i, i, i, i, vp, vp, vp, i, vp]),
+            ("ts_grouped_drelu_grad", [vp, vp, i, vp, vp, i, i, i, i, i, vp, vp, vp, vp, vp, i, vp]),
+            ("ts_drelu_unpack", [vp, vp, i, i, vp, vp, vp]),
             ("ts_grouped_mm_dw", [vp, vp, i, vp, vp, i, i, i, i, i, vp, i, vp]),
             ("ts_fp8_quant", [vp, i, i, i, vp, vp, vp]),
             ("ts_fp8_quant_weights", [vp, i, i, i, i, i, vp, vp, vp]),
@@ -428,7 +432,7 @@ def moe_dense(x, w_router, w_gate, w_up, w_down_t, top_k: int, out=None, ws=None
 # under torch.cuda.stream(stream): memory that other streams freed may still be
 # in use there, and a workspace is freed as the call returns.
 
-_i32, _e4m3 = torch.int32, torch.float8_e4m3fn
+_i32, _u8, _e4m3 = torch.int32, torch.uint8, torch.float8_e4m3fn
 _int_max = 0x7fffffff
 
 
@@ -660,6 +664,75 @@ def drelu_grad(gate, up, d_c, stream=None):
     if code:
         _check(code, "ts_drelu_grad")
     return dg, du
+
+
+def _need_kept(codes, exps, rows, n):
+    _need(codes, "codes", _u8, (rows, n, 2))
+    _need(exps, "exps", _u8, (rows, (n + 15) // 16, 2))
+
+
+def grouped_drelu_pack(x, w_gate, w_up, offsets=None, row_src=None, out=None, out_dtype=None, codes=None, exps=None,
+                       stream=None):
+    """ts_grouped_drelu_pack: grouped_drelu that keeps max(0, gate) and
+    max(0, up) in 8 bits.  Returns c [rows][n], codes uint8 [rows][n][2], exps
+    uint8 [rows][ceil(n / 16)][2]."""
+    if stream is not None:
+        return _run_on(stream, grouped_drelu_pack, x, w_gate, w_up, offsets, row_src, out, out_dtype, codes, exps)
+    _need(x, "x", (_f32, _bf16), 2)
+    S, k = x.shape
+    _need(w_gate, "w_gate", x.dtype, (None, None, k))
+    _need(w_up, "w_up", x.dtype, tuple(w_gate.shape))
+    G, n = w_gate.shape[:2]
+    R = _rows_of(x, offsets, row_src, G)
+    odt, od = _odtype(out, out_dtype, x.dtype)
+    st = _here(x, w_gate, w_up, offsets, row_src, out, codes, exps)
+    out = _new(out, "out", (R, n), odt, x.device)
+    codes = _new(codes, "codes", (R, n, 2), _u8, x.device)
+    exps = _new(exps, "exps", (R, (n + 15) // 16, 2), _u8, x.device)
+    code = lib.ts_grouped_drelu_pack(_ptr(x), _ptr(w_gate), _ptr(w_up), wdtype_of_rows(x.dtype), _ptr(row_src),
+                                     _ptr(offsets), R, S, G, n, k, _ptr(out), _ptr(codes), _ptr(exps), od, st)
+    if code:
+        _check(code, "ts_grouped_drelu_pack")
+    return out, codes, exps
+
+
+def grouped_drelu_grad(d_y, w, codes, exps, offsets=None, row_src=None, want_c: bool = True, out_dtype=None,
+                       stream=None):
+    """ts_grouped_drelu_grad.  d_y [S][k], w [G][n][k] (w_down_t), codes and
+    exps of grouped_drelu_pack.  Returns d_gate, d_up [rows][n] and, with want_c,
+    c (d_y's dtype unless given)."""
+    if stream is not None:
+        return _run_on(stream, grouped_drelu_grad, d_y, w, codes, exps, offsets, row_src, want_c, out_dtype)
+    _need(d_y, "d_y", (_f32, _bf16), 2)
+    S, k = d_y.shape
+    _need(w, "w", d_y.dtype, (None, None, k))
+    G, n = w.shape[:2]
+    R = _rows_of(d_y, offsets, row_src, G)
+    _need_kept(codes, exps, R, n)
+    odt, od = _odtype(None, out_dtype, d_y.dtype)
+    st = _here(d_y, w, codes, exps, offsets, row_src)
+    dg, du = (torch.empty(R, n, dtype=odt, device=d_y.device) for _ in range(2))
+    c = torch.empty(R, n, dtype=odt, device=d_y.device) if want_c else None
+    code = lib.ts_grouped_drelu_grad(_ptr(d_y), _ptr(w), wdtype_of_rows(d_y.dtype), _ptr(row_src), _ptr(offsets), R, S,
+                                     G, n, k, _ptr(codes), _ptr(exps), _ptr(dg), _ptr(du), _ptr(c), od, st)
+    if code:
+        _check(code, "ts_grouped_drelu_grad")
+    return (dg, du, c) if want_c else (dg, du)
+
+
+def drelu_unpack(codes, exps, stream=None):
+    """ts_drelu_unpack: max(0, gate) and max(0, up) as kept, bf16 [rows][n]."""
+    if stream is not None:
+        return _run_on(stream, drelu_unpack, codes, exps)
+    _need(codes, "codes", _u8, (None, None, 2))
+    R, n = codes.shape[:2]
+    _need_kept(codes, exps, R, n)
+    st = _here(codes, exps)
+    g, u = (torch.empty(R, n, dtype=_bf16, device=codes.device) for _ in range(2))
+    code = lib.ts_drelu_unpack(_ptr(codes), _ptr(exps), R, n, _ptr(g), _ptr(u), st)
+    if code:
+        _check(code, "ts_drelu_unpack")
+    return g, u
 
 
 def grouped_mm_dw(d_y, x, offsets=None, row_src=None, out=None, out_dtype=None, stream=None):

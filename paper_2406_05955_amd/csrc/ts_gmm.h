@@ -47,6 +47,7 @@
 
 #include "ts_device.h"
 #include "ts_group.h"
+#include "ts_keep.h"
 #include "ts_runtime.h"
 
 namespace ts {
@@ -57,7 +58,24 @@ typedef short s16x4g __attribute__((ext_vector_type(4)));
 
 static __device__ const u32x4 g_zero_chunk[8] = {};  // (a step's 128 bytes of a row)
 
-enum GmmMode { kFwd = 0, kDrelu = 1, kGradW = 2 };
+// kDreluPack: dReLU whose activations are also kept in 8 bits; kDreluGrad: a
+// forward product (the gradient of Combined) with dReLU's gradient behind it.
+enum GmmMode { kFwd = 0, kDrelu = 1, kGradW = 2, kDreluPack = 3, kDreluGrad = 4 };
+// Gate and up interleaved in the P operand.
+constexpr bool is_drelu(GmmMode m) { return m == kDrelu || m == kDreluPack; }
+
+template <GmmMode MODE>
+struct GmmArgsOf {
+    using type = GmmArgs;
+};
+template <>
+struct GmmArgsOf<kDreluPack> {
+    using type = GmmKeepArgs;
+};
+template <>
+struct GmmArgsOf<kDreluGrad> {
+    using type = GmmKeepArgs;
+};
 
 // 16 bytes a lane from global memory into LDS at byte `l` + 16 x lane (all
 // lanes active).  Written out, with no register to return to: the compiler
@@ -271,16 +289,17 @@ constexpr int gmm_chunks() {
 // KW of them run side by side).  WIDE: x is 4 GB or
 // more, its rows' offsets take 64 bits.
 template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int AR, int BR, int KW, bool WIDE>
-__global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
+__global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsOf<MODE>::type a) {
     constexpr int THREADS = 64 * WP * WQ;  // of one contraction group
     constexpr bool BCOL = MODE == kGradW;
     using TA = GmmTile<KIND, ACOL, BP, THREADS>;
     using TB = GmmTile<KIND, BCOL, BQ, THREADS>;
     constexpr int SZ = TA::SZ, KS = TA::KS, RB = TA::RB;
     constexpr int MI = BP / WP / 16, MJ = BQ / WQ / 16;
-    constexpr int PT = MODE == kDrelu ? BP / 2 : BP;  // output columns per tile
+    constexpr bool DRELU = is_drelu(MODE);
+    constexpr int PT = DRELU ? BP / 2 : BP;  // output columns per tile
     static_assert(MODE != kGradW || ACOL, "the weight gradient contracts over rows");
-    static_assert(MODE != kDrelu || (!ACOL && MI % 2 == 0), "gate and up in pairs of 16 rows");
+    static_assert(!DRELU || (!ACOL && MI % 2 == 0), "gate and up in pairs of 16 rows");
 
     constexpr int LB = BR == 1 ? 2 : BR;  // steps that the other operand is loaded ahead, and one
     static_assert(AR == LB || AR == LB + 1, "P stages");
@@ -373,7 +392,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
     constexpr int NS = KIND == kGmmFp8 ? 1 : RB / 64, NG = NS * MI;
     // (fp8 dReLU: the gate's blocks, then the up projection's: one set of factors)
     constexpr auto order = [](int G) constexpr {
-        return FP8 && MODE == kDrelu ? G % (MI / 2) * 2 + G / (MI / 2) : G % MI;
+        return FP8 && DRELU ? G % (MI / 2) * 2 + G / (MI / 2) : G % MI;
     };
     [[maybe_unused]] int slot8 = 0;  // the step's among 8 scales
     auto contract = [&](const u32x4 *A, const u32x4 *B, [[maybe_unused]] const float *scale,
@@ -399,7 +418,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
         [[maybe_unused]] float f[MJ];
         [[maybe_unused]] f32x4 d[2][MJ];
         [[maybe_unused]] auto factors = [&](auto up) {
-            const int sel = MODE == kDrelu ? (int)up : wp * (BP / WP) / kScaleBlock;
+            const int sel = DRELU ? (int)up : wp * (BP / WP) / kScaleBlock;
             const float w = AHEAD8 ? wscale[up] : scale[(NX + sel) * 64 + lane];
             constexpr int ROW = AHEAD8 ? 8 : 1;
             const float *x = scale + (wq * MJ * 16 + lm) * ROW + (AHEAD8 ? slot8 ^ lm >> 2 : 0);
@@ -428,7 +447,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
                         a_, bf[0][j], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
                     if constexpr (G > 0) acc[order(G - 1)][j] += d[(G - 1) & 1][j] * f[j];
                 }
-                if constexpr (MODE == kDrelu && G == MI / 2) factors(std::integral_constant<int, 1>{});
+                if constexpr (DRELU && G == MI / 2) factors(std::integral_constant<int, 1>{});
                 // (in this order: the scheduler puts the sums first, which wait)
                 if constexpr (G > 0) unroll<MJ>([&](auto) {
                     __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
@@ -461,7 +480,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
     for (int pair = 0; blocks > 0 && pair < pairs; ++pair) {
         // dReLU: a wave's chunks are of 64 / CR consecutive rows (and of those
         // 32 or more further on), so all of w_gate or all of w_up
-        const bool second = MODE == kDrelu ? ((wave * (64 / TA::CR)) >> 4) & 1 : pair == 1;
+        const bool second = DRELU ? ((wave * (64 / TA::CR)) >> 4) & 1 : pair == 1;
         const char *abase = (second ? a.w[1] : a.w[0]) + (MODE == kGradW ? 0 : g * wbytes);
         const char *bbase = (pair == 1 ? a.x[1] : a.x[0]) + (MODE == kGradW ? (size_t)b * a.n * SZ : 0);
         // bytes from one block to the next
@@ -487,7 +506,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
             } else if constexpr (ACOL) {
                 aoff[j] = (uint32_t)row * (uint32_t)(a.n * SZ) + (uint32_t)min(p0 * SZ + ch * 16, a.n * SZ - 16);
             } else {
-                const int n = MODE == kDrelu ? p0 + (row >> 5) * 16 + (row & 15) : p0 + row;
+                const int n = DRELU ? p0 + (row >> 5) * 16 + (row & 15) : p0 + row;
                 aoff[j] = AHEAD8 ? n : (uint32_t)min(n, a.n - 1) * (uint32_t)(a.k * SZ) + ch * 16;
             }
         }
@@ -541,7 +560,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
         auto a_off = [&](auto j) {
             if constexpr (MODE == kGradW) return (Off)(rowoff[j] + aoff[j]);
             else if constexpr (AHEAD8)
-                return (uint32_t)min((int)aoff[0] + j * (MODE == kDrelu ? 32 : 64), a.n - 1) * krow + ka;
+                return (uint32_t)min((int)aoff[0] + j * (DRELU ? 32 : 64), a.n - 1) * krow + ka;
             else return aoff[j];
         };
         auto b_off = [&](auto j) {
@@ -559,16 +578,16 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
         if constexpr (FP8) {
             const int kbn = (a.k + kScaleBlock - 1) / kScaleBlock, nbn = (a.n + kScaleBlock - 1) / kScaleBlock;
             if constexpr (AHEAD8) {
-                const int nb = min(p0 / kScaleBlock + (MODE == kDrelu ? 0 : wp * (BP / WP) / kScaleBlock), nbn - 1);
+                const int nb = min(p0 / kScaleBlock + (DRELU ? 0 : wp * (BP / WP) / kScaleBlock), nbn - 1);
                 const size_t at = ((size_t)g * nbn + nb) * kbn;
                 wsbase[0] = (cfloat *)reinterpret_cast<uintptr_t>(a.ws[0] + at);
-                wsbase[1] = MODE == kDrelu ? (cfloat *)reinterpret_cast<uintptr_t>(a.ws[1] + at) : wsbase[0];
+                wsbase[1] = DRELU ? (cfloat *)reinterpret_cast<uintptr_t>(a.ws[1] + at) : wsbase[0];
             } else if (wave < NX) {
                 soff = (Off)source(min(q0 + wave * 64 + lane, e - 1)) * (Off)(4 * kbn);
             } else {
                 const int sel = (wave - NX) & 1;
-                const int nb = min(p0 / kScaleBlock + (MODE == kDrelu ? 0 : sel), nbn - 1);
-                sbase = (MODE == kDrelu && sel ? a.ws[1] : a.ws[0]) + ((size_t)g * nbn + nb) * kbn;
+                const int nb = min(p0 / kScaleBlock + (DRELU ? 0 : sel), nbn - 1);
+                sbase = (DRELU && sel ? a.ws[1] : a.ws[0]) + ((size_t)g * nbn + nb) * kbn;
             }
         }
         constexpr int LOADS_A = TA::NJ, LOADS_B = TB::NJ + FP8, LOADS = LOADS_A + LOADS_B;  // of a stage, per wave
@@ -726,21 +745,60 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
     for (int j = 0; j < MJ; ++j) {
         const int q = q0 + (wq * MJ + j) * 16 + lm;
         if (q >= q_end) continue;
-        if constexpr (MODE == kDrelu) {
+        if constexpr (DRELU) {
 #pragma unroll
             for (int i = 0; i < MI; i += 2) {
                 const int p = p0 + (wp * MI + i) / 2 * 16 + 4 * lq;
+                const f32x4 gt = acc[i][j], u = acc[i + 1][j];
+                [[maybe_unused]] uint2 codes;
+                [[maybe_unused]] uint32_t exps;
+                // (all four lanes of a block take part)
+                if constexpr (MODE == kDreluPack) codes = keep_four(gt, u, p < a.n, &exps);
                 if (p >= a.n) continue;
                 const size_t at = (size_t)q * a.n + p;
-                const f32x4 gt = acc[i][j], u = acc[i + 1][j];
                 f32x4 c;
 #pragma unroll
                 for (int v = 0; v < 4; ++v) c[v] = drelu1(gt[v], u[v]);
                 store4(a.out, a.out_f32, at, c);
-                if (a.gate) {
-                    store4(a.gate, a.out_f32, at, gt);
-                    store4(a.up, a.out_f32, at, u);
+                if constexpr (MODE == kDreluPack) {
+                    *reinterpret_cast<uint2 *>(a.codes + 2 * at) = codes;
+                    if (lq == 0)
+                        reinterpret_cast<uint16_t *>(a.exps)[(size_t)q * ceil_div(a.n, kKeepBlock) + p / kKeepBlock] =
+                            (uint16_t)exps;
+                } else {
+                    if (a.gate) {
+                        store4(a.gate, a.out_f32, at, gt);
+                        store4(a.up, a.out_f32, at, u);
+                    }
                 }
+            }
+        } else if constexpr (MODE == kDreluGrad) {
+            // the codes of all blocks, then block by block
+            const size_t base = (size_t)q * a.n, ebase = (size_t)q * ceil_div(a.n, kKeepBlock);
+            uint2 codes[MI];
+            uint32_t exps[MI];
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const int p = min(p0 + (wp * MI + i) * 16 + 4 * lq, a.n - 4);
+                codes[i] = *reinterpret_cast<const uint2 *>(a.codes + 2 * (base + p));
+                exps[i] = reinterpret_cast<const uint16_t *>(a.exps)[ebase + p / kKeepBlock];
+            }
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const int p = p0 + (wp * MI + i) * 16 + 4 * lq;
+                if (p >= a.n) continue;
+                f32x4 g, u, dg, du, c;
+                keep_values4(codes[i], exps[i], g, u);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const bool on = g[v] > 0.f && u[v] > 0.f;
+                    dg[v] = on ? acc[i][j][v] * u[v] : 0.f;
+                    du[v] = on ? acc[i][j][v] * g[v] : 0.f;
+                    c[v] = on ? g[v] * u[v] : 0.f;
+                }
+                store4(a.gate, a.out_f32, base + p, dg);
+                store4(a.up, a.out_f32, base + p, du);
+                if (a.out) store4(a.out, a.out_f32, base + p, c);
             }
         } else {
             const size_t base = MODE == kGradW ? ((size_t)g * a.n + q) * a.k : (size_t)q * a.n;
@@ -757,7 +815,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(GmmArgs a) {
 // groups have is known on the device only), a multiple of the 8 XCDs.
 template <GmmMode MODE, int BP, int BQ>
 inline long long gmm_grid(const GmmArgs &a) {
-    const int PT = MODE == kDrelu ? BP / 2 : BP;
+    const int PT = is_drelu(MODE) ? BP / 2 : BP;
     const long long npt = ceil_div(MODE == kGradW ? a.k : a.n, PT);
     if (MODE == kGradW) return (npt * ceil_div(a.n, BQ) + 7) / 8 * 8 * a.groups;
     const long long nqt = a.offsets ? (long long)a.rows / BQ + a.groups : ceil_div(a.rows, BQ);
@@ -778,11 +836,11 @@ constexpr bool gmm_in_table() {
 
 // Launches it; a grid beyond the runtime's 2^32 threads is refused.
 template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int AR, int BR, int KW = 1, bool WIDE = false>
-ts_status run_tiled(const char *name, const GmmArgs &a, hipStream_t st) {
+ts_status run_tiled(const char *name, const typename GmmArgsOf<MODE>::type &a, hipStream_t st) {
     static_assert(MODE == kGradW || WIDE || gmm_in_table<KIND, BP, BQ, WP, WQ, AR, BR, KW>(), "the tile's line in kTileSize");
     const long long grid = gmm_grid<MODE, BP, BQ>(a);
     if (grid * (64 * WP * WQ * KW) >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
-    launch<GmmArgs>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, AR, BR, KW, WIDE>, dim3((unsigned)grid),
+    launch<typename GmmArgsOf<MODE>::type>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, AR, BR, KW, WIDE>, dim3((unsigned)grid),
                     dim3(64 * WP * WQ * KW), st, a);
     return check_launch(name);
 }
@@ -797,15 +855,15 @@ inline bool gmm_wide(const GmmArgs &a) {
 // tile (bf16 4096 x 14336, rows gathered from x of 4 GB and, for comparison, of 8 MB:
 // 1 row 62 / 26 us, 512 rows 82 / 66).
 template <GmmKind KIND, GmmMode MODE, bool ACOL>
-ts_status run_fwd(const char *name, const GmmArgs &a, hipStream_t st) {
+ts_status run_fwd(const char *name, const typename GmmArgsOf<MODE>::type &a, hipStream_t st) {
     if (gmm_wide<KIND>(a)) return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2, 1, true>(name, a, st);
-    switch (pick_tile(KIND, MODE == kDrelu, a.groups, a.rows, a.n, a.k)) {
+    switch (pick_tile(KIND, is_drelu(MODE), a.groups, a.rows, a.n, a.k)) {
         case kTile64x32: return run_tiled<KIND, MODE, ACOL, 64, 32, 2, 2, 3, 3, 2>(name, a, st);
         case kTile64x64:
             if constexpr (KIND != kGmmF32) return run_tiled<KIND, MODE, ACOL, 64, 64, 2, 2, 4, 4, 2>(name, a, st);
             break;
         case kTile32x32:
-            if constexpr (MODE != kDrelu) return run_tiled<KIND, MODE, ACOL, 32, 32, 2, 2, 3, 3, 3>(name, a, st);
+            if constexpr (!is_drelu(MODE)) return run_tiled<KIND, MODE, ACOL, 32, 32, 2, 2, 3, 3, 3>(name, a, st);
             break;
         case kTile128x64: return run_tiled<KIND, MODE, ACOL, 128, 64, 4, 1, 3, 3>(name, a, st);
         case kTile128x128: return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2>(name, a, st);

@@ -61,41 +61,13 @@ __global__ __launch_bounds__(256) void drelu_grad_kernel(const u32x4 *gate, cons
 
 }  // namespace ts
 
-namespace {
-
-int quantum(ts_dtype d) { return d == TS_F32 ? 4 : 8; }
-
-// Checks that the forward products share; TS_OK with *empty set: nothing to do.
-ts_status check_fwd(const void *x, const void *w, ts_dtype dtype, ts_dtype odtype, const int32_t *row_src,
-                    const int32_t *offsets, int rows, int src_rows, int groups, int n, int k, const void *out,
-                    bool *empty) {
-    *empty = false;
-    if (!ts::type_ok(dtype) || !ts::type_ok(odtype)) return TS_ERR_DTYPE;
-    ts_status s = ts::check_group_dims(rows, groups, n, k, quantum(dtype));
-    if (s != TS_OK) return s;
-    if (!offsets && groups != 1) return TS_ERR_NULL;
-    if (src_rows < 0 || src_rows > ts::kMaxRows || (rows > 0 && src_rows < 1) || (!row_src && src_rows < rows))
-        return TS_ERR_SHAPE;
-    if (rows == 0) {
-        *empty = true;
-        return TS_OK;
-    }
-    if (!x || !w || !out) return TS_ERR_NULL;
-    if (!ts::aligned16(x) || !ts::aligned16(w) || !ts::aligned16(out) || !ts::aligned4(row_src) ||
-        !ts::aligned4(offsets))
-        return TS_ERR_ALIGN;
-    return TS_OK;
-}
-
-}  // namespace
-
 extern "C" {
 
 ts_status ts_grouped_mm(const void *x, const void *w, const void *x2, const void *w2, ts_dtype dtype, int w_kn,
                         const int32_t *row_src, const int32_t *offsets, int rows, int src_rows, int n_groups, int n,
                         int k, void *out, ts_dtype odtype, void *stream) {
     bool empty;
-    ts_status s = check_fwd(x, w, dtype, odtype, row_src, offsets, rows, src_rows, n_groups, n, k, out, &empty);
+    ts_status s = ts::check_fwd(x, w, dtype, odtype, row_src, offsets, rows, src_rows, n_groups, n, k, out, &empty);
     if (s != TS_OK) return s;
     if ((x2 == nullptr) != (w2 == nullptr)) return TS_ERR_NULL;
     if (!ts::aligned16(x2) || !ts::aligned16(w2)) return TS_ERR_ALIGN;
@@ -127,7 +99,7 @@ ts_status ts_grouped_drelu(const void *x, const void *w_gate, const void *w_up, 
                            const int32_t *row_src, const int32_t *offsets, int rows, int src_rows, int n_groups,
                            int n, int k, void *c, void *gate, void *up, ts_dtype odtype, void *stream) {
     bool empty;
-    ts_status s = check_fwd(x, w_gate, dtype, odtype, row_src, offsets, rows, src_rows, n_groups, n, k, c, &empty);
+    ts_status s = ts::check_fwd(x, w_gate, dtype, odtype, row_src, offsets, rows, src_rows, n_groups, n, k, c, &empty);
     if (s != TS_OK) return s;
     if ((gate == nullptr) != (up == nullptr)) return TS_ERR_NULL;
     if (!ts::aligned16(w_up) || !ts::aligned16(gate) || !ts::aligned16(up)) return TS_ERR_ALIGN;
@@ -157,7 +129,7 @@ ts_status ts_grouped_mm_dw(const void *d_y, const void *x, ts_dtype dtype, const
                            const int32_t *offsets, int rows, int src_rows, int n_groups, int n, int k, void *d_w,
                            ts_dtype odtype, void *stream) {
     bool empty;
-    ts_status s = check_fwd(x, d_y, dtype, odtype, row_src, offsets, rows, src_rows, n_groups, n, k, d_w, &empty);
+    ts_status s = ts::check_fwd(x, d_y, dtype, odtype, row_src, offsets, rows, src_rows, n_groups, n, k, d_w, &empty);
     if (s != TS_OK) return s;
     if (!d_w) return TS_ERR_NULL;
     if (!ts::aligned16(d_w) || !ts::aligned4(offsets)) return TS_ERR_ALIGN;  // (read without rows, too)
@@ -180,13 +152,13 @@ ts_status ts_grouped_mm_dw(const void *d_y, const void *x, ts_dtype dtype, const
 ts_status ts_drelu_grad(const void *gate, const void *up, const void *d_c, ts_dtype dtype, int rows, int n,
                         void *d_gate, void *d_up, void *stream) {
     if (!ts::type_ok(dtype)) return TS_ERR_DTYPE;
-    if (rows < 0 || rows > ts::kMaxRows || n < quantum(dtype) || n > ts::kMaxDim || n % quantum(dtype) != 0)
+    if (rows < 0 || rows > ts::kMaxRows || n < ts::quantum(dtype) || n > ts::kMaxDim || n % ts::quantum(dtype) != 0)
         return TS_ERR_SHAPE;
     if (rows == 0) return TS_OK;
     if (!gate || !up || !d_c || !d_gate || !d_up) return TS_ERR_NULL;
     for (const void *p : {gate, up, d_c, (const void *)d_gate, (const void *)d_up})
         if (!ts::aligned16(p)) return TS_ERR_ALIGN;
-    const long long chunks = (long long)rows * (n / quantum(dtype));
+    const long long chunks = (long long)rows * (n / ts::quantum(dtype));
     const unsigned grid = (unsigned)std::min<long long>((chunks + 255) / 256, 256 * 64);
     using ts::u32x4;
     auto go = [&](auto kernel) {

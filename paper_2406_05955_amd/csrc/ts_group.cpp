@@ -20,6 +20,26 @@ ts_status check_group_dims(int rows, int groups, int n, int k, int quantum) {
     return TS_OK;
 }
 
+ts_status check_fwd(const void *x, const void *w, ts_dtype dtype, ts_dtype odtype, const int32_t *row_src,
+                    const int32_t *offsets, int rows, int src_rows, int groups, int n, int k, const void *out,
+                    bool *empty) {
+    *empty = false;
+    if (!type_ok(dtype) || !type_ok(odtype)) return TS_ERR_DTYPE;
+    ts_status s = check_group_dims(rows, groups, n, k, quantum(dtype));
+    if (s != TS_OK) return s;
+    if (!offsets && groups != 1) return TS_ERR_NULL;
+    if (src_rows < 0 || src_rows > kMaxRows || (rows > 0 && src_rows < 1) || (!row_src && src_rows < rows))
+        return TS_ERR_SHAPE;
+    if (rows == 0) {
+        *empty = true;
+        return TS_OK;
+    }
+    if (!x || !w || !out) return TS_ERR_NULL;
+    if (!aligned16(x) || !aligned16(w) || !aligned16(out) || !aligned4(row_src) || !aligned4(offsets))
+        return TS_ERR_ALIGN;
+    return TS_OK;
+}
+
 ts_status check_route_dims(int tokens, int n_experts, int top_k) {
     if (n_experts < 1 || n_experts > kMaxExperts || top_k < 1 || top_k > kMaxTopK || top_k > n_experts)
         return TS_ERR_SHAPE;

@@ -37,6 +37,14 @@ struct GmmArgs {
     int out_f32 = 0;
 };
 
+// With dReLU's activations in 8 bits (ts_keep.h): written behind gate and up
+// (out: Combined), or read behind the gradient of Combined (gate, up: their
+// gradients; out: Combined or null).
+struct GmmKeepArgs : GmmArgs {
+    uint8_t *codes = nullptr;  // [rows][n][2]
+    uint8_t *exps = nullptr;   // [rows][ceil(n / 16)][2]
+};
+
 // Tiles of the forward products: columns (dReLU: of gate and up together) x
 // rows, workgroups of it that a compute unit holds, stages, contraction groups.
 // (equal costs: the first)
@@ -55,6 +63,11 @@ GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k
 
 ts_status check_group_dims(int rows, int groups, int n, int k, int quantum);
 bool type_ok(ts_dtype d);
+constexpr int quantum(ts_dtype d) { return d == TS_F32 ? 4 : 8; }  // elements in 16 bytes
+// Checks that the forward products share; TS_OK with *empty set: nothing to do.
+ts_status check_fwd(const void *x, const void *w, ts_dtype dtype, ts_dtype odtype, const int32_t *row_src,
+                    const int32_t *offsets, int rows, int src_rows, int groups, int n, int k, const void *out,
+                    bool *empty);
 ts_status check_route_dims(int tokens, int n_experts, int top_k);
 
 // Row maps: tokens per workgroup of the two-launch form (0: one workgroup
