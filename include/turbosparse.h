@@ -331,6 +331,32 @@ ts_status ts_moe_group(const int32_t *topk_idx, int tokens, int n_experts, int t
 ts_status ts_moe_route_grad(const int32_t *topk_idx, const float *topk_w, const float *d_w, int tokens, int n_experts,
                             int top_k, float *d_logits, void *stream);
 
+/* Workspace bytes of ts_moe_balance (0: none is needed, or out of range). */
+size_t ts_moe_balance_workspace_bytes(int tokens, int n_experts, int top_k);
+
+/*
+ * Load of the experts and the losses that balance it.  A token counts if its mask
+ * is not 0 and it has a logit above -FLT_MAX (NaN counts as -inf).  Over the n tokens
+ * that count, with p the softmax of a token's n_experts logits:
+ *   counts[e] = pairs (token, slot) whose topk_idx is e; counts[n_experts] = n
+ *   loss[0] = n_experts sum_e counts[e] / (top_k n) * (sum_t p[t][e]) / n
+ *   loss[1] = sum_t (log sum_e exp logits[t][e])^2 / n
+ * and both losses are 0 for n = 0.  A logit of +inf takes the whole of p (several share
+ * it) and makes loss[1] infinite.  Indices out of range are not counted.
+ *   logits [tokens][n_experts] fp32, topk_idx [tokens][top_k]; mask [tokens] bytes
+ *   or NULL; loss [2] fp32, counts [n_experts + 1] (both also written without tokens).
+ */
+ts_status ts_moe_balance(const float *logits, const int32_t *topk_idx, const uint8_t *mask, int tokens, int n_experts,
+                         int top_k, float *loss, int32_t *counts, void *ws, size_t ws_bytes, void *stream);
+
+/* Its gradient, with the counts as constants: d_logits[t][e] = p (d_loss[0] n_experts
+ * / n (f_e - sum_j f_j p_j) + d_loss[1] 2 / n lse), f_e = counts[e] / (top_k n); 0
+ * for tokens that do not count; plus add[t][e] unless add is NULL (d_logits may be
+ * add itself).  d_loss is device fp32 [2], counts ts_moe_balance's.  Where d_loss[1] is
+ * 0 an infinite log-sum leaves no trace. */
+ts_status ts_moe_balance_grad(const float *logits, const int32_t *counts, const float *d_loss, const uint8_t *mask,
+                              const float *add, int tokens, int n_experts, int top_k, float *d_logits, void *stream);
+
 /*
  * Product grouped by expert: out[r][j] = sum_i x[src(r)][i] w[g][j][i] for
  * the rows r of group g.
@@ -465,7 +491,8 @@ const char *ts_version(void);
  * synchronises on the recorded events and returns, for the kernel named
  * `kernel` ("ffn_main", "ffn_reduce", "ffn_gate_up", "ffn_down",
  * "ffn_topk_select", "ffn_topk_down", "ffn_given", "given_counts", "ffn_stats", "ffn_union",
- * "moe_router", "moe_route", "moe_place", "moe_route_grad", "grouped_mm",
+ * "moe_router", "moe_route", "moe_place", "moe_route_grad", "moe_balance",
+ * "moe_balance_sum", "moe_balance_grad", "grouped_mm",
  * "grouped_drelu", "drelu_grad", "grouped_drelu_pack", "grouped_drelu_grad",
  * "drelu_unpack", "grouped_mm_dw", "fp8_quant",
  * "fp8_quant_weights", "fp8_mm", "fp8_drelu", "moe_combine",

@@ -25,7 +25,8 @@ EXPORTED = ["ts_ffn_workspace_bytes", "ts_ffn_sparse", "ts_ffn_sparse_act", "ts_
             "ts_ffn_sparse_given", "ts_moe_workspace_bytes", "ts_moe_sparse",
             "ts_moe_dense", "ts_status_str", "ts_last_error", "ts_version", "ts_prof_enable", "ts_prof_reset",
             "ts_prof_read", "ts_probe_read", "ts_probe_copy", "ts_tune_set",
-            "ts_moe_route_workspace_bytes", "ts_moe_route", "ts_moe_group", "ts_moe_route_grad", "ts_grouped_mm",
+            "ts_moe_route_workspace_bytes", "ts_moe_route", "ts_moe_group", "ts_moe_route_grad",
+            "ts_moe_balance_workspace_bytes", "ts_moe_balance", "ts_moe_balance_grad", "ts_grouped_mm",
             "ts_grouped_drelu", "ts_drelu_grad",
             "ts_grouped_drelu_pack", "ts_grouped_drelu_grad", "ts_drelu_unpack", "ts_grouped_mm_dw", "ts_fp8_quant", "ts_fp8_quant_weights",
             "ts_fp8_mm", "ts_fp8_drelu", "ts_moe_combine", "ts_moe_combine_grad"]
@@ -73,7 +74,11 @@ def _load() -> ctypes.CDLL:
     lib.ts_moe_dense.restype = st
     lib.ts_moe_route_workspace_bytes.argtypes = [i, i, i]
     lib.ts_moe_route_workspace_bytes.restype = sz
+    lib.ts_moe_balance_workspace_bytes.argtypes = [i, i, i]
+    lib.ts_moe_balance_workspace_bytes.restype = sz
     for name, args in (
+            ("ts_moe_balance", [vp, vp, vp, i, i, i, vp, vp, vp, sz, vp]),
+            ("ts_moe_balance_grad", [vp, vp, vp, vp, vp, i, i, i, vp, vp]),
             ("ts_moe_route", [vp, i, i, i, vp, vp, vp, vp, vp, vp, sz, vp]),
             ("ts_moe_group", [vp, i, i, i, vp, vp, vp, vp, sz, vp]),
             ("ts_moe_route_grad", [vp, vp, vp, i, i, i, vp, vp]),
@@ -568,6 +573,58 @@ def moe_route_grad(topk_idx, topk_w, d_w, n_experts: int, out=None, stream=None)
     code = lib.ts_moe_route_grad(_ptr(topk_idx), _ptr(topk_w), _ptr(d_w), T, E, K, _ptr(out), st)
     if code:
         _check(code, "ts_moe_route_grad")
+    return out
+
+
+def _need_mask(mask, T):
+    if mask is not None:
+        _need(mask, "mask", (torch.bool, _u8), (T,))
+
+
+def moe_balance(logits, topk_idx, mask=None, ws=None, stream=None):
+    """ts_moe_balance.  logits [T][E] f32, topk_idx [T][K] int32, mask [T] bool or
+    uint8 (tokens that count).  Returns loss f32 [2] (balance, squared log-sum)
+    and counts int32 [E + 1] (pairs of each expert, tokens)."""
+    if stream is not None:
+        return _run_on(stream, moe_balance, logits, topk_idx, mask, ws)
+    _need(logits, "logits", _f32, 2)
+    T, E = logits.shape
+    _need(topk_idx, "topk_idx", _i32, (T, None))
+    _need_mask(mask, T)
+    st = _here(logits, topk_idx, mask, ws)
+    K, dev = topk_idx.shape[1], logits.device
+    loss, counts = torch.empty(2, dtype=_f32, device=dev), torch.empty(E + 1, dtype=_i32, device=dev)
+    n = 0 if ws is not None else int(lib.ts_moe_balance_workspace_bytes(T, E, K))
+    if n:
+        ws = torch.empty(n, dtype=_u8, device=dev)
+    code = lib.ts_moe_balance(_ptr(logits), _ptr(topk_idx), _ptr(mask), T, E, K, _ptr(loss), _ptr(counts), _ptr(ws),
+                              _nbytes(ws) if ws is not None else 0, st)
+    if code:
+        _check(code, "ts_moe_balance")
+    return loss, counts
+
+
+def moe_balance_grad(logits, counts, d_loss, top_k: int, mask=None, add=None, out=None, stream=None):
+    """ts_moe_balance_grad.  d_loss f32 [2] on the device.  Returns d_logits
+    [T][E], added to `add` if given (out may be add: in place)."""
+    if stream is not None:
+        return _run_on(stream, moe_balance_grad, logits, counts, d_loss, top_k, mask, add, out)
+    _need(logits, "logits", _f32, 2)
+    T, E = logits.shape
+    K = int(top_k)
+    if not 1 <= K <= E:
+        raise ValueError(f"top_k must be in 1..{E}, got {K}")
+    _need(counts, "counts", _i32, (E + 1,))
+    _need(d_loss, "d_loss", _f32, (2,))
+    _need_mask(mask, T)
+    if add is not None:
+        _need(add, "add", _f32, (T, E))
+    st = _here(logits, counts, d_loss, mask, add, out)
+    out = _new(out, "out", (T, E), _f32, logits.device)
+    code = lib.ts_moe_balance_grad(_ptr(logits), _ptr(counts), _ptr(d_loss), _ptr(mask), _ptr(add), T, E, K, _ptr(out),
+                                   st)
+    if code:
+        _check(code, "ts_moe_balance_grad")
     return out
 
 
