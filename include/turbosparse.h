@@ -457,6 +457,35 @@ ts_status ts_fp8_drelu(const void *x, const float *x_scale, const void *w_gate, 
                        const void *w_up, const float *up_scale, const int32_t *row_src, const int32_t *offsets,
                        int rows, int src_rows, int n_groups, int n, int k, void *c, ts_dtype odtype, void *stream);
 
+/* Workspace bytes of ts_adapter_mm (products 1) and ts_adapter_drelu (2); 0:
+ * out of range. */
+size_t ts_adapter_workspace_bytes(int rows, int rank, int products, ts_dtype dtype, ts_dtype odtype);
+
+/*
+ * Low-rank adapters of many requests beside a shared projection.  Rows come in
+ * `segments` (requests): offsets [segments + 1] ascending, adapter [segments]; a
+ * segment whose adapter is outside [0, n_adapters) has none.
+ *   out[r] = x[r] w^T + scale[a] (x[r] a[a]^T) b[a]^T
+ *   x [rows][k], w [n][k], a [n_adapters][rank][k], b [n_adapters][n][rank]; with
+ *   w_kn 1: w [k][n], b [n_adapters][rank][n]; scale fp32 [n_adapters] or NULL (ones).
+ *   rank is a multiple of 8 (TS_BF16) or 4 (TS_F32) up to 128; smaller adapters are
+ *   padded with zeros in a and b.  segments, n_adapters <= 2^23.
+ * ts_adapter_drelu: c = max(0, gate) * max(0, up), both projections adapted so
+ *   (w_gate, w_up [n][k], a pair of a and b for each).
+ * Rows outside the segments are not written.  The product in the middle (rank values a
+ * row) is summed in fp32; with TS_BF16 operands it enters the second product as
+ * bf16, or as two bf16 parts (16 bits) where the output is fp32.  An adapter's
+ * infinities and NaN reach the rows that have it, no others.
+ */
+ts_status ts_adapter_mm(const void *x, const void *w, const void *a, const void *b, const float *scale, ts_dtype dtype,
+                        int w_kn, const int32_t *offsets, const int32_t *adapter, int rows, int segments,
+                        int n_adapters, int rank, int n, int k, void *out, ts_dtype odtype, void *ws, size_t ws_bytes,
+                        void *stream);
+ts_status ts_adapter_drelu(const void *x, const void *w_gate, const void *w_up, const void *a_gate, const void *b_gate,
+                           const void *a_up, const void *b_up, const float *scale, ts_dtype dtype,
+                           const int32_t *offsets, const int32_t *adapter, int rows, int segments, int n_adapters,
+                           int rank, int n, int k, void *c, ts_dtype odtype, void *ws, size_t ws_bytes, void *stream);
+
 /*
  * Combine: out[t] = sum_k w[t][k] y[pair_row[t][k]]; w NULL: weights of one
  * (the sum of the rows' gradients into their token's).  Pairs whose row is
@@ -494,7 +523,7 @@ const char *ts_version(void);
  * "moe_router", "moe_route", "moe_place", "moe_route_grad", "moe_balance",
  * "moe_balance_sum", "moe_balance_grad", "grouped_mm",
  * "grouped_drelu", "drelu_grad", "grouped_drelu_pack", "grouped_drelu_grad",
- * "drelu_unpack", "grouped_mm_dw", "fp8_quant",
+ * "drelu_unpack", "adapter_rows", "adapter_mm", "adapter_drelu", "grouped_mm_dw", "fp8_quant",
  * "fp8_quant_weights", "fp8_mm", "fp8_drelu", "moe_combine",
  * "moe_combine_grad", "batch_prep", "batch_gate_up", "batch_down",
  * "batch_reduce", "batch_stats", "batch_union", "probe_read",

@@ -29,7 +29,7 @@ EXPORTED = ["ts_ffn_workspace_bytes", "ts_ffn_sparse", "ts_ffn_sparse_act", "ts_
             "ts_moe_balance_workspace_bytes", "ts_moe_balance", "ts_moe_balance_grad", "ts_grouped_mm",
             "ts_grouped_drelu", "ts_drelu_grad",
             "ts_grouped_drelu_pack", "ts_grouped_drelu_grad", "ts_drelu_unpack", "ts_grouped_mm_dw", "ts_fp8_quant", "ts_fp8_quant_weights",
-            "ts_fp8_mm", "ts_fp8_drelu", "ts_moe_combine", "ts_moe_combine_grad"]
+            "ts_fp8_mm", "ts_fp8_drelu", "ts_adapter_workspace_bytes", "ts_adapter_mm", "ts_adapter_drelu", "ts_moe_combine", "ts_moe_combine_grad"]
 
 
 class TSError(RuntimeError):
@@ -76,7 +76,11 @@ def _load() -> ctypes.CDLL:
     lib.ts_moe_route_workspace_bytes.restype = sz
     lib.ts_moe_balance_workspace_bytes.argtypes = [i, i, i]
     lib.ts_moe_balance_workspace_bytes.restype = sz
+    lib.ts_adapter_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.ts_adapter_workspace_bytes.restype = sz
     for name, args in (
+            ("ts_adapter_mm", [vp, vp, vp, vp, vp, i, i, vp, vp, i, i, i, i, i, i, vp, i, vp, sz, vp]),
+            ("ts_adapter_drelu", [vp, vp, vp, vp, vp, vp, vp, vp, i, vp, vp, i, i, i, i, i, i, vp, i, vp, sz, vp]),
             ("ts_moe_balance", [vp, vp, vp, i, i, i, vp, vp, vp, sz, vp]),
             ("ts_moe_balance_grad", [vp, vp, vp, vp, vp, i, i, i, vp, vp]),
             ("ts_moe_route", [vp, i, i, i, vp, vp, vp, vp, vp, vp, sz, vp]),
@@ -901,6 +905,77 @@ def fp8_drelu(x, x_scale, w_gate, gate_scale, w_up, up_scale, offsets=None, row_
                             _ptr(row_src), _ptr(offsets), R, S, G, n, k, _ptr(out), od, st)
     if code:
         _check(code, "ts_fp8_drelu")
+    return out
+
+
+def _adapter_shapes(x, offsets, adapter, scale, a, name):
+    """(rows, k, segments, adapters, rank)."""
+    _need(x, "x", (_f32, _bf16), 2)
+    R, k = x.shape
+    _need(a, name, x.dtype, (None, None, k))
+    N, rank = a.shape[:2]
+    _need(adapter, "adapter", _i32, 1)
+    S = adapter.shape[0]
+    _need(offsets, "offsets", _i32, (S + 1,))
+    if scale is not None:
+        _need(scale, "scale", _f32, (N,))
+    return R, k, S, N, rank
+
+
+def adapter_workspace_bytes(rows: int, rank: int, products: int, dtype, out_dtype) -> int:
+    return int(lib.ts_adapter_workspace_bytes(rows, rank, products, wdtype_of_rows(dtype), wdtype_of_rows(out_dtype)))
+
+
+def _adapter_ws(dev, ws, *sizes):
+    return ws if ws is not None else torch.empty(adapter_workspace_bytes(*sizes), dtype=_u8, device=dev)
+
+
+def adapter_mm(x, w, a, b, offsets, adapter, scale=None, w_kn: bool = False, out=None, out_dtype=None, ws=None,
+               stream=None):
+    """ts_adapter_mm.  x [rows][k], w [n][k], a [N][rank][k], b [N][n][rank]; with
+    w_kn w [k][n], b [N][rank][n]; bf16 or f32, one dtype; offsets [S + 1], adapter
+    [S] int32, scale [N] f32 or None.  Returns out [rows][n] (x's dtype unless
+    given); rows outside the segments are not written."""
+    if stream is not None:
+        return _run_on(stream, adapter_mm, x, w, a, b, offsets, adapter, scale, w_kn, out, out_dtype, ws)
+    R, k, S, N, rank = _adapter_shapes(x, offsets, adapter, scale, a, "a")
+    _need(w, "w", x.dtype, (k, None) if w_kn else (None, k))
+    n = w.shape[1] if w_kn else w.shape[0]
+    _need(b, "b", x.dtype, (N, rank, n) if w_kn else (N, n, rank))
+    odt, od = _odtype(out, out_dtype, x.dtype)
+    st = _here(x, w, a, b, offsets, adapter, scale, out, ws)
+    out = _new(out, "out", (R, n), odt, x.device)
+    ws = _adapter_ws(x.device, ws, R, rank, 1, x.dtype, odt)
+    code = lib.ts_adapter_mm(_ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), wdtype_of_rows(x.dtype), int(bool(w_kn)),
+                             _ptr(offsets), _ptr(adapter), R, S, N, rank, n, k, _ptr(out), od, _ptr(ws), _nbytes(ws), st)
+    if code:
+        _check(code, "ts_adapter_mm")
+    return out
+
+
+def adapter_drelu(x, w_gate, w_up, a_gate, b_gate, a_up, b_up, offsets, adapter, scale=None, out=None, out_dtype=None,
+                  ws=None, stream=None):
+    """ts_adapter_drelu.  w_gate, w_up [n][k], a_gate, a_up [N][rank][k], b_gate,
+    b_up [N][n][rank], the rest as adapter_mm.  Returns c [rows][n]."""
+    if stream is not None:
+        return _run_on(stream, adapter_drelu, x, w_gate, w_up, a_gate, b_gate, a_up, b_up, offsets, adapter, scale, out,
+                       out_dtype, ws)
+    R, k, S, N, rank = _adapter_shapes(x, offsets, adapter, scale, a_gate, "a_gate")
+    _need(w_gate, "w_gate", x.dtype, (None, k))
+    n = w_gate.shape[0]
+    _need(w_up, "w_up", x.dtype, (n, k))
+    _need(a_up, "a_up", x.dtype, (N, rank, k))
+    _need(b_gate, "b_gate", x.dtype, (N, n, rank))
+    _need(b_up, "b_up", x.dtype, (N, n, rank))
+    odt, od = _odtype(out, out_dtype, x.dtype)
+    st = _here(x, w_gate, w_up, a_gate, b_gate, a_up, b_up, offsets, adapter, scale, out, ws)
+    out = _new(out, "out", (R, n), odt, x.device)
+    ws = _adapter_ws(x.device, ws, R, rank, 2, x.dtype, odt)
+    code = lib.ts_adapter_drelu(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(a_gate), _ptr(b_gate), _ptr(a_up), _ptr(b_up),
+                                _ptr(scale), wdtype_of_rows(x.dtype), _ptr(offsets), _ptr(adapter), R, S, N, rank, n,
+                                k, _ptr(out), od, _ptr(ws), _nbytes(ws), st)
+    if code:
+        _check(code, "ts_adapter_drelu")
     return out
 
 

@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libturbosparse.so")
 ARCH = os.environ.get("TS_OFFLOAD_ARCH", "gfx950")
 
 HIP_SOURCES = ["ts_ffn.hip", "ts_batch.hip", "ts_wide.hip", "ts_rows.hip", "ts_gmm.hip", "ts_fp8.hip", "ts_keep.hip", "ts_route.hip",
-               "ts_balance.hip", "ts_probe.hip", "ts_runtime.cpp"]
+               "ts_balance.hip", "ts_adapt.hip", "ts_probe.hip", "ts_runtime.cpp"]
 HOST_SOURCES = ["ts_plan.cpp", "ts_group.cpp"]
 
 # -packed-fp32-ops: keep the compiler from emitting packed fp32 VALU ops.

@@ -60,9 +60,11 @@ static __device__ const u32x4 g_zero_chunk[8] = {};  // (a step's 128 bytes of a
 
 // kDreluPack: dReLU whose activations are also kept in 8 bits; kDreluGrad: a
 // forward product (the gradient of Combined) with dReLU's gradient behind it.
-enum GmmMode { kFwd = 0, kDrelu = 1, kGradW = 2, kDreluPack = 3, kDreluGrad = 4 };
+// kFwdAdapt, kDreluAdapt: one group, with the rows' adapters.
+enum GmmMode { kFwd = 0, kDrelu = 1, kGradW = 2, kDreluPack = 3, kDreluGrad = 4, kFwdAdapt = 5, kDreluAdapt = 6 };
 // Gate and up interleaved in the P operand.
-constexpr bool is_drelu(GmmMode m) { return m == kDrelu || m == kDreluPack; }
+constexpr bool is_drelu(GmmMode m) { return m == kDrelu || m == kDreluPack || m == kDreluAdapt; }
+constexpr bool is_adapt(GmmMode m) { return m == kFwdAdapt || m == kDreluAdapt; }
 
 template <GmmMode MODE>
 struct GmmArgsOf {
@@ -75,6 +77,14 @@ struct GmmArgsOf<kDreluPack> {
 template <>
 struct GmmArgsOf<kDreluGrad> {
     using type = GmmKeepArgs;
+};
+template <>
+struct GmmArgsOf<kFwdAdapt> {
+    using type = GmmAdaptArgs;
+};
+template <>
+struct GmmArgsOf<kDreluAdapt> {
+    using type = GmmAdaptArgs;
 };
 
 // 16 bytes a lane from global memory into LDS at byte `l` + 16 x lane (all
@@ -149,6 +159,14 @@ __device__ __forceinline__ void seg_bounds(const GmmArgs &a, int lane, int &b, i
     e = min(max(a.offsets[min(lane + 1, a.groups)], 0), a.rows);
     b = wave_scan<true>(b);
     e = max(b, e);
+}
+
+// The rows of all segments, as one group.
+__device__ __forceinline__ void seg_bounds(const GmmAdaptArgs &a, int lane, int &b, int &e) {
+    b = e = 0;
+    if (lane > 0) return;
+    b = min(max(a.offsets[0], 0), a.rows);
+    e = max(b, min(max(a.offsets[a.segs], 0), a.rows));
 }
 
 template <GmmKind KIND>
@@ -270,6 +288,93 @@ __device__ __forceinline__ void unroll(F f) {
 
 constexpr int kStrip = 8;
 
+// Whether 16 bytes of bf16 or fp32 values hold an infinity or a NaN; those values
+// alone (BAD), or all others.
+template <GmmKind KIND>
+__device__ __forceinline__ bool not_finite(u32x4 v) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        bad |= KIND == kGmmF32 ? (v[i] & 0x7F800000u) == 0x7F800000u
+                               : (((v[i] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) != 0u;
+    return bad;
+}
+template <GmmKind KIND, bool BAD>
+__device__ __forceinline__ u32x4 only_finite(u32x4 v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t bad;  // their bits
+        if constexpr (KIND == kGmmF32) {
+            bad = (v[i] & 0x7F800000u) == 0x7F800000u ? ~0u : 0u;
+        } else {
+            const uint32_t top = ((v[i] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+            bad = (top & 0x80000000u ? 0xFFFF0000u : 0u) | (top & 0x8000u ? 0xFFFFu : 0u);
+        }
+        v[i] &= BAD ? bad : ~bad;
+    }
+    return v;
+}
+
+// One 64-byte sub-step of contraction of a 16 x 16 block, bf16 or fp32.
+template <GmmKind KIND>
+__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (KIND == kGmmBf16) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+                                                       0, 0, 0);
+    } else {
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[v]), __uint_as_float(b[v]), c, 0, 0, 0);
+        return c;
+    }
+}
+
+// Slots of a tile's adapters, by one wave.  Row q of the tile (ids[c], lane l: q =
+// 64 c + l; -1: none) gets the slot of its adapter in slot[q] (-1), the slots'
+// adapters stand in ad[], in the order of their first rows.  Returns how many.
+// Runs of rows with one adapter are looked up one after another: a tile of prompts
+// has few.
+template <int BQ>
+__device__ __forceinline__ int adapter_slots(const int (&ids)[(BQ + 63) / 64], int lane, int *ad, int *slot) {
+    constexpr int NC = (BQ + 63) / 64;
+    int list[NC], n = 0, last_id = -1, last_slot = -1;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) list[c] = -1;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const int id = ids[c];
+        int before = __shfl_up(id, 1);
+        if (lane == 0) before = last_id;
+        uint64_t starts = __ballot(id != before && id >= 0);
+        int mine = last_slot;
+        while (starts) {
+            const int at = __builtin_ctzll(starts);
+            starts &= starts - 1;
+            const int want = __builtin_amdgcn_readlane(id, at);
+            int s = -1;
+#pragma unroll
+            for (int d = 0; d < NC; ++d) {
+                const uint64_t same = __ballot(list[d] == want);
+                if (same) s = 64 * d + __builtin_ctzll(same);
+            }
+            if (s < 0) {
+                s = n++;
+#pragma unroll
+                for (int d = 0; d < NC; ++d)
+                    if (s == 64 * d + lane) list[d] = want;
+            }
+            mine = lane >= at ? s : mine;
+        }
+        if (64 * c + lane < BQ) slot[64 * c + lane] = id >= 0 ? mine : -1;
+        last_id = __builtin_amdgcn_readlane(id, 63);
+        last_slot = __builtin_amdgcn_readlane(mine, 63);
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+        if (64 * c + lane < n) ad[64 * c + lane] = list[c];
+    return n;
+}
+
 // LDS of one contraction group of gmm_tiled in 16-byte chunks: the stages of
 // both operands and (fp8) of the scales.
 template <GmmKind KIND, int BP, int BQ, int WP, int WQ, int AR, int BR>
@@ -367,6 +472,16 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
         }
     }
     const int p0 = pt * PT;
+    // (asked for here, needed behind the product)
+    [[maybe_unused]] int ids[(BQ + 63) / 64];
+    if constexpr (is_adapt(MODE)) {
+#pragma unroll
+        for (int c = 0; c < (BQ + 63) / 64; ++c) {
+            const int q = 64 * c + lane;
+            const int id = a.ids[min(q0 + q, q_end - 1)];
+            ids[c] = q < BQ && q0 + q < q_end && id >= 0 && id < a.adapters ? id : -1;
+        }
+    }
     // contraction: k, or the group's rows, in blocks of KS
     const int C = MODE == kGradW ? e - b : a.k;
     const int blocks = (C + KS - 1) / KS;
@@ -718,6 +833,96 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
             }
             ar = ar == AR - 1 ? 0 : ar + 1;
             br = BR == 1 || br == BR - 1 ? 0 : br + 1;
+        }
+        gmm_barrier<0>();
+    }
+    if constexpr (is_adapt(MODE)) {
+        // Rows' adapters, as a contraction over the ranks of all adapters that the
+        // tile has, one after another: a row's t stands at its own adapter's ranks,
+        // zeros at the others', so the bytes are those of the adapters' B and a
+        // tile of single-token requests takes as few steps as their ranks fill.
+        int *tab;
+        if constexpr (AR >= 3) {
+            tab = reinterpret_cast<int *>(s_all + (AR - 1) * TA::CHUNKS);  // (two stages are used below)
+        } else {
+            __shared__ int own[2 * BQ + 1];
+            tab = own;
+        }
+        int *const ad = tab, *const slot = tab + BQ;
+        if (threadIdx.x < 64) {
+            const int n = adapter_slots<BQ>(ids, lane, ad, slot);
+            if (lane == 0) tab[2 * BQ] = n;
+        }
+        __syncthreads();
+        const int r2 = DRELU ? 2 * a.rank : a.rank, per = r2 * a.parts;  // ranks of a slot
+        const int all = __builtin_amdgcn_readfirstlane(tab[2 * BQ]) * per, steps = (all + KS - 1) / KS;
+        const bool second = DRELU && (((wave * (64 / TA::CR)) >> 4) & 1);
+        const char *const bbase = second ? a.b[1] : a.b[0];
+        const uint32_t lds_a = lds_addr(s_a) + wave * 1024, lds_b = lds_a + AR * TA::CHUNKS * 16;
+        auto load = [&](int step, int to) {
+            unroll<TB::NJ>([&](auto j) {
+                int row, ch;
+                TB::at(tid + THREADS * j, row, ch);
+                const int v = step * KS + ch * (16 / SZ), s = v / per;
+                const char *p = slot[row] == s ? a.t + ((size_t)(q0 + row) * per + (v - s * per)) * SZ : zero;
+                ld_lds16(p, lds_b + (uint32_t)(to * TB::CHUNKS + THREADS * j) * 16);
+            });
+            unroll<TA::NJ>([&](auto j) {
+                int row, ch;
+                TA::at(tid + THREADS * j, row, ch);
+                const int v = step * KS + (ACOL ? row : ch * (16 / SZ)), s = v / per;
+                int r = v - s * per;
+                if (r >= r2) r -= r2;  // (a part's lower half meets the same B)
+                const char *p = zero;
+                if (v < all) {
+                    const size_t m = ad[s];
+                    if constexpr (ACOL) {
+                        p = bbase + (m * a.rank + r) * ((size_t)a.n * SZ) + min(p0 * SZ + ch * 16, a.n * SZ - 16);
+                    } else if (DRELU) {
+                        const int n = min(p0 + (row >> 5) * 16 + (row & 15), a.n - 1);
+                        if ((r >= a.rank) == second) p = bbase + ((m * a.n + n) * a.rank + (r - (second ? a.rank : 0))) * SZ;
+                    } else {
+                        p = bbase + ((m * a.n + min(p0 + row, a.n - 1)) * a.rank + r) * SZ;
+                    }
+                }
+                ld_lds16(p, lds_a + (uint32_t)(to * TA::CHUNKS + THREADS * j) * 16);
+            });
+        };
+        if (kg < steps) load(kg, 0);
+        for (int i = 0; i * KW < steps; ++i) {
+            gmm_barrier<0>();
+            const int step = kg + i * KW;
+            if (step + KW < steps) load(step + KW, (i + 1) & 1);
+            if (step >= steps) continue;
+            const u32x4 *const A = s_a + (i & 1) * TA::CHUNKS, *const B = s_b + (i & 1) * TB::CHUNKS;
+#pragma unroll
+            for (int s = 0; s < RB / 64; ++s) {
+                u32x4 bf[MJ];
+#pragma unroll
+                for (int j = 0; j < MJ; ++j) bf[j] = TB::frag(B, wq * MJ + j, s, lane);
+#pragma unroll
+                for (int m = 0; m < MI; ++m) {
+                    u32x4 af = TA::frag(A, wp * MI + m, s, lane);
+                    if (__any(not_finite<KIND>(af))) {
+                        // An adapter's infinities and NaN concern its own rows: 0 x
+                        // inf of the others is left out, 16 bytes of ranks at a time.
+                        const u32x4 bad = only_finite<KIND, true>(af);
+                        for (int h = 0; h < 4; ++h) {
+                            const u32x4 one = lq == h ? bad : u32x4{0u, 0u, 0u, 0u};
+                            if (!__any(not_finite<KIND>(one))) continue;
+                            const int own = (step * KS + s * (64 / SZ) + h * (16 / SZ)) / per;
+#pragma unroll
+                            for (int j = 0; j < MJ; ++j) {
+                                const f32x4 d = mma<KIND>(one, bf[j], f32x4{0.f, 0.f, 0.f, 0.f});
+                                if (slot[(wq * MJ + j) * 16 + lm] == own) acc[m][j] += d;
+                            }
+                        }
+                        af = only_finite<KIND, false>(af);
+                    }
+#pragma unroll
+                    for (int j = 0; j < MJ; ++j) acc[m][j] = mma<KIND>(af, bf[j], acc[m][j]);
+                }
+            }
         }
         gmm_barrier<0>();
     }

@@ -45,6 +45,14 @@ struct GmmKeepArgs : GmmArgs {
     uint8_t *exps = nullptr;   // [rows][ceil(n / 16)][2]
 };
 
+// Adapters beside one group's product (ts_adapt.hip).  offsets: the segments'.
+struct GmmAdaptArgs : GmmArgs {
+    const char *t = nullptr;            // [rows][parts][gate's ranks, up's]: scale x A^T, from adapter_rows
+    const int32_t *ids = nullptr;       // [rows]: a row's adapter
+    const char *b[2] = {nullptr, nullptr};
+    int segs = 0, adapters = 0, rank = 0, parts = 1;
+};
+
 // Tiles of the forward products: columns (dReLU: of gate and up together) x
 // rows, workgroups of it that a compute unit holds, stages, contraction groups.
 // (equal costs: the first)
