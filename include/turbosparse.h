@@ -459,7 +459,8 @@ ts_status ts_fp8_drelu(const void *x, const float *x_scale, const void *w_gate, 
 
 /* Workspace bytes of ts_adapter_mm (products 1) and ts_adapter_drelu (2); 0:
  * out of range. */
-size_t ts_adapter_workspace_bytes(int rows, int rank, int products, ts_dtype dtype, ts_dtype odtype);
+size_t ts_adapter_workspace_bytes(int rows, int rank, int products, int w_kn, int n, int k, ts_dtype dtype,
+                                  ts_dtype odtype);
 
 /*
  * Low-rank adapters of many requests beside a shared projection.  Rows come in
@@ -523,7 +524,8 @@ const char *ts_version(void);
  * "moe_router", "moe_route", "moe_place", "moe_route_grad", "moe_balance",
  * "moe_balance_sum", "moe_balance_grad", "grouped_mm",
  * "grouped_drelu", "drelu_grad", "grouped_drelu_pack", "grouped_drelu_grad",
- * "drelu_unpack", "adapter_rows", "adapter_mm", "adapter_drelu", "grouped_mm_dw", "fp8_quant",
+ * "drelu_unpack", "adapter_rows", "adapter_mm", "adapter_drelu", "adapter_sum",
+ * "grouped_mm_dw", "fp8_quant",
  * "fp8_quant_weights", "fp8_mm", "fp8_drelu", "moe_combine",
  * "moe_combine_grad", "batch_prep", "batch_gate_up", "batch_down",
  * "batch_reduce", "batch_stats", "batch_union", "probe_read",

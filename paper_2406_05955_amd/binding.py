@@ -76,7 +76,7 @@ def _load() -> ctypes.CDLL:
     lib.ts_moe_route_workspace_bytes.restype = sz
     lib.ts_moe_balance_workspace_bytes.argtypes = [i, i, i]
     lib.ts_moe_balance_workspace_bytes.restype = sz
-    lib.ts_adapter_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.ts_adapter_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
     lib.ts_adapter_workspace_bytes.restype = sz
     for name, args in (
             ("ts_adapter_mm", [vp, vp, vp, vp, vp, i, i, vp, vp, i, i, i, i, i, i, vp, i, vp, sz, vp]),
@@ -922,8 +922,9 @@ def _adapter_shapes(x, offsets, adapter, scale, a, name):
     return R, k, S, N, rank
 
 
-def adapter_workspace_bytes(rows: int, rank: int, products: int, dtype, out_dtype) -> int:
-    return int(lib.ts_adapter_workspace_bytes(rows, rank, products, wdtype_of_rows(dtype), wdtype_of_rows(out_dtype)))
+def adapter_workspace_bytes(rows: int, rank: int, products: int, w_kn: bool, n: int, k: int, dtype, out_dtype) -> int:
+    return int(lib.ts_adapter_workspace_bytes(rows, rank, products, int(bool(w_kn)), n, k, wdtype_of_rows(dtype),
+                                              wdtype_of_rows(out_dtype)))
 
 
 def _adapter_ws(dev, ws, *sizes):
@@ -945,7 +946,7 @@ def adapter_mm(x, w, a, b, offsets, adapter, scale=None, w_kn: bool = False, out
     odt, od = _odtype(out, out_dtype, x.dtype)
     st = _here(x, w, a, b, offsets, adapter, scale, out, ws)
     out = _new(out, "out", (R, n), odt, x.device)
-    ws = _adapter_ws(x.device, ws, R, rank, 1, x.dtype, odt)
+    ws = _adapter_ws(x.device, ws, R, rank, 1, w_kn, n, k, x.dtype, odt)
     code = lib.ts_adapter_mm(_ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), wdtype_of_rows(x.dtype), int(bool(w_kn)),
                              _ptr(offsets), _ptr(adapter), R, S, N, rank, n, k, _ptr(out), od, _ptr(ws), _nbytes(ws), st)
     if code:
@@ -970,7 +971,7 @@ def adapter_drelu(x, w_gate, w_up, a_gate, b_gate, a_up, b_up, offsets, adapter,
     odt, od = _odtype(out, out_dtype, x.dtype)
     st = _here(x, w_gate, w_up, a_gate, b_gate, a_up, b_up, offsets, adapter, scale, out, ws)
     out = _new(out, "out", (R, n), odt, x.device)
-    ws = _adapter_ws(x.device, ws, R, rank, 2, x.dtype, odt)
+    ws = _adapter_ws(x.device, ws, R, rank, 2, False, n, k, x.dtype, odt)
     code = lib.ts_adapter_drelu(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(a_gate), _ptr(b_gate), _ptr(a_up), _ptr(b_up),
                                 _ptr(scale), wdtype_of_rows(x.dtype), _ptr(offsets), _ptr(adapter), R, S, N, rank, n,
                                 k, _ptr(out), od, _ptr(ws), _nbytes(ws), st)

@@ -2,10 +2,12 @@
 //   y[r] = x[r] W^T + s_a (x[r] A_a^T) B_a^T,  a = adapter of r's segment (or none)
 // and the same in front of dReLU for gate and up.
 //
-// Two launches.  adapter_rows computes t = s_a x A_a^T, `rank` values a row (a
-// few ranks, a long contraction).  The product then contracts t with B behind x with
-// W, in the same accumulators (gmm_tiled's adapter steps): y is written once and nothing is
-// read twice.
+// adapter_rows computes t = s_a x A_a^T, `rank` values a row (a few ranks, a long
+// contraction), and of each row tile of the product which adapters it meets.  The
+// product then contracts t with B behind x with W, in the same accumulators
+// (gmm_tiled's adapter steps): y is written once and nothing is read twice.  Few
+// rows and columns with a long contraction share it among workgroups, whose sums
+// a third launch adds in a fixed order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -24,8 +26,10 @@ struct AdaptRowsArgs {
     const float *scale = nullptr;
     const int32_t *offsets = nullptr, *adapter = nullptr;
     char *t = nullptr;
-    int32_t *ids = nullptr;
+    int32_t *slots = nullptr, *slot_ad = nullptr, *slot_count = nullptr;
     int rows = 0, segs = 0, adapters = 0, rank = 0, ranks = 0, parts = 1, k = 0;  // ranks: of both matrices
+    int pieces = 0, per = 16;     // ranks of a workgroup
+    int wr = 0, blocks = 0;       // rows of one of the product's waves, their number
 };
 
 // Segment s's rows in pieces of Q: its first piece has the number offsets[s] / Q +
@@ -46,6 +50,59 @@ __device__ __forceinline__ int segment_of(const AdaptRowsArgs &a, int p, int lan
     return lo;
 }
 
+// Slots of the adapters of rows r0 ... of one of the product's waves (a.wr rows: lane
+// l has row r0 + l), by one wave: a slot for each adapter, in the order of their
+// first rows.  Runs of rows with one adapter are looked up one after another: prompts
+// have few.
+__device__ __forceinline__ void wave_slots(const AdaptRowsArgs &a, int block, int lane) {
+    const int b = min(max(a.offsets[0], 0), a.rows), e = min(max(a.offsets[a.segs], 0), a.rows);
+    const int r0 = b + block * a.wr, row = r0 + lane;
+    if (r0 >= e) return;
+    // the last segment that begins at or in front of the row
+    int lo = 0, hi = a.segs;
+    while (__any(hi - lo > 1)) {
+        const int mid = (lo + hi) / 2;
+        if (hi - lo > 1) (a.offsets[mid] <= row ? lo : hi) = mid;
+    }
+    int id = a.adapter[lo];
+    if (lane >= a.wr || row >= e || id < 0 || id >= a.adapters) id = -1;
+    const int before = __shfl_up(id, 1);
+    uint64_t starts = __ballot(id >= 0 && (lane == 0 || id != before));
+    int list = -1, n = 0, slot = -1;
+    while (starts) {
+        const int at = __builtin_ctzll(starts);
+        starts &= starts - 1;
+        const int want = __builtin_amdgcn_readlane(id, at);
+        const uint64_t same = __ballot(list == want);
+        const int s = same ? __builtin_ctzll(same) : n++;
+        if (lane == s) list = want;
+        if (lane >= at) slot = s;
+    }
+    if (lane < a.wr) {
+        a.slots[(size_t)block * a.wr + lane] = id >= 0 ? slot : -1;
+        a.slot_ad[(size_t)block * a.wr + lane] = max(list, 0);
+    }
+    if (lane == 0) a.slot_count[block] = n;
+}
+
+// Where t of a row and rank stands: gate's parts, then up's.
+__device__ __forceinline__ size_t t_at(const AdaptRowsArgs &a, int row, int r) {
+    return (size_t)row * a.ranks * a.parts + r + (r >= a.rank ? (size_t)a.rank * (a.parts - 1) : 0);
+}
+template <GmmKind KIND>
+__device__ __forceinline__ void store_t(const AdaptRowsArgs &a, int row, int r, float v) {
+    const size_t at = t_at(a, row, r);
+    if constexpr (KIND == kGmmF32) {
+        reinterpret_cast<float *>(a.t)[at] = v;
+    } else {
+        __bf16 *const t = reinterpret_cast<__bf16 *>(a.t);
+        const __bf16 hi = (__bf16)v;
+        t[at] = hi;
+        // what the first rounding left (nothing of what has no remainder)
+        if (a.parts == 2) t[at + a.rank] = (__bf16)(fabsf((float)hi) < INFINITY ? v - (float)hi : 0.f);
+    }
+}
+
 }  // namespace
 
 // t of up to 16 RT rows of a segment and 16 NR ranks; W waves share the contraction,
@@ -53,25 +110,76 @@ __device__ __forceinline__ int segment_of(const AdaptRowsArgs &a, int p, int lan
 template <GmmKind KIND, int RT, int NR, int W>
 __global__ __launch_bounds__(64 * W) void adapter_rows(AdaptRowsArgs a) {
     constexpr int SZ = GmmElem<KIND>::SZ, KS = 64 / SZ, CE = 16 / SZ, Q = 16 * RT;
-    constexpr int U = RT * NR == 1 ? 8 : RT * NR <= 8 ? 4 : 2;  // steps whose loads are on their way together
+    constexpr int U = RT * NR == 1 ? 8 : 4;  // steps whose loads are on their way together
     __shared__ f32x4 red[W][RT * NR][64];
     const int lane = threadIdx.x & 63, lm = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int)blockIdx.x >= a.pieces) {
+        const int block = ((int)blockIdx.x - a.pieces) * W + wave;
+        if (blockIdx.y == 0 && block < a.blocks) wave_slots(a, block, lane);
+        return;
+    }
     const int seg = __builtin_amdgcn_readfirstlane(segment_of<Q>(a, blockIdx.x, lane));
     const int b = min(max(a.offsets[seg], 0), a.rows), e = min(max(a.offsets[seg + 1], 0), a.rows);
     const int piece = (int)blockIdx.x - (b / Q + seg);
     if (piece < 0 || b + (long long)piece * Q >= e) return;
     const int r0 = b + piece * Q, r1 = min(r0 + Q, e);
     const int id = a.adapter[seg];
-    const bool none = id < 0 || id >= a.adapters;
-    if (blockIdx.y == 0 && (int)threadIdx.x < r1 - r0) a.ids[r0 + threadIdx.x] = none ? -1 : id;
-    if (none) return;
+    if (id < 0 || id >= a.adapters) return;
+    // ranks [k0, k1) (of both matrices, one behind the other)
+    const int k0 = blockIdx.y * a.per, k1 = min(k0 + a.per, a.ranks);
 
     const size_t row_bytes = (size_t)a.k * SZ;
+    const float scale = a.scale ? a.scale[id] : 1.f;
+    if constexpr (RT == 1) {
+        if (r1 - r0 == 1) {
+            // A single row (a decoded token): W / a.per waves a rank, 1 KB of its A a load,
+            // all of a wave's loads on their way together (as a matrix product, 16 rows x
+            // 64 bytes a load and 1 of 16 columns used: k 14336 rank 16 15 us, this 8).
+            constexpr int V = 8;
+            float *const part = reinterpret_cast<float *>(red);
+            const int g = W / a.per, r = k0 + wave / g, chunks = a.k / CE;
+            float sum = 0.f;
+            if (r < k1) {
+                const bool second = r >= a.rank;
+                const char *const pa = a.a[second] + ((size_t)id * a.rank + (second ? r - a.rank : r)) * row_bytes;
+                const char *const px = a.x + (size_t)r0 * row_bytes;
+                for (int c0 = wave % g * 64 + lane; c0 < chunks; c0 += V * g * 64) {
+                    u32x4 va[V], vx[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const size_t at = (size_t)min(c0 + v * g * 64, chunks - 1) * 16;
+                        va[v] = ld_cached(pa + at);
+                        vx[v] = ld_cached(px + at);
+                    }
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        using T = std::conditional_t<KIND == kGmmF32, float, uint16_t>;
+                        float fa[CE], fx[CE];
+                        unpack<T>(va[v], fa);
+                        unpack<T>(vx[v], fx);
+                        float dot = 0.f;
+#pragma unroll
+                        for (int i = 0; i < CE; ++i) dot += fa[i] * fx[i];
+                        sum += c0 + v * g * 64 < chunks ? dot : 0.f;
+                    }
+                }
+            }
+            sum = wave_sum(sum);
+            if (lane == 0) part[wave] = sum;
+            __syncthreads();
+            const int i = threadIdx.x, rr = k0 + i;
+            if (i >= a.per || rr >= k1) return;
+            float v = part[i * g];
+            for (int w = 1; w < g; ++w) v += part[i * g + w];
+            store_t<KIND>(a, r0, rr, v * scale);
+            return;
+        }
+    }
     const char *ar[NR], *xr[RT];
 #pragma unroll
     for (int f = 0; f < NR; ++f) {
-        const int r = min(((int)blockIdx.y * NR + f) * 16 + lm, a.ranks - 1);
+        const int r = min(k0 + f * 16 + lm, k1 - 1);
         const bool second = r >= a.rank;
         ar[f] = a.a[second] + ((size_t)id * a.rank + (second ? r - a.rank : r)) * row_bytes;
     }
@@ -110,27 +218,46 @@ __global__ __launch_bounds__(64 * W) void adapter_rows(AdaptRowsArgs a) {
 #pragma unroll
         for (int j = 0; j < RT; ++j) red[wave][f * RT + j][lane] = acc[f][j];
     __syncthreads();
-    const float scale = a.scale ? a.scale[id] : 1.f;
     for (int i = wave; i < NR * RT; i += W) {
         f32x4 v = red[0][i][lane];
 #pragma unroll
         for (int w = 1; w < W; ++w) v += red[w][i][lane];
         v *= scale;
         // lane (lm, lq): ranks 4 lq ... of row lm
-        const int row = r0 + i % RT * 16 + lm, r = ((int)blockIdx.y * NR + i / RT) * 16 + 4 * lq;
-        if (row >= r1 || r >= a.ranks) continue;
-        const size_t at = (size_t)row * a.ranks * a.parts + r;
-        store4(a.t, KIND == kGmmF32, at, v);
-        if (KIND == kGmmBf16 && a.parts == 2) {
-            // what the first rounding left (nothing of what has no remainder)
-            f32x4 rest;
+        const int row = r0 + i % RT * 16 + lm, r = k0 + i / RT * 16 + 4 * lq;
+        if (row >= r1 || r >= k1) continue;
+        if constexpr (KIND == kGmmF32) {
+            *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.t) + t_at(a, row, r)) = v;
+        } else {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const float hi = (float)(__bf16)v[c];
-                rest[c] = fabsf(hi) < INFINITY ? v[c] - hi : 0.f;
-            }
-            store4(a.t, 0, at + a.ranks, rest);
+            for (int c = 0; c < 4; ++c) store_t<KIND>(a, row, r + c, v[c]);
         }
+    }
+}
+
+// The sums of `split` workgroups a tile, in their order; dReLU behind gate's and
+// up's.  Four columns a lane.
+template <bool DRELU>
+__global__ __launch_bounds__(256) void adapter_sum_kernel(GmmAdaptArgs a) {
+    constexpr int both = DRELU ? 2 : 1;
+    const int b = min(max(a.offsets[0], 0), a.rows), e = min(max(a.offsets[a.segs], 0), a.rows);
+    const long long per = a.n / 4, total = (e - b) * per, step = (long long)gridDim.x * 256;
+    const size_t part = (size_t)a.rows * both * a.n;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+        const size_t q = b + i / per, p = i % per * 4;
+        const float *s = a.sums + q * both * a.n + p;
+        f32x4 v[both];
+#pragma unroll
+        for (int h = 0; h < both; ++h) {
+            v[h] = *reinterpret_cast<const f32x4 *>(s + (size_t)h * a.n);
+#pragma unroll 4
+            for (int k = 1; k < a.split; ++k) v[h] += *reinterpret_cast<const f32x4 *>(s + k * part + (size_t)h * a.n);
+        }
+        if constexpr (DRELU) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[0][c] = drelu1(v[0][c], v[1][c]);
+        }
+        store4(a.out, a.out_f32, q * a.n + p, v[0]);
     }
 }
 
@@ -151,9 +278,34 @@ bool adapt_dims_ok(int rows, int rank, ts_dtype dtype) {
     return rows >= 0 && rows <= kMaxRows && rank >= quantum(dtype) && rank <= kMaxRank && rank % quantum(dtype) == 0;
 }
 
-size_t adapt_ws_bytes(int rows, int rank, int products, ts_dtype dtype, ts_dtype odtype) {
-    if (!type_ok(dtype) || !type_ok(odtype) || products < 1 || products > 2 || !adapt_dims_ok(rows, rank, dtype)) return 0;
-    return adapt_t_bytes(rows, rank, products, dtype, odtype) + align_up256((size_t)rows * 4);
+struct AdaptPlan {
+    GmmTileId tile;
+    int split;
+    size_t t, slots, sums;  // bytes
+    size_t all() const { return t + slots + sums; }
+};
+
+AdaptPlan adapt_plan(int rows, int rank, int products, bool w_kn, int n, int k, ts_dtype dtype, ts_dtype odtype) {
+    AdaptPlan p;
+    const bool drelu = products == 2;
+    const GmmKind kind = dtype == TS_F32 ? kGmmF32 : kGmmBf16;
+    const int esz = dtype == TS_F32 ? 4 : 2;
+    const bool wide = (unsigned long long)rows * k * esz >= (1ull << 32);
+    p.tile = kTile128x128;
+    p.split = 1;
+    if (!wide && rows > 0) adapt_tile(kind, drelu, w_kn, rows, n, k, &p.tile, &p.split);
+    p.t = adapt_t_bytes(rows, rank, products, dtype, odtype);
+    const size_t wr = wave_rows(p.tile), blocks = ceil_div(rows, (int)wr);
+    p.slots = align_up256(blocks * (wr + wr + 1) * 4);
+    p.sums = p.split > 1 ? align_up256((size_t)p.split * rows * products * n * 4) : 0;
+    return p;
+}
+
+size_t adapt_ws_bytes(int rows, int rank, int products, bool w_kn, int n, int k, ts_dtype dtype, ts_dtype odtype) {
+    if (!type_ok(dtype) || !type_ok(odtype) || products < 1 || products > 2 || !adapt_dims_ok(rows, rank, dtype) ||
+        check_group_dims(rows, 1, n, k, quantum(dtype)) != TS_OK)
+        return 0;
+    return adapt_plan(rows, rank, products, w_kn, n, k, dtype, odtype).all();
 }
 
 struct AdaptCall {
@@ -168,16 +320,25 @@ struct AdaptCall {
 };
 
 template <GmmKind KIND, int RT, int NR, int W>
-ts_status run_rows(const AdaptRowsArgs &r, hipStream_t st) {
+ts_status run_rows(AdaptRowsArgs r, hipStream_t st) {
     const long long pieces = (long long)r.rows / (16 * RT) + r.segs;
-    const int tall = ceil_div(r.ranks, 16 * NR);
-    if (pieces * tall * 64 * W >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
-    launch<AdaptRowsArgs>("adapter_rows", adapter_rows<KIND, RT, NR, W>, dim3((unsigned)pieces, tall), dim3(64 * W), st, r);
+    // few pieces: fewer ranks a workgroup (its A comes through one unit's loads)
+    r.per = 16 * NR;
+    while (NR == 1 && r.per > 4 && pieces * ceil_div(r.ranks, r.per) < 128) r.per /= 2;
+    const int tall = ceil_div(r.ranks, r.per);
+    const long long wide = pieces + ceil_div(r.blocks, W);
+    if (wide * tall * 64 * W >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
+    r.pieces = (int)pieces;
+    launch<AdaptRowsArgs>("adapter_rows", adapter_rows<KIND, RT, NR, W>, dim3((unsigned)wide, tall), dim3(64 * W), st, r);
     return check_launch("adapter_rows");
 }
 
 template <GmmKind KIND>
 ts_status run_adapt(const AdaptCall &c) {
+    const AdaptPlan plan = adapt_plan(c.rows, c.rank, c.products, c.w_kn != 0, c.n, c.k, c.dtype, c.odtype);
+    GmmAdaptArgs a;
+    a.tile = plan.tile;
+    a.split = plan.split;
     AdaptRowsArgs r;
     r.x = static_cast<const char *>(c.x);
     for (int i = 0; i < c.products; ++i) r.a[i] = static_cast<const char *>(c.a[i]);
@@ -185,7 +346,11 @@ ts_status run_adapt(const AdaptCall &c) {
     r.offsets = c.offsets;
     r.adapter = c.adapter;
     r.t = static_cast<char *>(c.ws);
-    r.ids = reinterpret_cast<int32_t *>(r.t + adapt_t_bytes(c.rows, c.rank, c.products, c.dtype, c.odtype));
+    r.wr = wave_rows(plan.tile);
+    r.blocks = ceil_div(c.rows, r.wr);
+    r.slots = reinterpret_cast<int32_t *>(r.t + plan.t);
+    r.slot_ad = r.slots + (size_t)r.blocks * r.wr;
+    r.slot_count = r.slot_ad + (size_t)r.blocks * r.wr;
     r.rows = c.rows;
     r.segs = c.segments;
     r.adapters = c.adapters;
@@ -194,12 +359,11 @@ ts_status run_adapt(const AdaptCall &c) {
     r.parts = adapt_parts(c.dtype, c.odtype);
     r.k = c.k;
     ts_status s;
-    if (c.rows < 16LL * c.segments) s = run_rows<KIND, 1, 1, 16>(r, c.stream);
+    if (c.rows < 2048 || c.rows < 16LL * c.segments) s = run_rows<KIND, 1, 1, 16>(r, c.stream);
     else if (r.ranks <= 16) s = run_rows<KIND, 4, 1, 8>(r, c.stream);
-    else s = run_rows<KIND, 4, 4, 4>(r, c.stream);
+    else s = run_rows<KIND, 4, 4, 8>(r, c.stream);
     if (s != TS_OK) return s;
 
-    GmmAdaptArgs a;
     a.x[0] = static_cast<const char *>(c.x);
     for (int i = 0; i < c.products; ++i) {
         a.w[i] = static_cast<const char *>(c.w[i]);
@@ -212,14 +376,22 @@ ts_status run_adapt(const AdaptCall &c) {
     a.out = c.out;
     a.out_f32 = c.odtype == TS_F32;
     a.t = r.t;
-    a.ids = r.ids;
+    a.slots = r.slots;
+    a.slot_ad = r.slot_ad;
+    a.slot_count = r.slot_count;
+    a.sums = reinterpret_cast<float *>(r.t + plan.t + plan.slots);
     a.segs = c.segments;
     a.adapters = c.adapters;
     a.rank = c.rank;
     a.parts = r.parts;
-    if (c.products == 2) return run_fwd<KIND, kDreluAdapt, false>("adapter_drelu", a, c.stream);
-    return c.w_kn ? run_fwd<KIND, kFwdAdapt, true>("adapter_mm", a, c.stream)
-                  : run_fwd<KIND, kFwdAdapt, false>("adapter_mm", a, c.stream);
+    if (c.products == 2) s = run_fwd<KIND, kDreluAdapt, false>("adapter_drelu", a, c.stream);
+    else if (c.w_kn) s = run_fwd<KIND, kFwdAdapt, true>("adapter_mm", a, c.stream);
+    else s = run_fwd<KIND, kFwdAdapt, false>("adapter_mm", a, c.stream);
+    if (s != TS_OK || a.split == 1) return s;
+    const unsigned grid = (unsigned)std::min<long long>(((long long)c.rows * (c.n / 4) + 255) / 256, 256 * 16);
+    launch<GmmAdaptArgs>("adapter_sum", c.products == 2 ? adapter_sum_kernel<true> : adapter_sum_kernel<false>, dim3(grid),
+                         dim3(256), c.stream, a);
+    return check_launch("adapter_sum");
 }
 
 ts_status adapt(const AdaptCall &c) {
@@ -237,7 +409,7 @@ ts_status adapt(const AdaptCall &c) {
         if (!c.w[i] || !c.a[i] || !c.b[i]) return TS_ERR_NULL;
         if (!aligned16(c.w[i]) || !aligned16(c.a[i]) || !aligned16(c.b[i])) return TS_ERR_ALIGN;
     }
-    if (!c.ws || c.ws_bytes < adapt_ws_bytes(c.rows, c.rank, c.products, c.dtype, c.odtype)) return TS_ERR_WORKSPACE;
+    if (!c.ws || c.ws_bytes < adapt_ws_bytes(c.rows, c.rank, c.products, c.w_kn != 0, c.n, c.k, c.dtype, c.odtype)) return TS_ERR_WORKSPACE;
     if (!aligned16(c.ws)) return TS_ERR_ALIGN;
     return c.dtype == TS_BF16 ? run_adapt<kGmmBf16>(c) : run_adapt<kGmmF32>(c);
 }
@@ -248,8 +420,9 @@ ts_status adapt(const AdaptCall &c) {
 
 extern "C" {
 
-size_t ts_adapter_workspace_bytes(int rows, int rank, int products, ts_dtype dtype, ts_dtype odtype) {
-    return ts::adapt_ws_bytes(rows, rank, products, dtype, odtype);
+size_t ts_adapter_workspace_bytes(int rows, int rank, int products, int w_kn, int n, int k, ts_dtype dtype,
+                                  ts_dtype odtype) {
+    return ts::adapt_ws_bytes(rows, rank, products, w_kn != 0, n, k, dtype, odtype);
 }
 
 ts_status ts_adapter_mm(const void *x, const void *w, const void *a, const void *b, const float *scale, ts_dtype dtype,

@@ -329,52 +329,6 @@ __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     }
 }
 
-// Slots of a tile's adapters, by one wave.  Row q of the tile (ids[c], lane l: q =
-// 64 c + l; -1: none) gets the slot of its adapter in slot[q] (-1), the slots'
-// adapters stand in ad[], in the order of their first rows.  Returns how many.
-// Runs of rows with one adapter are looked up one after another: a tile of prompts
-// has few.
-template <int BQ>
-__device__ __forceinline__ int adapter_slots(const int (&ids)[(BQ + 63) / 64], int lane, int *ad, int *slot) {
-    constexpr int NC = (BQ + 63) / 64;
-    int list[NC], n = 0, last_id = -1, last_slot = -1;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) list[c] = -1;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int id = ids[c];
-        int before = __shfl_up(id, 1);
-        if (lane == 0) before = last_id;
-        uint64_t starts = __ballot(id != before && id >= 0);
-        int mine = last_slot;
-        while (starts) {
-            const int at = __builtin_ctzll(starts);
-            starts &= starts - 1;
-            const int want = __builtin_amdgcn_readlane(id, at);
-            int s = -1;
-#pragma unroll
-            for (int d = 0; d < NC; ++d) {
-                const uint64_t same = __ballot(list[d] == want);
-                if (same) s = 64 * d + __builtin_ctzll(same);
-            }
-            if (s < 0) {
-                s = n++;
-#pragma unroll
-                for (int d = 0; d < NC; ++d)
-                    if (s == 64 * d + lane) list[d] = want;
-            }
-            mine = lane >= at ? s : mine;
-        }
-        if (64 * c + lane < BQ) slot[64 * c + lane] = id >= 0 ? mine : -1;
-        last_id = __builtin_amdgcn_readlane(id, 63);
-        last_slot = __builtin_amdgcn_readlane(mine, 63);
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-        if (64 * c + lane < n) ad[64 * c + lane] = list[c];
-    return n;
-}
-
 // LDS of one contraction group of gmm_tiled in 16-byte chunks: the stages of
 // both operands and (fp8) of the scales.
 template <GmmKind KIND, int BP, int BQ, int WP, int WQ, int AR, int BR>
@@ -472,15 +426,21 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
         }
     }
     const int p0 = pt * PT;
-    // (asked for here, needed behind the product)
-    [[maybe_unused]] int ids[(BQ + 63) / 64];
-    if constexpr (is_adapt(MODE)) {
+    // Adapters, of this wave's columns: their rows' slots, the slots' adapters (lane s:
+    // slot s's), how many (asked for here, needed behind the product).
+    constexpr bool ADAPT = is_adapt(MODE);
+    [[maybe_unused]] int slot_q[MJ], ad = 0, slots = 0;
+    [[maybe_unused]] int part = 0, KWS = KW;  // steps from one of this group's to its next
+    if constexpr (ADAPT) {
+        constexpr int WR = MJ * 16;
+        const int blk = (q0 - b) / WR + wq;
+        const bool have = q0 + wq * WR < q_end;
 #pragma unroll
-        for (int c = 0; c < (BQ + 63) / 64; ++c) {
-            const int q = 64 * c + lane;
-            const int id = a.ids[min(q0 + q, q_end - 1)];
-            ids[c] = q < BQ && q0 + q < q_end && id >= 0 && id < a.adapters ? id : -1;
-        }
+        for (int j = 0; j < MJ; ++j) slot_q[j] = have ? a.slots[(size_t)blk * WR + j * 16 + lm] : -1;
+        ad = have ? a.slot_ad[(size_t)blk * WR + min(lane, WR - 1)] : 0;
+        slots = have ? a.slot_count[blk] : 0;
+        part = blockIdx.y;
+        KWS = KW * gridDim.y;
     }
     // contraction: k, or the group's rows, in blocks of KS
     const int C = MODE == kGradW ? e - b : a.k;
@@ -731,7 +691,8 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
                          lds_b + (uint32_t)((BR == 1 ? 0 : to) * TB::CHUNKS + THREADS * j) * 16);
         };
 
-        if (kg == 0) {
+        [[maybe_unused]] const int kgs = ADAPT ? part * KW + kg : kg;
+        if (ADAPT ? kgs == 0 : kg == 0) {
             ask(last);
             take();
             const int left = C - last * KS;
@@ -772,9 +733,12 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
         // other operand) and t + AR - 1 (the P operand) into the stages that
         // step t - 1 read.  The last steps have none to load and load the last
         // whole block again: no branch between the matrix instructions.
-        auto block = [&](int t) { return max(min(kg + t * KW - 1, last - 1), 0); };
-        if constexpr (KW > 1)
-            if (kg > 0) {
+        auto block = [&](int t) {
+            if constexpr (ADAPT) return max(min(kgs + t * KWS - 1, last - 1), 0);
+            else return max(min(kg + t * KW - 1, last - 1), 0);
+        };
+        if constexpr (KW > 1 || ADAPT)
+            if (ADAPT ? kgs > 0 : kg > 0) {
                 unroll<LOADS_B>([&](auto j) { load_b(j, block(0), 0); });
                 unroll<LOADS_A>([&](auto j) { load_a(j, block(0), 0); });
             }
@@ -791,7 +755,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
             take();
         }
         int ar = 0, br = 0;  // stages of step t
-        for (int t = 0; t * KW <= last; ++t) {
+        for (int t = 0; ADAPT ? part * KW + t * KWS <= last : t * KW <= last; ++t) {
             // what may be on its way: all that was asked for behind this step's
             gmm_barrier<(AR == LB ? (LB - 2) * LOADS : (LB - 2) * LOADS + LOADS_A)>();
             const int blk_a = block(t + AR - 1), blk_b = block(t + LB - 1);
@@ -809,7 +773,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
                 wnext[0] = wsbase[0][block(t + 1)];
                 wnext[1] = wsbase[1][block(t + 1)];
             }
-            if (KW == 1 || kg + t * KW <= last)
+            if (ADAPT ? kgs + t * KWS <= last : KW == 1 || kg + t * KW <= last)
                 contract(s_a + ar * TA::CHUNKS, s_b + br * TB::CHUNKS,
                          s_s + (AHEAD8 ? (u >> 3 & 1) * BQ * 8 : br * SS), wscale, [&](auto gi) {
                     // (in the earlier half of the groups, the later half covers
@@ -836,95 +800,102 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
         }
         gmm_barrier<0>();
     }
-    if constexpr (is_adapt(MODE)) {
-        // Rows' adapters, as a contraction over the ranks of all adapters that the
-        // tile has, one after another: a row's t stands at its own adapter's ranks,
-        // zeros at the others', so the bytes are those of the adapters' B and a
-        // tile of single-token requests takes as few steps as their ranks fill.
-        int *tab;
-        if constexpr (AR >= 3) {
-            tab = reinterpret_cast<int *>(s_all + (AR - 1) * TA::CHUNKS);  // (two stages are used below)
-        } else {
-            __shared__ int own[2 * BQ + 1];
-            tab = own;
-        }
-        int *const ad = tab, *const slot = tab + BQ;
-        if (threadIdx.x < 64) {
-            const int n = adapter_slots<BQ>(ids, lane, ad, slot);
-            if (lane == 0) tab[2 * BQ] = n;
-        }
-        __syncthreads();
-        const int r2 = DRELU ? 2 * a.rank : a.rank, per = r2 * a.parts;  // ranks of a slot
-        const int all = __builtin_amdgcn_readfirstlane(tab[2 * BQ]) * per, steps = (all + KS - 1) / KS;
-        const bool second = DRELU && (((wave * (64 / TA::CR)) >> 4) & 1);
-        const char *const bbase = second ? a.b[1] : a.b[0];
-        const uint32_t lds_a = lds_addr(s_a) + wave * 1024, lds_b = lds_a + AR * TA::CHUNKS * 16;
-        auto load = [&](int step, int to) {
-            unroll<TB::NJ>([&](auto j) {
-                int row, ch;
-                TB::at(tid + THREADS * j, row, ch);
-                const int v = step * KS + ch * (16 / SZ), s = v / per;
-                const char *p = slot[row] == s ? a.t + ((size_t)(q0 + row) * per + (v - s * per)) * SZ : zero;
-                ld_lds16(p, lds_b + (uint32_t)(to * TB::CHUNKS + THREADS * j) * 16);
-            });
-            unroll<TA::NJ>([&](auto j) {
-                int row, ch;
-                TA::at(tid + THREADS * j, row, ch);
-                const int v = step * KS + (ACOL ? row : ch * (16 / SZ)), s = v / per;
-                int r = v - s * per;
-                if (r >= r2) r -= r2;  // (a part's lower half meets the same B)
-                const char *p = zero;
-                if (v < all) {
-                    const size_t m = ad[s];
-                    if constexpr (ACOL) {
-                        p = bbase + (m * a.rank + r) * ((size_t)a.n * SZ) + min(p0 * SZ + ch * 16, a.n * SZ - 16);
-                    } else if (DRELU) {
-                        const int n = min(p0 + (row >> 5) * 16 + (row & 15), a.n - 1);
-                        if ((r >= a.rank) == second) p = bbase + ((m * a.n + n) * a.rank + (r - (second ? a.rank : 0))) * SZ;
-                    } else {
-                        p = bbase + ((m * a.n + min(p0 + row, a.n - 1)) * a.rank + r) * SZ;
+    if constexpr (ADAPT) {
+        // The contraction goes on over the ranks of all adapters that the wave's rows
+        // have, one after another, 64 bytes a step.  A row's t stands at its own
+        // adapter's ranks, zeros at the others'.  Operands come straight into
+        // registers, several steps' together: no other wave's loads are waited for, and a
+        // wave takes what its own rows need.  (Through LDS with all of the workgroup, two
+        // stages: 8 rounds of loads for 32 requests of rank 16, and for prompts
+        // each wave takes the steps of its neighbours' adapters too: gate + up 58 us, 6001
+        // rows 1390 to 1420.)
+        constexpr int both = DRELU ? 2 : 1, CE = 16 / SZ, CK = 64 / SZ;
+        constexpr int REGS = (MI + both * MJ) * 4, LEFT = 176 - MI * MJ * 4, U = LEFT >= 4 * REGS ? 4 : LEFT >= 2 * REGS ? 2 : 1;
+        const int per = a.rank * a.parts, all = __builtin_amdgcn_readfirstlane(slots) * per;
+        const size_t stride = (size_t)both * per;
+        // [ranks][columns] matrices go through a part of LDS of this wave's own, for
+        // the transposing reads
+        using TW = GmmTile<KIND, true, MI * 16, 64>;
+        static_assert(!ACOL || (WP * WQ * KW * U * TW::CHUNKS <= 2 * KW * ALL), "half a step a wave");
+        [[maybe_unused]] const int widx = kg * (WP * WQ) + wave;
+        for (int s0 = (part * KW + kg) * U; s0 * CK < all; s0 += KWS * U) {
+            u32x4 af[U][MI], bf[both][U][MJ];
+            int f0[U], f1[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int w0 = (s0 + u) * CK, v = w0 + lq * CE, own = v / per, rv = v - own * per;
+                const bool in = v < all;
+                f0[u] = w0 / per;
+                f1[u] = (w0 + CK - 1) / per;
+#pragma unroll
+                for (int h = 0; h < both; ++h)
+#pragma unroll
+                    for (int j = 0; j < MJ; ++j) {
+                        const char *p = a.t + ((size_t)(q0 + (wq * MJ + j) * 16 + lm) * stride + h * per + rv) * SZ;
+                        bf[h][u][j] = ld_cached(in && slot_q[j] == own ? p : zero);
+                    }
+                if constexpr (!ACOL) {
+                    const int m = __shfl(ad, in ? own : 0), r = rv >= a.rank ? rv - a.rank : rv;  // (parts: the same B)
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) {
+                        const int n = min(p0 + (wp * MI + i) / both * 16 + lm, a.n - 1);
+                        const char *p = a.b[i % both] + (((size_t)m * a.n + n) * a.rank + r) * SZ;
+                        af[u][i] = ld_cached(in ? p : zero);
                     }
                 }
-                ld_lds16(p, lds_a + (uint32_t)(to * TA::CHUNKS + THREADS * j) * 16);
-            });
-        };
-        if (kg < steps) load(kg, 0);
-        for (int i = 0; i * KW < steps; ++i) {
-            gmm_barrier<0>();
-            const int step = kg + i * KW;
-            if (step + KW < steps) load(step + KW, (i + 1) & 1);
-            if (step >= steps) continue;
-            const u32x4 *const A = s_a + (i & 1) * TA::CHUNKS, *const B = s_b + (i & 1) * TB::CHUNKS;
+            }
+            if constexpr (ACOL) {
+                // U sub-steps of 64 bytes of contraction each
+                char *const own_lds = reinterpret_cast<char *>(s_all) + (size_t)widx * (U * TW::CHUNKS / 2) * 16;
+                const uint32_t l = lds_addr(own_lds);
+                const int pc = (p0 + wp * MI * 16) * SZ;
+                unroll<U * TW::NJ / 2>([&](auto j) {
+                    int row, ch;
+                    TW::at(lane + 64 * j, row, ch);
+                    const int v = s0 * CK + row, own = v / per, rv = v - own * per;
+                    const int m = __shfl(ad, v < all ? own : 0), r = rv >= a.rank ? rv - a.rank : rv;
+                    const char *p = a.b[0] + ((size_t)m * a.rank + r) * ((size_t)a.n * SZ) + min(pc + ch * 16, a.n * SZ - 16);
+                    ld_lds16(v < all ? p : zero, l + 1024 * j);
+                });
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-            for (int s = 0; s < RB / 64; ++s) {
-                u32x4 bf[MJ];
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int j = 0; j < MJ; ++j) bf[j] = TB::frag(B, wq * MJ + j, s, lane);
+                    for (int i = 0; i < MI; ++i)
+                        af[u][i] = TW::frag(reinterpret_cast<const u32x4 *>(own_lds), i, u, lane);
+                // (the next round's loads may overwrite them)
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
 #pragma unroll
-                for (int m = 0; m < MI; ++m) {
-                    u32x4 af = TA::frag(A, wp * MI + m, s, lane);
-                    if (__any(not_finite<KIND>(af))) {
-                        // An adapter's infinities and NaN concern its own rows: 0 x
-                        // inf of the others is left out, 16 bytes of ranks at a time.
-                        const u32x4 bad = only_finite<KIND, true>(af);
+            for (int u = 0; u < U; ++u) {
+                bool use[MJ];  // columns with a row of these ranks
+#pragma unroll
+                for (int j = 0; j < MJ; ++j) use[j] = __any(slot_q[j] >= f0[u] && slot_q[j] <= f1[u]);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    if (__any(not_finite<KIND>(af[u][i]))) {
+                        // An adapter's infinities and NaN concern its own rows: 0 x inf of
+                        // the others is left out, 16 bytes of ranks at a time.
+                        const u32x4 bad = only_finite<KIND, true>(af[u][i]);
                         for (int h = 0; h < 4; ++h) {
                             const u32x4 one = lq == h ? bad : u32x4{0u, 0u, 0u, 0u};
                             if (!__any(not_finite<KIND>(one))) continue;
-                            const int own = (step * KS + s * (64 / SZ) + h * (16 / SZ)) / per;
+                            const int own = ((s0 + u) * CK + h * CE) / per;
 #pragma unroll
                             for (int j = 0; j < MJ; ++j) {
-                                const f32x4 d = mma<KIND>(one, bf[j], f32x4{0.f, 0.f, 0.f, 0.f});
-                                if (slot[(wq * MJ + j) * 16 + lm] == own) acc[m][j] += d;
+                                const f32x4 d = mma<KIND>(one, bf[i % both][u][j], f32x4{0.f, 0.f, 0.f, 0.f});
+                                if (slot_q[j] == own) acc[i][j] += d;
                             }
                         }
-                        af = only_finite<KIND, false>(af);
+                        af[u][i] = only_finite<KIND, false>(af[u][i]);
                     }
 #pragma unroll
-                    for (int j = 0; j < MJ; ++j) acc[m][j] = mma<KIND>(af, bf[j], acc[m][j]);
+                    for (int j = 0; j < MJ; ++j)
+                        if (use[j]) acc[i][j] = mma<KIND>(af[u][i], bf[i % both][u][j], acc[i][j]);
                 }
             }
         }
-        gmm_barrier<0>();
+        if constexpr (KW > 1 && ACOL) __syncthreads();  // (the sums go where other waves' matrices are)
     }
     if constexpr (KW > 1) {
         static_assert((KW - 1) * BP * BQ / 4 <= KW * ALL, "the groups' sums fit the stages");
@@ -950,6 +921,19 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
     for (int j = 0; j < MJ; ++j) {
         const int q = q0 + (wq * MJ + j) * 16 + lm;
         if (q >= q_end) continue;
+        if constexpr (ADAPT) {
+            if (gridDim.y > 1) {
+                // this part's sums, added up by a launch of their own
+                constexpr int both = DRELU ? 2 : 1;
+                float *const sums = a.sums + ((size_t)part * a.rows + q) * both * a.n;
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    const int p = p0 + (wp * MI + i) / both * 16 + 4 * lq;
+                    if (p < a.n) store4(sums, 1, (size_t)(i % both) * a.n + p, acc[i][j]);
+                }
+                continue;
+            }
+        }
         if constexpr (DRELU) {
 #pragma unroll
             for (int i = 0; i < MI; i += 2) {
@@ -1040,12 +1024,15 @@ constexpr bool gmm_in_table() {
 }
 
 // Launches it; a grid beyond the runtime's 2^32 threads is refused.
+inline unsigned gmm_split(const GmmArgs &) { return 1; }
+inline unsigned gmm_split(const GmmAdaptArgs &a) { return (unsigned)a.split; }
+
 template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int AR, int BR, int KW = 1, bool WIDE = false>
 ts_status run_tiled(const char *name, const typename GmmArgsOf<MODE>::type &a, hipStream_t st) {
     static_assert(MODE == kGradW || WIDE || gmm_in_table<KIND, BP, BQ, WP, WQ, AR, BR, KW>(), "the tile's line in kTileSize");
     const long long grid = gmm_grid<MODE, BP, BQ>(a);
-    if (grid * (64 * WP * WQ * KW) >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
-    launch<typename GmmArgsOf<MODE>::type>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, AR, BR, KW, WIDE>, dim3((unsigned)grid),
+    if (grid * gmm_split(a) * (64 * WP * WQ * KW) >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
+    launch<typename GmmArgsOf<MODE>::type>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, AR, BR, KW, WIDE>, dim3((unsigned)grid, gmm_split(a)),
                     dim3(64 * WP * WQ * KW), st, a);
     return check_launch(name);
 }
@@ -1062,7 +1049,10 @@ inline bool gmm_wide(const GmmArgs &a) {
 template <GmmKind KIND, GmmMode MODE, bool ACOL>
 ts_status run_fwd(const char *name, const typename GmmArgsOf<MODE>::type &a, hipStream_t st) {
     if (gmm_wide<KIND>(a)) return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2, 1, true>(name, a, st);
-    switch (pick_tile(KIND, is_drelu(MODE), a.groups, a.rows, a.n, a.k)) {
+    GmmTileId tile;
+    if constexpr (is_adapt(MODE)) tile = a.tile;
+    else tile = pick_tile(KIND, is_drelu(MODE), a.groups, a.rows, a.n, a.k);
+    switch (tile) {
         case kTile64x32: return run_tiled<KIND, MODE, ACOL, 64, 32, 2, 2, 3, 3, 2>(name, a, st);
         case kTile64x64:
             if constexpr (KIND != kGmmF32) return run_tiled<KIND, MODE, ACOL, 64, 64, 2, 2, 4, 4, 2>(name, a, st);
@@ -1071,7 +1061,9 @@ ts_status run_fwd(const char *name, const typename GmmArgsOf<MODE>::type &a, hip
             if constexpr (!is_drelu(MODE)) return run_tiled<KIND, MODE, ACOL, 32, 32, 2, 2, 3, 3, 3>(name, a, st);
             break;
         case kTile128x64: return run_tiled<KIND, MODE, ACOL, 128, 64, 4, 1, 3, 3>(name, a, st);
-        case kTile128x128: return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2>(name, a, st);
+        case kTile128x128:
+            if constexpr (!(is_adapt(MODE) && KIND == kGmmBf16)) return run_tiled<KIND, MODE, ACOL, 128, 128, 2, 2, 2, 2>(name, a, st);
+            break;
         case kTile256x128:
             if constexpr (KIND != kGmmF32) return run_tiled<KIND, MODE, ACOL, 256, 128, 4, 2, 3, 3>(name, a, st);
             break;

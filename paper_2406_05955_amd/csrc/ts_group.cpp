@@ -120,4 +120,56 @@ GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k
     return best;
 }
 
+// The same for a product with adapters, whose contraction may be split over up to 16
+// workgroups a tile (their sums cost a launch, 14000 cycles, and their bytes twice).
+// The matrix's bytes come on top of the tiles' time, as the root of the squares'
+// sum: with few rows both count.  Rows of [k][n] that a tile cuts below 128 bytes
+// are fetched twice.  The constants are those of the least mean over 131 sizes (both
+// layouts and dReLU, 1 to 6000 rows, 512 x 1792 to 4096 x 14336) timed at every tile and
+// split: 2% above each size's best, 23% at most.  Us, one workgroup a tile / this:
+// [k][n] 4096 x 14336 1 row 35 / 25, 64 rows 53 / 35, 300 rows 103 / 58; [n][k] 2048 x
+// 8192 32 rows 23 / 16; fp32 512 x 1792 1 row 14 / 11.
+void adapt_tile(GmmKind kind, bool drelu, bool w_kn, int rows, int n, int k, GmmTileId *tile, int *split) {
+    const int esz = kind == kGmmF32 ? 4 : 2, both = drelu ? 2 : 1;
+    const double bytes = (double)n * k * esz * both / 2600;
+    double least = 0.0;
+    *tile = kTile128x64;
+    *split = 1;
+    for (int i = 0; i < kTiles; ++i) {
+        const GmmTileSize &t = kTileSize[i];
+        if (kind == kGmmF32 && (t.p == 256 || i == kTile64x64)) continue;
+        if (drelu && i == kTile32x32) continue;
+        // (bf16: with the adapters' registers one workgroup a unit, and never the best)
+        if (kind == kGmmBf16 && i == kTile128x128) continue;
+        const int all = ceil_div(k * esz, 128);
+        // (of large outputs no sums: 64 MB of workspace at most)
+        const double sums = (double)rows * n * both * 4;
+        for (int s = 1; s <= 16 && (s == 1 || (all / s >= 4 && s * sums <= 64 << 20)); s *= 2) {
+            const double tiles = (double)ceil_div(n, drelu ? t.p / 2 : t.p) * ceil_div(rows, t.q) * s;
+            const double steps = ceil_div(all, s);
+            const double matrix = (double)t.p * t.q / (kind == kGmmF32 ? 2.0 : 18.0);
+            const int p = w_kn && t.p * esz < 128 ? 2 * t.p : t.p;
+            const double step = std::max(matrix, (p + t.q) * 128 / 24.0);
+            const double trip = 2500.0 / (t.stages - 1) / t.kw, start = 1000.0 * (t.kw + 1);
+            double cycles;
+            if (kind == kGmmF32) {
+                const double each = tiles / 256 < 8 ? std::ceil(tiles / 256) : tiles / 256 + 0.5;
+                const double together = std::min<double>(t.per_unit, each);
+                cycles = each * (steps * std::max(step + 100, trip / together) + start / together);
+            } else {
+                const double together = std::min<double>(t.per_unit, std::max(1.0, tiles / 256));
+                const double r = tiles / (256.0 * t.per_unit);
+                cycles = (r < 4 ? std::ceil(r) : r + 0.5) * (steps * std::max(together * step, trip) + start);
+            }
+            cycles = std::sqrt(cycles * cycles + bytes * bytes);
+            if (s > 1) cycles += 14000 + 400 * s + s * sums * 2 / 2500;
+            if (least == 0.0 || cycles < least) {
+                least = cycles;
+                *tile = (GmmTileId)i;
+                *split = s;
+            }
+        }
+    }
+}
+
 }  // namespace ts

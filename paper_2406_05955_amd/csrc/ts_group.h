@@ -45,14 +45,6 @@ struct GmmKeepArgs : GmmArgs {
     uint8_t *exps = nullptr;   // [rows][ceil(n / 16)][2]
 };
 
-// Adapters beside one group's product (ts_adapt.hip).  offsets: the segments'.
-struct GmmAdaptArgs : GmmArgs {
-    const char *t = nullptr;            // [rows][parts][gate's ranks, up's]: scale x A^T, from adapter_rows
-    const int32_t *ids = nullptr;       // [rows]: a row's adapter
-    const char *b[2] = {nullptr, nullptr};
-    int segs = 0, adapters = 0, rank = 0, parts = 1;
-};
-
 // Tiles of the forward products: columns (dReLU: of gate and up together) x
 // rows, workgroups of it that a compute unit holds, stages, contraction groups.
 // (equal costs: the first)
@@ -67,6 +59,20 @@ constexpr GmmTileSize kTileSize[kTiles] = {{256, 256, 1, 2, 1}, {128, 128, 2, 2,
 constexpr int tiles_per_unit(GmmKind kind, int t) {
     return kind == kGmmFp8 && t == kTile32x32 ? 1 : kTileSize[t].per_unit;
 }
+// Adapters beside one group's product (ts_adapt.hip).  offsets: the segments'.
+// Of the rows of each wave of the product: the rows' slots (-1: no adapter), the
+// slots' adapters, how many slots.
+struct GmmAdaptArgs : GmmArgs {
+    const char *t = nullptr;  // [rows][gate, up][parts][rank]: scale x A^T
+    const int32_t *slots = nullptr, *slot_ad = nullptr, *slot_count = nullptr;
+    const char *b[2] = {nullptr, nullptr};
+    float *sums = nullptr;    // [split][rows][gate, up][n]
+    int segs = 0, adapters = 0, rank = 0, parts = 1, split = 1;
+    GmmTileId tile = kTile128x64;
+};
+// Rows of a wave of each tile.
+constexpr int wave_rows(GmmTileId t) { return t == kTile64x32 || t == kTile32x32 ? 16 : t == kTile64x64 ? 32 : 64; }
+void adapt_tile(GmmKind kind, bool drelu, bool w_kn, int rows, int n, int k, GmmTileId *tile, int *split);
 GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k);
 
 ts_status check_group_dims(int rows, int groups, int n, int k, int quantum);

@@ -5,10 +5,12 @@ import torch
 import group_util as ref
 from group_util import BF16, D, F32
 
-# (rows, n) that take every tile at this contraction, for one product and for gate + up
-TILE_K = 336
-TILES = [(1, 144), (41, 4112), (41, 6160), (41, 8208), (300, 1552), (700, 1040), (100, 8208), (300, 8208), (700, 6160),
-         (1000, 2064), (2500, 1552), (2500, 6160), (700, 8208), (1000, 6160), (1000, 8208), (2000, 4112)]
+# (rows, n, k) that between them take every tile of both types and modes, with the
+# contraction in one workgroup and shared by several
+TILES = [(1, 144, 136), (1, 144, 2056), (1500, 528, 136), (1500, 1040, 136), (1, 144, 4104), (200, 144, 4104),
+         (1500, 4112, 136), (2500, 144, 136), (300, 144, 4104), (130, 528, 4104), (1000, 8208, 136), (200, 528, 4104),
+         (700, 2064, 4104), (200, 1040, 4104), (700, 4112, 4104), (700, 1040, 4104), (1000, 1040, 4104), (500, 2064, 8192),
+         (500, 4112, 8192), (1700, 528, 28672), (1700, 1040, 28672)]
 
 
 def segments(rows, S, N, gen, lead=0, tail=0):
@@ -41,29 +43,32 @@ def adapted(x, w, a, b, offsets, adapter, scale, w_kn, parts):
     y, mag = x @ w, x.abs() @ w.abs()
     extra = torch.zeros_like(y)
     N, rank = a.shape[:2]
+    of_row = torch.full((R,), -1, dtype=torch.int64)
     for s, p, q in ref.spans(offsets):
-        i = int(adapter[s])
-        if q <= p or not 0 <= i < N:
+        of_row[p:q] = int(adapter[s])
+    for i in range(N):
+        at = (of_row == i).nonzero()[:, 0].to(x.device)
+        if not at.numel():
             continue
         f = float(scale[i]) if scale is not None else 1.0
-        t = f * (x[p:q] @ a[i].t())
-        e = abs(f) * ref.sum_bound(x[p:q].abs() @ a[i].abs().t(), k) + 2.0 ** -24 * t.abs()
+        t = f * (x[at] @ a[i].t())
+        e = abs(f) * ref.sum_bound(x[at].abs() @ a[i].abs().t(), k) + 2.0 ** -24 * t.abs()
         if parts:
             e = e + ref.half_step(BF16) ** parts * (t.abs() + e)
-        y[p:q] += t @ b[i]
-        mag[p:q] += (t.abs() + e) @ b[i].abs()
-        extra[p:q] = e @ b[i].abs()
+        y[at] += t @ b[i]
+        mag[at] += (t.abs() + e) @ b[i].abs()
+        extra[at] = e @ b[i].abs()
     return y, extra + ref.sum_bound(mag, k + 2 * rank)
 
 
 def case(rows, S, N, rank, n, k, dtype, w_kn, g, products=1, lead=0, tail=0, scaled=True):
-    off, ad = segments(rows, S, N, g, lead, tail)
-    x = torch.randn(rows, k, generator=g).to(dtype)
-    scale = torch.rand(N, generator=g) + 0.5 if scaled else None
-    mats = []
-    for _ in range(products):
-        w = torch.randn(*((k, n) if w_kn else (n, k)), generator=g) * k ** -0.5
-        a = torch.randn(N, rank, k, generator=g) * k ** -0.5
-        b = torch.randn(N, *((rank, n) if w_kn else (n, rank)), generator=g) * rank ** -0.5
-        mats.append([m.to(dtype) for m in (w, a, b)])
+    """x, the products' (w, a, b), offsets, adapters, scales; matrices on g's device."""
+    off, ad = segments(rows, S, N, torch.Generator().manual_seed(g.initial_seed() % 2 ** 31 + products), lead, tail)
+
+    def draw(*shape, scale=1.0):
+        return (torch.randn(*shape, generator=g, device=g.device) * scale).to(dtype)
+    x = draw(rows, k)
+    scale = torch.rand(N, generator=g, device=g.device).cpu() + 0.5 if scaled else None
+    mats = [(draw(*((k, n) if w_kn else (n, k)), scale=k ** -0.5), draw(N, rank, k, scale=k ** -0.5),
+             draw(N, *((rank, n) if w_kn else (n, rank)), scale=rank ** -0.5)) for _ in range(products)]
     return x, mats, off, ad, scale

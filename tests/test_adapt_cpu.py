@@ -1,5 +1,6 @@
 """Adapters beside a projection: what the host refuses, workspace sizes, the
 tiles that the GPU tests reach."""
+import os
 import subprocess
 
 import pytest
@@ -7,7 +8,6 @@ import torch
 
 import adapt_util as ref
 from paper_2406_05955_amd import binding as ts
-from test_group_cpu import build_check
 
 OK, NULL, SHAPE, DTYPE, ALIGN, WS, HIP, UNSUP = range(8)
 A = 0x10000
@@ -44,14 +44,16 @@ def test_refusals_of_up():
 
 
 def test_workspace():
-    size = ts.lib.ts_adapter_workspace_bytes
-    one = size(100, 16, 1, 1, 1)
+    size = lambda *a: ts.lib.ts_adapter_workspace_bytes(*a)  # noqa: E731
+    one = size(100, 16, 1, 0, 64, 64, 1, 1)
     assert one >= 100 * 16 * 2 + 400
-    assert size(100, 16, 2, 1, 1) >= one + 100 * 16 * 2 - 256 and size(100, 16, 1, 1, 0) == size(100, 16, 2, 1, 1)
-    assert size(100, 16, 1, 0, 0) >= 100 * 16 * 4 + 400
-    for bad in ((100, 16, 3, 1, 1), (100, 12, 1, 1, 1), (-1, 16, 1, 1, 1), (100, 16, 1, 2, 1), (100, 132, 1, 0, 0)):
+    assert size(100, 16, 2, 0, 64, 64, 1, 1) >= one + 100 * 16 * 2 - 256
+    assert size(100, 16, 1, 0, 64, 64, 1, 0) == size(100, 16, 2, 0, 64, 64, 1, 1)
+    assert size(100, 16, 1, 0, 64, 64, 0, 0) >= 100 * 16 * 4 + 400
+    for bad in ((100, 16, 3, 0, 64, 64, 1, 1), (100, 12, 1, 0, 64, 64, 1, 1), (-1, 16, 1, 0, 64, 64, 1, 1), (100, 16, 1, 0, 64, 64, 2, 1),
+                (100, 132, 1, 0, 64, 64, 0, 0), (100, 16, 1, 0, 60, 64, 1, 1), (100, 16, 1, 0, 64, 0, 1, 1)):
         assert size(*bad) == 0
-    assert _mm(wsb=size(10, 16, 1, 1, 1) - 1) == WS and _mm(odt=0, wsb=size(10, 16, 1, 1, 1)) == WS
+    assert _mm(wsb=size(10, 16, 1, 0, 64, 64, 1, 1) - 1) == WS and _mm(odt=0, wsb=size(10, 16, 1, 0, 64, 64, 1, 1)) == WS
 
 
 def test_binding_refuses_tensors():
@@ -76,11 +78,28 @@ def test_binding_refuses_tensors():
         ts.adapter_drelu(x, w, w, a, b, a, b[:, :16], off, ad)
 
 
+def build_tile_check(tmp_path):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    csrc, exe = os.path.join(root, "paper_2406_05955_amd", "csrc"), tmp_path / "adapt_tile_check"
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(root, "include"), "-I", csrc,
+                    os.path.join(root, "tests", "native", "adapt_tile_check.cpp"), os.path.join(csrc, "ts_group.cpp"),
+                    os.path.join(csrc, "ts_plan.cpp"), "-o", str(exe)], check=True)
+    return str(exe)
+
+
+def test_tile_choice(tmp_path):
+    r = subprocess.run([build_tile_check(tmp_path)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
 def test_the_gpu_tests_reach_every_tile(tmp_path):
-    exe = build_check(tmp_path, "-O2")
+    """Every tile that can be chosen, with the contraction in one workgroup and shared."""
+    exe = build_tile_check(tmp_path)
     for kind in (0, 1):
-        for drelu in (0, 1):
-            lines = "\n".join(f"{kind} {drelu} 1 {rows} {n} {ref.TILE_K}" for rows, n in ref.TILES)
-            r = subprocess.run([str(exe), "-"], input=lines, capture_output=True, text=True, check=True)
-            want = ({1, 2, 3} if kind else set(range(6))) | (set() if drelu else {6})
-            assert set(map(int, r.stdout.split())) == want, (kind, drelu)
+        for drelu, w_kn in ((0, 0), (0, 1), (1, 0)):
+            lines = "\n".join(f"{kind} {drelu} {w_kn} {rows} {n} {k}" for rows, n, k in ref.TILES)
+            r = subprocess.run([exe, "-"], input=lines, capture_output=True, text=True, check=True)
+            got = {(int(t), int(s) > 1) for t, s in (line.split() for line in r.stdout.splitlines())}
+            tiles = {1, 2, 3, 6} if kind else {0, 2, 3, 4, 5, 6}
+            want = {(t, s) for t in tiles - ({6} if drelu else set()) for s in (False, True)}
+            assert want <= got, (kind, drelu, w_kn, want - got)

@@ -63,15 +63,15 @@ def test_drelu(rows, S, N, rank, n, k, dtype):
         check(*ref.case(rows, S, N, rank, n, k, dtype, False, g, products=2, scaled=scaled), False, odt)
 
 
-@pytest.mark.parametrize("rows,n", ref.TILES)
+@pytest.mark.parametrize("rows,n,k", ref.TILES)
 @pytest.mark.parametrize("dtype", [BF16, F32])
-def test_every_tile(rows, n, dtype):
+def test_every_tile(rows, n, k, dtype):
     """Every tile, with a segment a row and with ragged ones."""
-    g = gen(82, rows, n)
+    g = torch.Generator(device=DEV).manual_seed(82)
     for S, rank in ((rows, 16), (max(rows // 60, 1), 24)):
         for w_kn in (False, True):
-            check(*ref.case(rows, S, 50, rank, n, ref.TILE_K, dtype, w_kn, g), w_kn, dtype)
-        check(*ref.case(rows, S, 50, rank, n, ref.TILE_K, dtype, False, g, products=2), False, dtype)
+            check(*ref.case(rows, S, 9, rank, n, k, dtype, w_kn, g), w_kn, dtype)
+        check(*ref.case(rows, S, 9, rank, n, k, dtype, False, g, products=2), False, dtype)
 
 
 @pytest.mark.parametrize("products", [1, 2])
