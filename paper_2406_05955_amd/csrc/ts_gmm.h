@@ -274,6 +274,22 @@ __device__ __forceinline__ void store4(void *out, int f32, size_t i, f32x4 v) {
     }
 }
 
+// V (4 or 8) consecutive outputs.
+template <int V>
+__device__ __forceinline__ void store_v(void *out, int f32, size_t i, const float (&y)[V]) {
+    if (V == 4 || f32) {
+#pragma unroll
+        for (int v = 0; v < V; v += 4) store4(out, f32, i + v, f32x4{y[v], y[v + 1], y[v + 2], y[v + 3]});
+    } else {
+        typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
+        typedef float f32x8 __attribute__((ext_vector_type(8)));
+        f32x8 t;
+#pragma unroll
+        for (int v = 0; v < V; ++v) t[v % 8] = y[v];
+        *reinterpret_cast<b16x8 *>(static_cast<__bf16 *>(out) + i) = __builtin_convertvector(t, b16x8);
+    }
+}
+
 // dReLU of a gate and an up projection (strict comparisons: a NaN closes).
 __device__ __forceinline__ float drelu1(float g, float u) { return g > 0.f && u > 0.f ? g * u : 0.f; }
 
@@ -915,6 +931,105 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
                 for (int j = 0; j < MJ; ++j) acc[i][j] += red[(h * MI * MJ + i * MJ + j) * THREADS + tid];
     }
 
+    if constexpr (MODE == kDreluPack || MODE == kDreluGrad) {
+        // Two to four bytes of each tensor an element, four tensors: through LDS, 16 rows
+        // of a wave's at a time, so that a lane has V neighbouring columns and a row's
+        // are whole lines.  (From the lanes that hold the sums, 8 bytes a lane: gate + up
+        // of 8192 rows 1780 us, the gradient of 6002 rows 860.)
+        constexpr int V = KIND == kGmmBf16 ? 8 : 4, H = DRELU ? 2 : 1, PW = MI * 16 / H, LPR = PW / V;
+        constexpr int RPP = 64 / LPR < 16 ? 64 / LPR : 16, NP = 16 / RPP, STR = H * PW + 4;
+        static_assert((KW - 1) * BP * BQ * 4 + WP * WQ * 16 * STR * 4 <= KW * ALL * 16, "16 rows a wave fit the stages");
+        float *const sc = reinterpret_cast<float *>(s_all + (KW - 1) * BP * BQ / 4) + wave * 16 * STR;
+        const int r = lane / LPR, c = lane % LPR * V, p = p0 + wp * PW + c, nb = ceil_div(a.n, kKeepBlock);
+        const bool in = p < a.n && r < 16;
+        // (gradient) the next 16 rows' codes
+        [[maybe_unused]] uint2 kc[NP][V / 4];
+        [[maybe_unused]] uint32_t ke[NP];
+        [[maybe_unused]] auto fetch = [&](int j) {
+            if constexpr (MODE == kDreluGrad)
+#pragma unroll
+                for (int h = 0; h < NP; ++h) {
+                    const int q = q0 + (wq * MJ + j) * 16 + h * RPP + r;
+                    const bool have = in && q < q_end;
+                    const size_t at = (size_t)(have ? q : q0) * a.n + (have ? p : 0);
+                    if constexpr (V == 8) {
+                        const u32x4 v = ld_stream(a.codes + 2 * at);
+                        kc[h][0] = uint2{v.x, v.y};
+                        kc[h][1] = uint2{v.z, v.w};
+                    } else {
+                        kc[h][0] = *reinterpret_cast<const uint2 *>(a.codes + 2 * at);
+                    }
+                    ke[h] = reinterpret_cast<const uint16_t *>(a.exps)[(size_t)(have ? q : q0) * nb + (have ? p / kKeepBlock : 0)];
+                }
+        };
+        fetch(0);
+        unroll<MJ>([&](auto j) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+                *reinterpret_cast<f32x4 *>(sc + lm * STR + i % H * PW + i / H * 16 + 4 * lq) = acc[i][j];
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            uint2 nc[NP][V / 4];
+            uint32_t ne[NP];
+            if constexpr (MODE == kDreluGrad) {
+#pragma unroll
+                for (int h = 0; h < NP; ++h) {
+                    ne[h] = ke[h];
+#pragma unroll
+                    for (int v = 0; v < V / 4; ++v) nc[h][v] = kc[h][v];
+                }
+                if constexpr (j + 1 < MJ) fetch(j + 1);
+            }
+#pragma unroll
+            for (int h = 0; h < NP; ++h) {
+                const int row = h * RPP + r, q = q0 + (wq * MJ + j) * 16 + row;
+                float x[H][V];
+#pragma unroll
+                for (int k = 0; k < H; ++k)
+#pragma unroll
+                    for (int v = 0; v < V; v += 4) {
+                        const f32x4 t = *reinterpret_cast<const f32x4 *>(sc + (r < 16 ? row : 0) * STR + k * PW + c + v);
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) x[k][v + w] = t[w];
+                    }
+                const bool ok = in && q < q_end;
+                const size_t at = (size_t)q * a.n + p;
+                float y[V];
+                if constexpr (MODE == kDreluPack) {
+                    const uint32_t exps = keep_codes<V>(x[0], x[1], in, nc[h], y);
+                    if (!ok) continue;
+                    if constexpr (V == 8)
+                        *reinterpret_cast<u32x4 *>(a.codes + 2 * at) = u32x4{nc[h][0].x, nc[h][0].y, nc[h][1].x, nc[h][1].y};
+                    else *reinterpret_cast<uint2 *>(a.codes + 2 * at) = nc[h][0];
+                    if (p % kKeepBlock == 0)
+                        reinterpret_cast<uint16_t *>(a.exps)[(size_t)q * nb + p / kKeepBlock] = (uint16_t)exps;
+                    store_v<V>(a.out, a.out_f32, at, y);
+                } else {
+                    if (!ok) continue;
+                    float g[V], u[V], z[V];
+                    bool go[V], uo[V];
+#pragma unroll
+                    for (int v = 0; v < V; v += 4) keep_values4(nc[h][v / 4], ne[h], g + v, u + v, go + v, uo + v);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const bool on = go[v] && uo[v];
+                        y[v] = on ? x[0][v] * u[v] : 0.f;
+                        z[v] = on ? x[0][v] * g[v] : 0.f;
+                        u[v] = on ? g[v] * u[v] : 0.f;
+                    }
+                    store_v<V>(a.gate, a.out_f32, at, y);
+                    store_v<V>(a.up, a.out_f32, at, z);
+                    if (a.out) store_v<V>(a.out, a.out_f32, at, u);
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        });
+        return;
+    }
+
     // lane (lm, lq) holds, of the 16 x 16 block (i, j), column lm (Q) and rows
     // 4 lq .. 4 lq + 3 (P)
 #pragma unroll
@@ -939,55 +1054,18 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
             for (int i = 0; i < MI; i += 2) {
                 const int p = p0 + (wp * MI + i) / 2 * 16 + 4 * lq;
                 const f32x4 gt = acc[i][j], u = acc[i + 1][j];
-                [[maybe_unused]] uint2 codes;
-                [[maybe_unused]] uint32_t exps;
-                // (all four lanes of a block take part)
-                if constexpr (MODE == kDreluPack) codes = keep_four(gt, u, p < a.n, &exps);
                 if (p >= a.n) continue;
                 const size_t at = (size_t)q * a.n + p;
                 f32x4 c;
 #pragma unroll
                 for (int v = 0; v < 4; ++v) c[v] = drelu1(gt[v], u[v]);
                 store4(a.out, a.out_f32, at, c);
-                if constexpr (MODE == kDreluPack) {
-                    *reinterpret_cast<uint2 *>(a.codes + 2 * at) = codes;
-                    if (lq == 0)
-                        reinterpret_cast<uint16_t *>(a.exps)[(size_t)q * ceil_div(a.n, kKeepBlock) + p / kKeepBlock] =
-                            (uint16_t)exps;
-                } else {
+                if constexpr (MODE == kDrelu) {
                     if (a.gate) {
                         store4(a.gate, a.out_f32, at, gt);
                         store4(a.up, a.out_f32, at, u);
                     }
                 }
-            }
-        } else if constexpr (MODE == kDreluGrad) {
-            // the codes of all blocks, then block by block
-            const size_t base = (size_t)q * a.n, ebase = (size_t)q * ceil_div(a.n, kKeepBlock);
-            uint2 codes[MI];
-            uint32_t exps[MI];
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const int p = min(p0 + (wp * MI + i) * 16 + 4 * lq, a.n - 4);
-                codes[i] = *reinterpret_cast<const uint2 *>(a.codes + 2 * (base + p));
-                exps[i] = reinterpret_cast<const uint16_t *>(a.exps)[ebase + p / kKeepBlock];
-            }
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const int p = p0 + (wp * MI + i) * 16 + 4 * lq;
-                if (p >= a.n) continue;
-                f32x4 g, u, dg, du, c;
-                keep_values4(codes[i], exps[i], g, u);
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const bool on = g[v] > 0.f && u[v] > 0.f;
-                    dg[v] = on ? acc[i][j][v] * u[v] : 0.f;
-                    du[v] = on ? acc[i][j][v] * g[v] : 0.f;
-                    c[v] = on ? g[v] * u[v] : 0.f;
-                }
-                store4(a.gate, a.out_f32, base + p, dg);
-                store4(a.up, a.out_f32, base + p, du);
-                if (a.out) store4(a.out, a.out_f32, base + p, c);
             }
         } else {
             const size_t base = MODE == kGradW ? ((size_t)g * a.n + q) * a.k : (size_t)q * a.n;

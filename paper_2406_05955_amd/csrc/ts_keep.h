@@ -13,64 +13,89 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "ts_device.h"
 
 namespace ts {
 
 constexpr int kKeepBlock = 16;  // columns per exponent byte
 
-// 16 x exponent + mantissa of max(0, v), rounded to nearest even; a finite value
-// to the largest finite one at most.  0 where v is not positive (or NaN), and
-// for the smallest subnormals, whose code is 1 all the same.
-__device__ __forceinline__ int keep_steps(float v) {
-    uint32_t b = __float_as_uint(v > 0.f ? v : 0.f);
-    b = b < 0x7F800000u ? min(b, 0x7F7BFFFFu) : b;
+// t of positive bits b (0: of what is not positive), a finite value's only up to
+// the largest if SAT.
+template <bool SAT>
+__device__ __forceinline__ int keep_steps(uint32_t b) {
+    if constexpr (SAT) b = b < 0x7F800000u ? min(b, 0x7F7BFFFFu) : b;
     return (int)((b + 0x3FFFFu + ((b >> 19) & 1u)) >> 19);
 }
-__device__ __forceinline__ uint32_t keep_code(float v, int t, int e0) {
-    return v > 0.f ? (uint32_t)max(t - 16 * e0 + 240, 1) : 0u;
-}
-// The value of a code (no block has a code that leads outside of fp32).
-__device__ __forceinline__ float keep_value(uint32_t code, int e0) {
-    return code ? __uint_as_float((code + 16u * (uint32_t)e0 - 240u) << 19) : 0.f;
-}
 
-// The largest of the four lanes l, l ^ 16, l ^ 32, l ^ 48.
-__device__ __forceinline__ int max_over_rows(int v) {
-    const auto a = __builtin_amdgcn_permlane16_swap((unsigned)v, (unsigned)v, false, false);
-    const int m = max((int)a[0], (int)a[1]);
-    const auto b = __builtin_amdgcn_permlane32_swap((unsigned)m, (unsigned)m, false, false);
-    return max((int)b[0], (int)b[1]);
-}
-
-// Four columns of gate and of up of a block that lanes l, l ^ 16, ... share:
-// eight codes, gate's and up's in turn, and the two exponent bytes.  `in`: the
-// columns exist.
-__device__ __forceinline__ uint2 keep_four(f32x4 g, f32x4 u, bool in, uint32_t *exps) {
-    int tg[4], tu[4], mg = 0, mu = 0;
+// V columns of gate and of up, whose block of 16 is in 16 / V neighbouring lanes: their
+// codes, gate's and up's in turn, four columns a pair of words, the block's two exponent
+// bytes, and c = max(0, gate) max(0, up).  `in`: the columns exist.  16 instructions a
+// column (with comparisons instead of the median and the check for what overflows
+// once a block, 32).
+template <int V>
+__device__ __forceinline__ uint32_t keep_codes(const float (&g)[V], const float (&u)[V], bool in, uint2 (&codes)[V / 4],
+                                               float (&c)[V]) {
+    uint32_t bg[V], bu[V];
+    int tg[V], tu[V], mg, mu;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        tg[v] = keep_steps(g[v]);
-        tu[v] = keep_steps(u[v]);
-        mg = max(mg, tg[v]);
-        mu = max(mu, tu[v]);
+    for (int v = 0; v < V; ++v) {
+        const float x = fmaxf(g[v], 0.f), y = fmaxf(u[v], 0.f);  // (NaN: 0)
+        c[v] = x * y;
+        bg[v] = __float_as_uint(x);
+        bu[v] = __float_as_uint(y);
     }
-    const int eg = max(15, max_over_rows(in ? mg : 0) >> 4), eu = max(15, max_over_rows(in ? mu : 0) >> 4);
-    uint32_t c[4];
+    auto steps = [&](auto sat) {
+        mg = mu = 0;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) c[v] = keep_code(g[v], tg[v], eg) | keep_code(u[v], tu[v], eu) << 8;
-    *exps = (uint32_t)eg | (uint32_t)eu << 8;
-    return uint2{c[0] | c[1] << 16, c[2] | c[3] << 16};
+        for (int v = 0; v < V; ++v) {
+            tg[v] = keep_steps<decltype(sat)::value>(bg[v]);
+            tu[v] = keep_steps<decltype(sat)::value>(bu[v]);
+            mg = max(mg, tg[v]);
+            mu = max(mu, tu[v]);
+        }
+        mg = in ? mg : 0;
+        mu = in ? mu : 0;
+        auto over = [&](auto ctrl) {
+            mg = max(mg, __builtin_amdgcn_update_dpp(0, mg, decltype(ctrl)::value, 0xF, 0xF, false));
+            mu = max(mu, __builtin_amdgcn_update_dpp(0, mu, decltype(ctrl)::value, 0xF, 0xF, false));
+        };
+        over(std::integral_constant<int, 0xB1>{});                        // quad_perm [1,0,3,2]
+        if constexpr (V == 4) over(std::integral_constant<int, 0x4E>{});  // quad_perm [2,3,0,1]
+    };
+    steps(std::false_type{});
+    if (__any(max(mg, mu) >= 0xFF0)) {
+        // values that round to 2^128, infinities (times what is not positive: 0)
+        steps(std::true_type{});
+#pragma unroll
+        for (int v = 0; v < V; ++v) c[v] = bg[v] && bu[v] ? c[v] : 0.f;
+    }
+    const int eg = max(15, mg >> 4), eu = max(15, mu >> 4), kg = 16 * eg - 240, ku = 16 * eu - 240;
+    // max(1, t - k) where b > 0, otherwise (t = 0) 0: the middle one of t - k, 1 and b
+    auto code = [](int t, int k, uint32_t b) { return (uint32_t)max(min(max(t - k, 1), (int)b), min(t - k, 1)); };
+#pragma unroll
+    for (int v = 0; v < V; v += 4) {
+        uint32_t q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = code(tg[v + i], kg, bg[v + i]) | code(tu[v + i], ku, bu[v + i]) << 8;
+        codes[v / 4] = uint2{q[0] | q[1] << 16, q[2] | q[3] << 16};
+    }
+    return (uint32_t)eg | (uint32_t)eu << 8;
 }
 
-// Their values.
-__device__ __forceinline__ void keep_values4(uint2 codes, uint32_t exps, f32x4 &g, f32x4 &u) {
-    const int eg = exps & 255, eu = exps >> 8 & 255;
+// Four columns' codes as values (of a code 0: some finite number), and which codes are
+// not 0.  (No block has a code that leads outside of
+// fp32.)
+__device__ __forceinline__ void keep_values4(uint2 codes, uint32_t exps, float *g, float *u, bool *gate_on, bool *up_on) {
+    const uint32_t kg = (16u * (exps & 255u) - 240u) << 19, ku = (16u * (exps >> 8 & 255u) - 240u) << 19;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-        const uint32_t c = (v < 2 ? codes.x : codes.y) >> 16 * (v & 1);
-        g[v] = keep_value(c & 255u, eg);
-        u[v] = keep_value(c >> 8 & 255u, eu);
+        const uint32_t c = v < 2 ? codes.x : codes.y, a = c >> 16 * (v & 1) & 255u, b = c >> (16 * (v & 1) + 8) & 255u;
+        gate_on[v] = a != 0u;
+        up_on[v] = b != 0u;
+        g[v] = __uint_as_float((a << 19) + kg);
+        u[v] = __uint_as_float((b << 19) + ku);
     }
 }
 

@@ -32,8 +32,14 @@ __global__ __launch_bounds__(256) void drelu_unpack_kernel(const uint8_t *codes,
         uint32_t g[V / 2], u[V / 2];
 #pragma unroll
         for (int h = 0; h < V / 4; ++h) {
-            f32x4 gv, uv;
-            keep_values4(q[h], e, gv, uv);
+            float gv[4], uv[4];
+            bool go[4], uo[4];
+            keep_values4(q[h], e, gv, uv, go, uo);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                gv[v] = go[v] ? gv[v] : 0.f;
+                uv[v] = uo[v] ? uv[v] : 0.f;
+            }
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
                 // exact: the low halves are zeros
