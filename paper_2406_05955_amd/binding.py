@@ -456,9 +456,19 @@ def _need(t, name, dtype, shape):
     extent; a number: so many dimensions)."""
     dt = t.dtype
     if dt is dtype or (type(dtype) is tuple and dt in dtype):
-        if (t.dim() == shape) if type(shape) is int else (t.shape == shape):
+        s = t.shape
+        if type(shape) is int:
+            ok = len(s) == shape
+        else:
+            ok = s == shape
+            if not ok and len(s) == len(shape):
+                ok = True
+                for n, w in zip(s, shape):
+                    if w is not None and n != w:
+                        ok = False
+        if ok:
             if t.numel() > _int_max:
-                _need_int(name, t.shape)
+                _need_int(name, s)
             return
     dts = dtype if isinstance(dtype, tuple) else (dtype,)
     if dt not in dts:

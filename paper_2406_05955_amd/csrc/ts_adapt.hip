@@ -105,12 +105,12 @@ __device__ __forceinline__ void store_t(const AdaptRowsArgs &a, int row, int r, 
 
 }  // namespace
 
-// t of up to 16 RT rows of a segment and 16 NR ranks; W waves share the contraction,
-// their sums are added in a fixed order.
-template <GmmKind KIND, int RT, int NR, int W>
+// t of up to 16 RT rows of a segment and 16 NR ranks; W waves share the contraction, U
+// steps' loads of each on their way together; their sums are added in a fixed order.
+template <GmmKind KIND, int RT, int NR, int W, int U>
 __global__ __launch_bounds__(64 * W) void adapter_rows(AdaptRowsArgs a) {
     constexpr int SZ = GmmElem<KIND>::SZ, KS = 64 / SZ, CE = 16 / SZ, Q = 16 * RT;
-    constexpr int U = RT * NR == 1 ? 8 : 4;  // steps whose loads are on their way together
+    static_assert(RT > 1 || (NR == 1 && W == 16), "a single row: W / per waves a rank");
     __shared__ f32x4 red[W][RT * NR][64];
     const int lane = threadIdx.x & 63, lm = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -188,7 +188,11 @@ __global__ __launch_bounds__(64 * W) void adapter_rows(AdaptRowsArgs a) {
     const int steps = (a.k + KS - 1) / KS, per = (steps + W - 1) / W;
     const int s0 = wave * per, s1 = min(s0 + per, steps);
     f32x4 acc[NR][RT] = {};
-    for (int s = s0; s < s1; s += U) {
+    // (from another step on in each workgroup: rows of 2^n bytes lie in one channel of
+    // the L2 at the same step)
+    const int turns = (s1 - s0 + U - 1) / U, ahead = turns > 0 ? (int)(blockIdx.x + blockIdx.y) % turns : 0;
+    for (int i = 0; i < turns; ++i) {
+        const int s = s0 + (i + ahead < turns ? i + ahead : i + ahead - turns) * U;
         u32x4 af[U][NR], xf[U][RT];
         bool in[U];
 #pragma unroll
@@ -319,7 +323,7 @@ struct AdaptCall {
     hipStream_t stream;
 };
 
-template <GmmKind KIND, int RT, int NR, int W>
+template <GmmKind KIND, int RT, int NR, int W, int RU>
 ts_status run_rows(AdaptRowsArgs r, hipStream_t st) {
     const long long pieces = (long long)r.rows / (16 * RT) + r.segs;
     // few pieces: fewer ranks a workgroup (its A comes through one unit's loads)
@@ -329,7 +333,7 @@ ts_status run_rows(AdaptRowsArgs r, hipStream_t st) {
     const long long wide = pieces + ceil_div(r.blocks, W);
     if (wide * tall * 64 * W >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
     r.pieces = (int)pieces;
-    launch<AdaptRowsArgs>("adapter_rows", adapter_rows<KIND, RT, NR, W>, dim3((unsigned)wide, tall), dim3(64 * W), st, r);
+    launch<AdaptRowsArgs>("adapter_rows", adapter_rows<KIND, RT, NR, W, RU>, dim3((unsigned)wide, tall), dim3(64 * W), st, r);
     return check_launch("adapter_rows");
 }
 
@@ -359,9 +363,10 @@ ts_status run_adapt(const AdaptCall &c) {
     r.parts = adapt_parts(c.dtype, c.odtype);
     r.k = c.k;
     ts_status s;
-    if (c.rows < 2048 || c.rows < 16LL * c.segments) s = run_rows<KIND, 1, 1, 16>(r, c.stream);
-    else if (r.ranks <= 16) s = run_rows<KIND, 4, 1, 8>(r, c.stream);
-    else s = run_rows<KIND, 4, 4, 8>(r, c.stream);
+    if (c.rows < 2048 || c.rows < 16LL * c.segments) s = run_rows<KIND, 1, 1, 16, 8>(r, c.stream);
+    else if (r.ranks <= 16) s = run_rows<KIND, 4, 1, 8, 4>(r, c.stream);
+    else if (r.ranks <= 64) s = run_rows<KIND, 2, 4, 8, 2>(r, c.stream);
+    else s = run_rows<KIND, 4, 4, 8, 2>(r, c.stream);
     if (s != TS_OK) return s;
 
     a.x[0] = static_cast<const char *>(c.x);

@@ -25,14 +25,18 @@ namespace ts {
 
 namespace {
 
-constexpr int kBalThreads = 256, kBalWaves = kBalThreads / 64;
+constexpr int kBalThreads = 1024, kBalWaves = kBalThreads / 64;  // loss
+constexpr int kMaxBalBlocks = 256;
+constexpr int kGradThreads = 256, kGradWaves = kGradThreads / 64;
 
 struct BalArgs {
     const float *logits = nullptr;
     const int32_t *idx = nullptr;
     const uint8_t *mask = nullptr;
-    float *part = nullptr;      // [workgroup][kMaxExperts + 1]: sums of p, of lse^2
-    int32_t *cpart = nullptr;   // [workgroup][kMaxExperts + 1]: counts, tokens
+    float *part = nullptr;      // [workgroup][kMaxExperts]: sums of p
+    int32_t *cpart = nullptr;   // [workgroup][kMaxExperts]: counts
+    float *zpart = nullptr;     // [workgroup]: sum of lse^2
+    int32_t *npart = nullptr;   // [workgroup]: tokens
     float *loss = nullptr;
     int32_t *counts = nullptr;  // [E + 1]
     const float *d_loss = nullptr, *add = nullptr;
@@ -74,7 +78,9 @@ __device__ __forceinline__ void load_logits(const BalArgs &a, int t, int e, bool
     for (int i = 0; i < 4; ++i) l[i] = l[i] == l[i] ? l[i] : -INFINITY;
 }
 
-// Softmax of a token's logits in place, its log-sum; whether it counts: the mask
+// Softmax of a token's logits in place, its log-sum, with the hardware's exp2, log2 and
+// reciprocal (a unit or two in the last place each; the difference to the largest is
+// multiplied once): the forward pass's time is its instructions.  Whether it counts: the mask
 // leaves it and a logit above the lowest finite value.
 template <int L>
 __device__ __forceinline__ bool soft(float (&l)[4], bool in, float &lse) {
@@ -82,12 +88,12 @@ __device__ __forceinline__ bool soft(float (&l)[4], bool in, float &lse) {
     in = in && m > -FLT_MAX;
     // (equal to the largest: 1, an infinite one too)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) l[i] = l[i] == m ? 1.f : expf(l[i] - m);
+    for (int i = 0; i < 4; ++i) l[i] = l[i] == m ? 1.f : __builtin_amdgcn_exp2f((l[i] - m) * 1.44269504f);
     const float s = lanes_sum<L>((l[0] + l[1]) + (l[2] + l[3]));
-    const float r = in ? 1.f / s : 0.f;
+    const float r = in ? __builtin_amdgcn_rcpf(s) : 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) l[i] = in ? l[i] * r : 0.f;
-    lse = in ? m + logf(s) : 0.f;
+    lse = in ? m + __builtin_amdgcn_logf(s) * 0.693147181f : 0.f;
     return in;
 }
 
@@ -116,12 +122,14 @@ __device__ __forceinline__ void finish_loss(const BalArgs &a, int lane, double p
     if (lane < a.E) a.counts[lane] = count;
 }
 
+// A wave takes 64 / L tokens at once, U rounds of them with their loads on their way
+// together (one after another, 200001 tokens of 64 experts 29 us; this 13).
 template <int L>
 __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalArgs a) {
-    constexpr int G = 64 / L;  // tokens a wave has at once
+    constexpr int G = 64 / L, U = 2, KL = (kMaxTopK + L - 1) / L;  // choices of a token a lane
     __shared__ int cnt[kMaxExperts + 1];
     __shared__ float sum[kBalWaves][4 * L + 1];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int sub = lane & (L - 1), tok = lane / L;
     for (int i = tid; i < kMaxExperts + 1; i += kBalThreads) cnt[i] = 0;
     __syncthreads();
@@ -129,22 +137,34 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalArgs a) {
     int n = 0;
     const int step = a.blocks * kBalWaves * G;
     // (whole waves stay in the loop: a token's lanes exchange their maxima)
-    for (int t0 = (blockIdx.x * kBalWaves + wave) * G; t0 < a.T; t0 += step) {
-        const int t = t0 + tok;
-        bool in = t < a.T;
-        if (a.mask) in = in && a.mask[in ? t : 0] != 0;
-        float l[4], lse;
-        load_logits(a, t, sub * 4, in, l);
-        in = soft<L>(l, in, lse);
+    for (int t0 = (blockIdx.x * kBalWaves + wave) * G; t0 < a.T; t0 += U * step) {
+        float l[U][4], lse[U];
+        int e[U][KL];
+        bool in[U];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] += l[i];
-        z += lse * lse;
-        n += in ? 1 : 0;
-        if (in)
-            for (int k = sub; k < a.K; k += L) {
-                const int e = a.idx[(size_t)t * a.K + k];
-                if (e >= 0 && e < a.E) atomicAdd(&cnt[e], 1);  // (in LDS: the order does not matter)
+        for (int u = 0; u < U; ++u) {
+            const int t = t0 + u * step + tok;
+            in[u] = t < a.T;
+            const int tt = in[u] ? t : 0;
+            if (a.mask) in[u] = in[u] && a.mask[tt] != 0;
+            load_logits(a, tt, sub * 4, in[u], l[u]);
+#pragma unroll
+            for (int k = 0; k < KL; ++k) {
+                const bool have = in[u] && sub + k * L < a.K;
+                e[u][k] = have ? a.idx[(size_t)tt * a.K + sub + k * L] : -1;
             }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            in[u] = soft<L>(l[u], in[u], lse[u]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] += l[u][i];
+            z += lse[u] * lse[u];
+            n += in[u] ? 1 : 0;
+#pragma unroll
+            for (int k = 0; k < KL; ++k)
+                if (in[u] && e[u][k] >= 0 && e[u][k] < a.E) atomicAdd(&cnt[e[u][k]], 1);  // (in LDS: the order does not matter)
+        }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i] = over_tokens<L>(acc[i]);
@@ -168,52 +188,74 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalArgs a) {
         finish_loss(a, lane, p, z, cnt[lane], cnt[kMaxExperts]);
         return;
     }
-    const size_t at = (size_t)blockIdx.x * (kMaxExperts + 1);
-    a.part[at + lane] = p;
-    a.cpart[at + lane] = cnt[lane];
+    a.part[blockIdx.x * kMaxExperts + lane] = p;
+    a.cpart[blockIdx.x * kMaxExperts + lane] = cnt[lane];
     if (lane == 0) {
-        a.part[at + kMaxExperts] = z;
-        a.cpart[at + kMaxExperts] = cnt[kMaxExperts];
+        a.zpart[blockIdx.x] = z;
+        a.npart[blockIdx.x] = cnt[kMaxExperts];
     }
 }
 
-// The workgroups' sums: a wave takes every 16th of them, then wave 0 the waves'.
+// The workgroups' sums (256 at most): a wave takes every 16th of them, all its loads
+// on their way together, then wave 0 the waves'.
 __global__ __launch_bounds__(1024) void balance_finish_kernel(BalArgs a) {
-    __shared__ double s_p[16][65];
-    __shared__ int s_c[16][65];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    double p = 0.0, z = 0.0;
-    int c = 0, n = 0;
-#pragma unroll 4
-    for (int b = wave; b < a.blocks; b += 16) {
-        const size_t at = (size_t)b * (kMaxExperts + 1);
-        p += a.part[at + lane];
-        c += a.cpart[at + lane];
-        z += a.part[at + kMaxExperts];
-        n += a.cpart[at + kMaxExperts];
+    constexpr int N = kMaxBalBlocks / 16;
+    __shared__ double s_p[16][64];
+    __shared__ int s_c[16][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    float v[N];
+    int w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int b = min(wave + 16 * i, a.blocks - 1);
+        v[i] = a.part[b * kMaxExperts + lane];
+        w[i] = a.cpart[b * kMaxExperts + lane];
+    }
+    double z = 0.0;
+    int n = 0;
+    if (wave == 0) {
+        float zv[kMaxBalBlocks / 64];
+        int nv[kMaxBalBlocks / 64];
+#pragma unroll
+        for (int i = 0; i < kMaxBalBlocks / 64; ++i) {
+            const int b = min(64 * i + lane, a.blocks - 1);
+            zv[i] = a.zpart[b];
+            nv[i] = a.npart[b];
+        }
+#pragma unroll
+        for (int i = 0; i < kMaxBalBlocks / 64; ++i) {
+            z += 64 * i + lane < a.blocks ? (double)zv[i] : 0.0;
+            n += 64 * i + lane < a.blocks ? nv[i] : 0;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            z += __shfl_xor(z, d);
+            n += __shfl_xor(n, d);
+        }
+    }
+    double p = 0.0;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        p += wave + 16 * i < a.blocks ? (double)v[i] : 0.0;
+        c += wave + 16 * i < a.blocks ? w[i] : 0;
     }
     s_p[wave][lane] = p;
     s_c[wave][lane] = c;
-    if (lane == 0) {
-        s_p[wave][64] = z;
-        s_c[wave][64] = n;
-    }
     __syncthreads();
     if (wave > 0) return;
-    p = z = 0.0;
-    c = n = 0;
+    p = 0.0;
+    c = 0;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) {
-        p += s_p[w][lane];
-        c += s_c[w][lane];
-        z += s_p[w][64];
-        n += s_c[w][64];
+    for (int i = 0; i < 16; ++i) {
+        p += s_p[i][lane];
+        c += s_c[i][lane];
     }
     finish_loss(a, lane, p, z, c, n);
 }
 
 template <int L>
-__global__ __launch_bounds__(kBalThreads) void balance_grad_kernel(BalArgs a) {
+__global__ __launch_bounds__(kGradThreads) void balance_grad_kernel(BalArgs a) {
     constexpr int G = 64 / L;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int sub = lane & (L - 1), tok = lane / L, e = sub * 4;
@@ -224,8 +266,8 @@ __global__ __launch_bounds__(kBalThreads) void balance_grad_kernel(BalArgs a) {
     float f[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = e + i < a.E ? (float)a.counts[e + i] * kn : 0.f;
-    const int step = gridDim.x * kBalWaves * G;
-    for (int t0 = (blockIdx.x * kBalWaves + wave) * G; t0 < a.T; t0 += step) {
+    const int step = gridDim.x * kGradWaves * G;
+    for (int t0 = (blockIdx.x * kGradWaves + wave) * G; t0 < a.T; t0 += step) {
         const int t = t0 + tok;
         const bool have = t < a.T;
         bool in = have;
@@ -263,10 +305,11 @@ int lanes_of(int E) {
     return L;
 }
 
-// Workgroups: one takes up to 8 rounds; above that every unit two of them.
+// Workgroups: one takes up to 4 rounds (1024 tokens of 16 experts; another launch adds up
+// several ones' sums); above that one a unit.
 int balance_blocks(int T, int E) {
     const int round = kBalThreads / lanes_of(E);
-    return T <= 8 * round ? 1 : std::min(ceil_div(T, round), 512);
+    return T <= 4 * round ? 1 : std::min(ceil_div(T, round), kMaxBalBlocks);
 }
 
 size_t balance_ws_bytes(int T, int E, int K) {
@@ -318,7 +361,9 @@ ts_status ts_moe_balance(const float *logits, const int32_t *topk_idx, const uin
         if (!ws || ws_bytes < ts::balance_ws_bytes(tokens, n_experts, top_k)) return TS_ERR_WORKSPACE;
         if (!ts::aligned16(ws)) return TS_ERR_ALIGN;
         a.part = static_cast<float *>(ws);
-        a.cpart = reinterpret_cast<int32_t *>(a.part + (size_t)a.blocks * (ts::kMaxExperts + 1));
+        a.cpart = reinterpret_cast<int32_t *>(a.part + (size_t)a.blocks * ts::kMaxExperts);
+        a.zpart = reinterpret_cast<float *>(a.cpart + (size_t)a.blocks * ts::kMaxExperts);
+        a.npart = reinterpret_cast<int32_t *>(a.zpart + a.blocks);
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
     ts::by_lanes(n_experts, [&](auto l) {
@@ -350,10 +395,10 @@ ts_status ts_moe_balance_grad(const float *logits, const int32_t *counts, const 
     a.E = n_experts;
     a.K = top_k;
     a.four = n_experts % 4 == 0 && ts::aligned16(logits) && ts::aligned16(d_logits) && ts::aligned16(add);
-    const int round = ts::kBalThreads / ts::lanes_of(n_experts);
+    const int round = ts::kGradThreads / ts::lanes_of(n_experts);
     const int grid = std::min(ts::ceil_div(tokens, round), 256 * 8);
     ts::by_lanes(n_experts, [&](auto l) {
-        ts::launch<ts::BalArgs>("moe_balance_grad", ts::balance_grad_kernel<l>, dim3(grid), dim3(ts::kBalThreads),
+        ts::launch<ts::BalArgs>("moe_balance_grad", ts::balance_grad_kernel<l>, dim3(grid), dim3(ts::kGradThreads),
                                 static_cast<hipStream_t>(stream), a);
     });
     return ts::check_launch("moe_balance_grad");

@@ -304,16 +304,28 @@ __device__ __forceinline__ void unroll(F f) {
 
 constexpr int kStrip = 8;
 
-// Whether 16 bytes of bf16 or fp32 values hold an infinity or a NaN; those values
+// Whether N x 16 bytes of bf16 or fp32 values hold an infinity or a NaN; those values
 // alone (BAD), or all others.
+template <GmmKind KIND, int N>
+__device__ __forceinline__ bool not_finite(const u32x4 (&v)[N]) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    if constexpr (KIND == kGmmF32) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) m = max(m, v[i / 4][i % 4] & 0x7FFFFFFFu);
+        return m >= 0x7F800000u;
+    } else {
+        u16x2 m = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i)
+            m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, v[i / 4][i % 4] & 0x7FFF7FFFu));
+        return m.x >= 0x7F80 || m.y >= 0x7F80;
+    }
+}
 template <GmmKind KIND>
 __device__ __forceinline__ bool not_finite(u32x4 v) {
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        bad |= KIND == kGmmF32 ? (v[i] & 0x7F800000u) == 0x7F800000u
-                               : (((v[i] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) != 0u;
-    return bad;
+    const u32x4 one[1] = {v};
+    return not_finite<KIND, 1>(one);
 }
 template <GmmKind KIND, bool BAD>
 __device__ __forceinline__ u32x4 only_finite(u32x4 v) {
@@ -825,92 +837,112 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
         // stages: 8 rounds of loads for 32 requests of rank 16, and for prompts
         // each wave takes the steps of its neighbours' adapters too: gate + up 58 us, 6001
         // rows 1390 to 1420.)
+        // A wave's blocks of P in groups (gate's and up's; eight in two halves), a group's
+        // operands of U steps at a time: whole lines of 64 ranks where U is even (gate
+        // and up together, 64 bytes of each line at a time: 6001 rows of rank 64 1145 us).
         constexpr int both = DRELU ? 2 : 1, CE = 16 / SZ, CK = 64 / SZ;
-        constexpr int REGS = (MI + both * MJ) * 4, LEFT = 176 - MI * MJ * 4, U = LEFT >= 4 * REGS ? 4 : LEFT >= 2 * REGS ? 2 : 1;
+        constexpr int NG = DRELU ? 2 : MI > 4 ? 2 : 1, MG = MI / NG;
+        constexpr int REGS = (MG + MJ) * 4, LEFT = (DRELU ? 192 : 176) - MI * MJ * 4;
+        constexpr int U = REGS <= 8 && !ACOL ? 8 : LEFT >= 4 * REGS ? 4 : LEFT >= 2 * REGS ? 2 : 1;
         const int per = a.rank * a.parts, all = __builtin_amdgcn_readfirstlane(slots) * per;
         const size_t stride = (size_t)both * per;
         // [ranks][columns] matrices go through a part of LDS of this wave's own, for
         // the transposing reads
-        using TW = GmmTile<KIND, true, MI * 16, 64>;
+        using TW = GmmTile<KIND, true, MG * 16, 64>;
         static_assert(!ACOL || (WP * WQ * KW * U * TW::CHUNKS <= 2 * KW * ALL), "half a step a wave");
         [[maybe_unused]] const int widx = kg * (WP * WQ) + wave;
-        for (int s0 = (part * KW + kg) * U; s0 * CK < all; s0 += KWS * U) {
-            u32x4 af[U][MI], bf[both][U][MJ];
-            int f0[U], f1[U];
+        // An adapter's infinities and NaN concern its own rows: the first pass leaves them
+        // out of B (0 x inf with the others' zeros) and notes that there are any; then
+        // a second one adds their products to the rows that have the adapter, 16 bytes of
+        // ranks at a time.
+        bool broken = false;
+        auto ranks = [&](auto second_pass) {
+            for (int s0 = (part * KW + kg) * U; s0 * CK < all; s0 += KWS * U) {
+                unroll<NG>([&](auto g) {
+                    // this group's e-th block
+                    constexpr int G = decltype(g)::value;
+                    constexpr auto block = [](int e) constexpr { return DRELU ? 2 * e + G : G * MG + e; };
+                    u32x4 af[U][MG], bf[U][MJ];
+                    int f0[U], f1[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int w0 = (s0 + u) * CK, v = w0 + lq * CE, own = v / per, rv = v - own * per;
-                const bool in = v < all;
-                f0[u] = w0 / per;
-                f1[u] = (w0 + CK - 1) / per;
+                    for (int u = 0; u < U; ++u) {
+                        const int w0 = (s0 + u) * CK, v = w0 + lq * CE, own = v / per, rv = v - own * per;
+                        const bool in = v < all;
+                        f0[u] = w0 / per;
+                        f1[u] = (w0 + CK - 1) / per;
 #pragma unroll
-                for (int h = 0; h < both; ++h)
+                        for (int j = 0; j < MJ; ++j) {
+                            const char *p = a.t + ((size_t)(q0 + (wq * MJ + j) * 16 + lm) * stride + (DRELU ? G * per : 0) + rv) * SZ;
+                            bf[u][j] = ld_cached(in && slot_q[j] == own ? p : zero);
+                        }
+                        if constexpr (!ACOL) {
+                            const int m = __shfl(ad, in ? own : 0), r = rv >= a.rank ? rv - a.rank : rv;  // (parts: the same B)
 #pragma unroll
-                    for (int j = 0; j < MJ; ++j) {
-                        const char *p = a.t + ((size_t)(q0 + (wq * MJ + j) * 16 + lm) * stride + h * per + rv) * SZ;
-                        bf[h][u][j] = ld_cached(in && slot_q[j] == own ? p : zero);
-                    }
-                if constexpr (!ACOL) {
-                    const int m = __shfl(ad, in ? own : 0), r = rv >= a.rank ? rv - a.rank : rv;  // (parts: the same B)
-#pragma unroll
-                    for (int i = 0; i < MI; ++i) {
-                        const int n = min(p0 + (wp * MI + i) / both * 16 + lm, a.n - 1);
-                        const char *p = a.b[i % both] + (((size_t)m * a.n + n) * a.rank + r) * SZ;
-                        af[u][i] = ld_cached(in ? p : zero);
-                    }
-                }
-            }
-            if constexpr (ACOL) {
-                // U sub-steps of 64 bytes of contraction each
-                char *const own_lds = reinterpret_cast<char *>(s_all) + (size_t)widx * (U * TW::CHUNKS / 2) * 16;
-                const uint32_t l = lds_addr(own_lds);
-                const int pc = (p0 + wp * MI * 16) * SZ;
-                unroll<U * TW::NJ / 2>([&](auto j) {
-                    int row, ch;
-                    TW::at(lane + 64 * j, row, ch);
-                    const int v = s0 * CK + row, own = v / per, rv = v - own * per;
-                    const int m = __shfl(ad, v < all ? own : 0), r = rv >= a.rank ? rv - a.rank : rv;
-                    const char *p = a.b[0] + ((size_t)m * a.rank + r) * ((size_t)a.n * SZ) + min(pc + ch * 16, a.n * SZ - 16);
-                    ld_lds16(v < all ? p : zero, l + 1024 * j);
-                });
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int i = 0; i < MI; ++i)
-                        af[u][i] = TW::frag(reinterpret_cast<const u32x4 *>(own_lds), i, u, lane);
-                // (the next round's loads may overwrite them)
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                bool use[MJ];  // columns with a row of these ranks
-#pragma unroll
-                for (int j = 0; j < MJ; ++j) use[j] = __any(slot_q[j] >= f0[u] && slot_q[j] <= f1[u]);
-#pragma unroll
-                for (int i = 0; i < MI; ++i) {
-                    if (__any(not_finite<KIND>(af[u][i]))) {
-                        // An adapter's infinities and NaN concern its own rows: 0 x inf of
-                        // the others is left out, 16 bytes of ranks at a time.
-                        const u32x4 bad = only_finite<KIND, true>(af[u][i]);
-                        for (int h = 0; h < 4; ++h) {
-                            const u32x4 one = lq == h ? bad : u32x4{0u, 0u, 0u, 0u};
-                            if (!__any(not_finite<KIND>(one))) continue;
-                            const int own = ((s0 + u) * CK + h * CE) / per;
-#pragma unroll
-                            for (int j = 0; j < MJ; ++j) {
-                                const f32x4 d = mma<KIND>(one, bf[i % both][u][j], f32x4{0.f, 0.f, 0.f, 0.f});
-                                if (slot_q[j] == own) acc[i][j] += d;
+                            for (int e = 0; e < MG; ++e) {
+                                const int n = min(p0 + (wp * MI + block(e)) / both * 16 + lm, a.n - 1);
+                                const char *p = a.b[DRELU ? G : 0] + (((size_t)m * a.n + n) * a.rank + r) * SZ;
+                                af[u][e] = ld_cached(in ? p : zero);
                             }
                         }
-                        af[u][i] = only_finite<KIND, false>(af[u][i]);
+                    }
+                    if constexpr (ACOL) {
+                        // U sub-steps of 64 bytes of contraction each
+                        char *const own_lds = reinterpret_cast<char *>(s_all) + (size_t)widx * (U * TW::CHUNKS / 2) * 16;
+                        const uint32_t l = lds_addr(own_lds);
+                        const int pc = (p0 + (wp * MI + block(0)) * 16) * SZ;
+                        unroll<U * TW::NJ / 2>([&](auto j) {
+                            int row, ch;
+                            TW::at(lane + 64 * j, row, ch);
+                            const int v = s0 * CK + row, own = v / per, rv = v - own * per;
+                            const int m = __shfl(ad, v < all ? own : 0), r = rv >= a.rank ? rv - a.rank : rv;
+                            const char *p = a.b[0] + ((size_t)m * a.rank + r) * ((size_t)a.n * SZ) + min(pc + ch * 16, a.n * SZ - 16);
+                            ld_lds16(v < all ? p : zero, l + 1024 * j);
+                        });
+                        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+                        for (int u = 0; u < U; ++u)
+#pragma unroll
+                            for (int e = 0; e < MG; ++e)
+                                af[u][e] = TW::frag(reinterpret_cast<const u32x4 *>(own_lds), e, u, lane);
+                        // (the next round's loads may overwrite them)
+                        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                     }
 #pragma unroll
-                    for (int j = 0; j < MJ; ++j)
-                        if (use[j]) acc[i][j] = mma<KIND>(af[u][i], bf[i % both][u][j], acc[i][j]);
-                }
+                    for (int u = 0; u < U; ++u) {
+                        if constexpr (second_pass) {
+#pragma unroll 1
+                            for (int h = 0; h < 4; ++h) {
+                                const int own = ((s0 + u) * CK + h * CE) / per;
+#pragma unroll
+                                for (int e = 0; e < MG; ++e) {
+                                    const u32x4 bad = only_finite<KIND, true>(af[u][e]), one = lq == h ? bad : u32x4{0u, 0u, 0u, 0u};
+                                    if (!__any(not_finite<KIND>(one))) continue;
+#pragma unroll
+                                    for (int j = 0; j < MJ; ++j) {
+                                        const f32x4 d = mma<KIND>(one, bf[u][j], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                                        for (int c = 0; c < 4; ++c) acc[block(e)][j][c] += slot_q[j] == own ? d[c] : 0.f;
+                                    }
+                                }
+                            }
+                            continue;
+                        }
+                        if (__any(not_finite<KIND>(af[u]))) {
+                            broken = true;
+#pragma unroll
+                            for (int e = 0; e < MG; ++e) af[u][e] = only_finite<KIND, false>(af[u][e]);
+                        }
+#pragma unroll
+                        for (int j = 0; j < MJ; ++j)
+                            if (__any(slot_q[j] >= f0[u] && slot_q[j] <= f1[u]))  // a column has a row of these ranks
+#pragma unroll
+                                for (int e = 0; e < MG; ++e) acc[block(e)][j] = mma<KIND>(af[u][e], bf[u][j], acc[block(e)][j]);
+                    }
+                });
             }
-        }
+        };
+        ranks(std::false_type{});
+        if (broken) ranks(std::true_type{});
         if constexpr (KW > 1 && ACOL) __syncthreads();  // (the sums go where other waves' matrices are)
     }
     if constexpr (KW > 1) {
