@@ -836,7 +836,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
         // wave takes what its own rows need.  (Through LDS with all of the workgroup, two
         // stages: 8 rounds of loads for 32 requests of rank 16, and for prompts
         // each wave takes the steps of its neighbours' adapters too: gate + up 58 us, 6001
-        // rows 1390 to 1420.)
+        // rows 1390 to 1420; this 50 and 1120 to 1150, without adapters 44 and 1070.)
         // A wave's blocks of P in groups (gate's and up's; eight in two halves), a group's
         // operands of U steps at a time: whole lines of 64 ranks where U is even (gate
         // and up together, 64 bytes of each line at a time: 6001 rows of rank 64 1145 us).
@@ -967,7 +967,8 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
         // Two to four bytes of each tensor an element, four tensors: through LDS, 16 rows
         // of a wave's at a time, so that a lane has V neighbouring columns and a row's
         // are whole lines.  (From the lanes that hold the sums, 8 bytes a lane: gate + up
-        // of 8192 rows 1780 us, the gradient of 6002 rows 860.)
+        // of 8192 rows 1780 us, the gradient of 6002 rows 860; this 1640 to 1700 and 690 to
+        // 740, where the products alone take 1590 and 600 to 630.)
         constexpr int V = KIND == kGmmBf16 ? 8 : 4, H = DRELU ? 2 : 1, PW = MI * 16 / H, LPR = PW / V;
         constexpr int RPP = 64 / LPR < 16 ? 64 / LPR : 16, NP = 16 / RPP, STR = H * PW + 4;
         static_assert((KW - 1) * BP * BQ * 4 + WP * WQ * 16 * STR * 4 <= KW * ALL * 16, "16 rows a wave fit the stages");
