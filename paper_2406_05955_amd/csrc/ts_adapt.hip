@@ -32,39 +32,63 @@ struct AdaptRowsArgs {
     int wr = 0, blocks = 0;       // rows of one of the product's waves, their number
 };
 
-// Segment s's rows in pieces of Q: its first piece has the number offsets[s] / Q +
-// s, which no other segment's piece has (a segment's pieces are at most its rows / Q
-// + 1), so the pieces need no count of those before.  This finds the last s whose
-// first piece is not behind piece `p`: 64 probes a round.
-template <int Q>
-__device__ __forceinline__ int segment_of(const AdaptRowsArgs &a, int p, int lane) {
-    auto first = [&](int s) { return min(max(a.offsets[s], 0), a.rows) / Q + s; };
-    int lo = 0, hi = a.segs;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) / 64, s = lo + lane * step;
-        const bool ok = s < hi && first(min(s, hi - 1)) <= p;
-        const int n = max(__popcll(__ballot(ok)), 1);
-        lo += (n - 1) * step;
-        hi = min(hi, lo + step);
+// The segments as a wave looks them up: up to 64 are held, one a lane, by loads on their
+// way together (probing memory for 9 to 32 segments, each probe waits for the last:
+// adapter_rows 2 us longer); more are probed where they are.
+struct Segments {
+    const AdaptRowsArgs &a;
+    int first = 0, behind = 0, adapter = 0;  // lane s: segment s's
+    bool held;
+    __device__ __forceinline__ int clamped(int s) const { return min(max(a.offsets[s], 0), a.rows); }
+    __device__ __forceinline__ Segments(const AdaptRowsArgs &args, int lane) : a(args), held(args.segs <= 64) {
+        if (held) {
+            first = clamped(min(lane, a.segs - 1));
+            behind = clamped(min(lane, a.segs - 1) + 1);
+            adapter = a.adapter[min(lane, a.segs - 1)];
+        }
     }
-    return lo;
-}
+    // (s uniform)
+    __device__ __forceinline__ int begin(int s) const { return held ? __builtin_amdgcn_readlane(first, s) : clamped(s); }
+    __device__ __forceinline__ int end(int s) const { return held ? __builtin_amdgcn_readlane(behind, s) : clamped(s + 1); }
+    __device__ __forceinline__ int id(int s) const { return held ? __builtin_amdgcn_readlane(adapter, s) : a.adapter[s]; }
+    // Segment s's rows in pieces of Q: its first piece has the number offsets[s] / Q +
+    // s, which no other segment's piece has (a segment's pieces are at most its rows / Q
+    // + 1), so the pieces need no count of those before.  The last s whose first piece is
+    // not behind piece `p`.
+    template <int Q>
+    __device__ __forceinline__ int of_piece(int p, int lane) const {
+        if (held) return max(__popcll(__ballot(lane < a.segs && first / Q + lane <= p)), 1) - 1;
+        int lo = 0, hi = a.segs;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 63) / 64, s = lo + lane * step;
+            const bool ok = s < hi && clamped(min(s, hi - 1)) / Q + min(s, hi - 1) <= p;
+            const int n = max(__popcll(__ballot(ok)), 1);
+            lo += (n - 1) * step;
+            hi = min(hi, lo + step);
+        }
+        return lo;
+    }
+    // The adapter of each lane's row: that of the last segment that begins at or in
+    // front of it.
+    __device__ __forceinline__ int id_of_row(int row) const {
+        int lo = 0, hi = a.segs;
+        while (__any(hi - lo > 1)) {
+            const int mid = (lo + hi) / 2, o = held ? __shfl(first, mid) : clamped(mid);
+            if (hi - lo > 1) (o <= row ? lo : hi) = mid;
+        }
+        return held ? __shfl(adapter, lo) : a.adapter[lo];
+    }
+};
 
 // Slots of the adapters of rows r0 ... of one of the product's waves (a.wr rows: lane
 // l has row r0 + l), by one wave: a slot for each adapter, in the order of their
 // first rows.  Runs of rows with one adapter are looked up one after another: prompts
 // have few.
-__device__ __forceinline__ void wave_slots(const AdaptRowsArgs &a, int block, int lane) {
-    const int b = min(max(a.offsets[0], 0), a.rows), e = min(max(a.offsets[a.segs], 0), a.rows);
+__device__ __forceinline__ void wave_slots(const AdaptRowsArgs &a, const Segments &seg, int block, int lane) {
+    const int b = seg.begin(0), e = seg.end(a.segs - 1);
     const int r0 = b + block * a.wr, row = r0 + lane;
     if (r0 >= e) return;
-    // the last segment that begins at or in front of the row
-    int lo = 0, hi = a.segs;
-    while (__any(hi - lo > 1)) {
-        const int mid = (lo + hi) / 2;
-        if (hi - lo > 1) (a.offsets[mid] <= row ? lo : hi) = mid;
-    }
-    int id = a.adapter[lo];
+    int id = seg.id_of_row(row);
     if (lane >= a.wr || row >= e || id < 0 || id >= a.adapters) id = -1;
     const int before = __shfl_up(id, 1);
     uint64_t starts = __ballot(id >= 0 && (lane == 0 || id != before));
@@ -114,17 +138,18 @@ __global__ __launch_bounds__(64 * W) void adapter_rows(AdaptRowsArgs a) {
     __shared__ f32x4 red[W][RT * NR][64];
     const int lane = threadIdx.x & 63, lm = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Segments segments(a, lane);
     if ((int)blockIdx.x >= a.pieces) {
         const int block = ((int)blockIdx.x - a.pieces) * W + wave;
-        if (blockIdx.y == 0 && block < a.blocks) wave_slots(a, block, lane);
+        if (blockIdx.y == 0 && block < a.blocks) wave_slots(a, segments, block, lane);
         return;
     }
-    const int seg = __builtin_amdgcn_readfirstlane(segment_of<Q>(a, blockIdx.x, lane));
-    const int b = min(max(a.offsets[seg], 0), a.rows), e = min(max(a.offsets[seg + 1], 0), a.rows);
+    const int seg = __builtin_amdgcn_readfirstlane(segments.of_piece<Q>(blockIdx.x, lane));
+    const int b = segments.begin(seg), e = segments.end(seg);
     const int piece = (int)blockIdx.x - (b / Q + seg);
     if (piece < 0 || b + (long long)piece * Q >= e) return;
     const int r0 = b + piece * Q, r1 = min(r0 + Q, e);
-    const int id = a.adapter[seg];
+    const int id = segments.id(seg);
     if (id < 0 || id >= a.adapters) return;
     // ranks [k0, k1) (of both matrices, one behind the other)
     const int k0 = blockIdx.y * a.per, k1 = min(k0 + a.per, a.ranks);
