@@ -634,7 +634,7 @@ def moe_balance_grad(logits, counts, d_loss, top_k: int, mask=None, add=None, ou
     if add is not None:
         _need(add, "add", _f32, (T, E))
     st = _here(logits, counts, d_loss, mask, add, out)
-    out = _new(out, "out", (T, E), _f32, logits.device)
+    out = torch.empty_like(logits) if out is None else _new(out, "out", (T, E), _f32, logits.device)
     code = lib.ts_moe_balance_grad(_ptr(logits), _ptr(counts), _ptr(d_loss), _ptr(mask), _ptr(add), T, E, K, _ptr(out),
                                    st)
     if code:

@@ -146,6 +146,29 @@ def test_layer_with_adapters(dtype, rows, S):
     within(y, want, gref.rounded(bound, want, dtype))
 
 
+def test_adapters_are_trained_as_groups():
+    """Rows sorted by adapter: the groups of grouped_mm and grouped_mm_dw give the
+    gradients of what adapter_mm computes, against 64-bit autograd."""
+    g = gen(100)
+    rows, N, rank, n, k = 150, 4, 8, 136, 72
+    off = gref.ragged(rows, N, g)
+    x, w = randn(g, rows, k), randn(g, n, k, scale=k ** -0.5)
+    a, b, d_y = randn(g, N, rank, k, scale=k ** -0.5), randn(g, N, n, rank), randn(g, rows, n)
+    xd, wd, ad, bd, dd, od = dev(x, w, a, b, d_y, off)
+    y = ts.adapter_mm(xd, wd, ad, bd, od, torch.arange(N, dtype=torch.int32, device=DEV))
+    t = ts.grouped_mm(xd, ad, od)
+    d_t = ts.grouped_mm(dd, bd, od, w_kn=True)
+    d_a, d_b = ts.grouped_mm_dw(d_t, xd, od), ts.grouped_mm_dw(dd, t, od)
+    d_x = ts.grouped_mm(dd, wd[None], w_kn=True) + ts.grouped_mm(d_t, ad, od, w_kn=True)
+    leaves = [v.double().requires_grad_() for v in (x, a, b)]
+    want = torch.cat([leaves[0][p:q] @ w.double().t() + leaves[0][p:q] @ leaves[1][i].t() @ leaves[2][i].t()
+                      for i, p, q in gref.spans(off)])
+    want.backward(d_y.double())
+    # two products in a row, sums of up to 150 terms each
+    for got, ref_ in zip((y, d_x, d_a, d_b), (want.detach(), *(v.grad for v in leaves))):
+        assert (got.cpu().double() - ref_).norm() <= 2 * 152 * 2.0 ** -23 * ref_.norm()
+
+
 # --- streams, graphs, workspaces ------------------------------------------------------
 
 def flat(r):
