@@ -854,7 +854,8 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
         // An adapter's infinities and NaN concern its own rows: the first pass leaves them
         // out of B (0 x inf with the others' zeros) and notes that there are any; then
         // a second one adds their products to the rows that have the adapter, 16 bytes of
-        // ranks at a time.
+        // ranks at a time.  Of t in two parts the first alone: an infinity takes its sign,
+        // and the remainder, 0 or of the other sign, would make it NaN.
         bool broken = false;
         auto ranks = [&](auto second_pass) {
             for (int s0 = (part * KW + kg) * U; s0 * CK < all; s0 += KWS * U) {
@@ -912,7 +913,8 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
                         if constexpr (second_pass) {
 #pragma unroll 1
                             for (int h = 0; h < 4; ++h) {
-                                const int own = ((s0 + u) * CK + h * CE) / per;
+                                const int v = (s0 + u) * CK + h * CE, own = v / per;
+                                if (v - own * per >= a.rank) continue;
 #pragma unroll
                                 for (int e = 0; e < MG; ++e) {
                                     const u32x4 bad = only_finite<KIND, true>(af[u][e]), one = lq == h ? bad : u32x4{0u, 0u, 0u, 0u};

@@ -1,0 +1,118 @@
+"""Adapters whose matrices hold infinities and NaN: each value of the result is the
+definition's, signs included, and other requests' rows keep theirs.  All finite
+values are small whole numbers (times powers of two), so that every sum is exact in
+any order and results are compared for equality."""
+import pytest
+import torch
+
+import adapt_util as ref
+import group_util as gref
+from adapt_util import BF16, F32
+from gpu_util import DEV
+from test_gpu_group import dev
+
+pytestmark = pytest.mark.gpu
+
+ts = pytest.importorskip("paper_2406_05955_amd.binding") if torch.cuda.is_available() else None
+
+INF, NAN = float("inf"), float("nan")
+N, BAD = 6, 2  # adapters, the broken one
+
+# rows, segments, rank, n, k: a single row, one row a request, a split contraction (its
+# last three), prompts, the large tiles
+SHAPES = [(1, 1, 16, 264, 136), (40, 40, 16, 264, 136), (300, 7, 64, 264, 136), (2500, 40, 24, 1552, 136),
+          (1, 1, 8, 144, 4104), (33, 5, 24, 144, 4104), (300, 300, 40, 144, 4104)]
+
+
+def whole(g, *shape, top=2, keep=1.0):
+    v = torch.randint(-top, top + 1, shape, generator=g).float()
+    return v * (torch.rand(shape, generator=g) < keep)
+
+
+def inputs(rows, S, rank, n, k, products, seed):
+    """x [rows][k], per product (w [n][k], a [N][rank][k], b [N][rank][n]), offsets,
+    adapters, scales: whole numbers, products of x with a below 2^8 (so that t is exact
+    in one bf16 part)."""
+    g = torch.Generator().manual_seed(1000 * seed + rows + k)
+    off, ad = ref.segments(rows, S, N, g)
+    ad[::3] = BAD
+    x = whole(g, rows, k)
+    mats = [(whole(g, n, k), whole(g, N, rank, k, keep=min(1.0, 100 / k)), whole(g, N, rank, n)) for _ in range(products)]
+    for _, a, _ in mats:
+        assert float((x @ a.view(-1, k).t()).abs().max()) <= 256
+    return x, mats, off, ad, torch.exp2(torch.randint(-1, 3, (N,), generator=g).float())
+
+
+def break_b(b):
+    """Infinities and NaN in [rank][n], one a column or two of one step's."""
+    rank, n = b.shape
+    j = torch.arange(n)
+    for every, at, value in ((5, 0, INF), (5, 1, -INF), (13, 3, NAN)):
+        c = j[j % every == at]
+        b[c % rank, c] = value
+    c = j[j % 11 == 2]
+    b[0, c], b[1, c] = INF, -INF
+    c = j[j % 17 == 4]
+    b[rank - 1, c], b[0, c] = INF, INF
+
+
+def projected(x, w, a, b, off, ad, scale):
+    """x w^T + scale (x a^T) b, term by term in 64 bits."""
+    x, y = x.double(), x.double() @ w.double().t()
+    for s, p, q in gref.spans(off):
+        i = int(ad[s])
+        if q > p and 0 <= i < N:
+            # (term by term: a library product may pad with zeros, and 0 x inf is NaN)
+            t = (x[p:q, :, None].expand(-1, -1, 1) * 0).sum(1).expand(-1, a.shape[1]).clone()
+            fin = torch.isfinite(a[i])
+            t += x[p:q] @ torch.where(fin, a[i], 0.0).double().t()
+            for r, c in (~fin).nonzero().tolist():
+                t[:, r] += x[p:q, c] * float(a[i, r, c])
+            t *= float(scale[i])
+            for r in range(a.shape[1]):
+                y[p:q] += t[:, r:r + 1] * b[i, r].double()
+    return y
+
+
+def equal(got, want):
+    nan = torch.isnan(want)
+    return torch.equal(torch.isnan(got), nan) and torch.equal(got[~nan], want[~nan])
+
+
+def compare(x, mats, off, ad, scale, dtype, odt):
+    d = lambda t: t.to(DEV)  # noqa: E731
+    o = dev(off, ad)
+    ys = [projected(d(x), d(w), d(a), d(b), off, ad, scale) for w, a, b in mats]
+    ops = [[t.to(dtype) for t in m] for m in mats]
+    if len(mats) == 1:
+        want = ys[0].to(odt)
+        (w, a, b), = ops
+        for kn in (False, True):
+            wk, bk = (w.t().contiguous(), b) if kn else (w, b.transpose(1, 2).contiguous())
+            got = ts.adapter_mm(*dev(x.to(dtype), wk, a, bk), *o, scale=dev(scale), w_kn=kn, out_dtype=odt)
+            assert equal(got, want), kn
+        return want
+    # (projections exact in fp32, one rounding of their product; a NaN closes)
+    want = gref.drelu(*[y.float() for y in ys]).to(odt)
+    (wg, ag, bg), (wu, au, bu) = ops
+    bg, bu = (b.transpose(1, 2).contiguous() for b in (bg, bu))
+    got = ts.adapter_drelu(*dev(x.to(dtype), wg, wu, ag, bg, au, bu), *o, scale=dev(scale), out_dtype=odt)
+    assert equal(got, want)
+    return want
+
+
+@pytest.mark.parametrize("dtype,odt", [(BF16, BF16), (BF16, F32), (F32, F32), (F32, BF16)])
+@pytest.mark.parametrize("rows,S,rank,n,k", SHAPES)
+def test_infinities_and_nan_of_b(rows, S, rank, n, k, dtype, odt):
+    if k > 4000:  # (the sums of two parts at least)
+        assert ts.adapter_workspace_bytes(rows, rank, 1, False, n, k, dtype, odt) > 2 * rows * n * 4
+    x, mats, off, ad, scale = inputs(rows, S, rank, n, k, 1, 1)
+    break_b(mats[0][2][BAD])
+    want = compare(x, mats, off, ad, scale, dtype, odt)
+    assert all(bool(v.any()) for v in (want == INF, want == -INF, torch.isnan(want)))
+    for broken in ((0,), (1,), (0, 1)):
+        x, mats, off, ad, scale = inputs(rows, S, rank, n, k, 2, 2)
+        for i in broken:
+            break_b(mats[i][2][BAD])
+        want = compare(x, mats, off, ad, scale, dtype, odt)
+        assert bool((want == INF).any())
