@@ -304,8 +304,7 @@ __device__ __forceinline__ void unroll(F f) {
 
 constexpr int kStrip = 8;
 
-// Whether N x 16 bytes of bf16 or fp32 values hold an infinity or a NaN; those values
-// alone (BAD), or all others.
+// Whether N x 16 bytes of bf16 or fp32 values hold an infinity or a NaN.
 template <GmmKind KIND, int N>
 __device__ __forceinline__ bool not_finite(const u32x4 (&v)[N]) {
     typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -327,18 +326,49 @@ __device__ __forceinline__ bool not_finite(u32x4 v) {
     const u32x4 one[1] = {v};
     return not_finite<KIND, 1>(one);
 }
-template <GmmKind KIND, bool BAD>
-__device__ __forceinline__ u32x4 only_finite(u32x4 v) {
+// Their bits.
+template <GmmKind KIND>
+__device__ __forceinline__ uint32_t not_finite_bits(uint32_t v) {
+    if constexpr (KIND == kGmmF32) {
+        return (v & 0x7F800000u) == 0x7F800000u ? ~0u : 0u;
+    } else {
+        const uint32_t top = ((v & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+        return (top & 0x80000000u ? 0xFFFF0000u : 0u) | (top & 0x8000u ? 0xFFFFu : 0u);
+    }
+}
+// Those values alone.
+template <GmmKind KIND>
+__device__ __forceinline__ u32x4 only_not_finite(u32x4 v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] &= not_finite_bits<KIND>(v[i]);
+    return v;
+}
+// The smallest normal number of their sign in their place.
+template <GmmKind KIND>
+__device__ __forceinline__ u32x4 tiny_for_not_finite(u32x4 v) {
+    constexpr uint32_t sign = KIND == kGmmF32 ? 0x80000000u : 0x80008000u, least = KIND == kGmmF32 ? 0x00800000u : 0x00800080u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t bad;  // their bits
-        if constexpr (KIND == kGmmF32) {
-            bad = (v[i] & 0x7F800000u) == 0x7F800000u ? ~0u : 0u;
-        } else {
-            const uint32_t top = ((v[i] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-            bad = (top & 0x80000000u ? 0xFFFF0000u : 0u) | (top & 0x8000u ? 0xFFFFu : 0u);
+        const uint32_t bad = not_finite_bits<KIND>(v[i]);
+        v[i] = (v[i] & (~bad | sign)) | (bad & least);
+    }
+    return v;
+}
+// One of their sign in infinities' place.
+template <GmmKind KIND>
+__device__ __forceinline__ u32x4 one_for_infinite(u32x4 v) {
+    constexpr int N = KIND == kGmmF32 ? 1 : 2, B = 32 / N;
+    constexpr uint32_t sign = KIND == kGmmF32 ? 0x80000000u : 0x8000u, inf = KIND == kGmmF32 ? 0x7F800000u : 0x7F80u,
+                       one = KIND == kGmmF32 ? 0x3F800000u : 0x3F80u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            const uint32_t b = v[i] >> (B * h) & (sign | (sign - 1));
+            w |= ((b & ~sign) == inf ? (b & sign) | one : b) << (B * h);
         }
-        v[i] &= BAD ? bad : ~bad;
+        v[i] = w;
     }
     return v;
 }
@@ -855,7 +885,10 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
         // out of B (0 x inf with the others' zeros) and notes that there are any; then
         // a second one adds their products to the rows that have the adapter, 16 bytes of
         // ranks at a time.  Of t in two parts the first alone: an infinity takes its sign,
-        // and the remainder, 0 or of the other sign, would make it NaN.
+        // and the remainder, 0 or of the other sign, would make it NaN.  Where t is
+        // infinite too, 0 in B's place (first pass) or beside its infinity (second) would
+        // be a NaN: 2^-126 of B's sign stands in the first pass, beside what the
+        // second adds nothing, and t's infinities are ones of their sign in the second.
         bool broken = false;
         auto ranks = [&](auto second_pass) {
             for (int s0 = (part * KW + kg) * U; s0 * CK < all; s0 += KWS * U) {
@@ -911,13 +944,15 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
                         if constexpr (second_pass) {
+#pragma unroll
+                            for (int j = 0; j < MJ; ++j) bf[u][j] = one_for_infinite<KIND>(bf[u][j]);
 #pragma unroll 1
                             for (int h = 0; h < 4; ++h) {
                                 const int v = (s0 + u) * CK + h * CE, own = v / per;
                                 if (v - own * per >= a.rank) continue;
 #pragma unroll
                                 for (int e = 0; e < MG; ++e) {
-                                    const u32x4 bad = only_finite<KIND, true>(af[u][e]), one = lq == h ? bad : u32x4{0u, 0u, 0u, 0u};
+                                    const u32x4 bad = only_not_finite<KIND>(af[u][e]), one = lq == h ? bad : u32x4{0u, 0u, 0u, 0u};
                                     if (!__any(not_finite<KIND>(one))) continue;
 #pragma unroll
                                     for (int j = 0; j < MJ; ++j) {
@@ -932,7 +967,7 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
                         if (__any(not_finite<KIND>(af[u]))) {
                             broken = true;
 #pragma unroll
-                            for (int e = 0; e < MG; ++e) af[u][e] = only_finite<KIND, false>(af[u][e]);
+                            for (int e = 0; e < MG; ++e) af[u][e] = tiny_for_not_finite<KIND>(af[u][e]);
                         }
 #pragma unroll
                         for (int j = 0; j < MJ; ++j)

@@ -116,3 +116,24 @@ def test_infinities_and_nan_of_b(rows, S, rank, n, k, dtype, odt):
             break_b(mats[i][2][BAD])
         want = compare(x, mats, off, ad, scale, dtype, odt)
         assert bool((want == INF).any())
+
+
+@pytest.mark.parametrize("dtype,odt", [(BF16, BF16), (BF16, F32), (F32, F32), (F32, BF16)])
+@pytest.mark.parametrize("rows,S,rank,n,k", SHAPES)
+def test_infinite_t_beside_infinities_of_b(rows, S, rank, n, k, dtype, odt):
+    """A's infinity makes t infinite at one rank; B has infinities, NaN and zeros
+    there and at other ranks of the same step."""
+    for broken in ((0,), (1,), (0, 1)):
+        for products in (1, 2):
+            if broken[-1] >= products:
+                continue
+            x, mats, off, ad, scale = inputs(rows, S, rank, n, k, products, 3)
+            x[:, 5] = torch.where(torch.arange(rows) % 2 == 0, 1.0, -1.0)
+            for i in broken:
+                _, a, b = mats[i]
+                a[BAD, 1, 5] = -INF
+                break_b(b[BAD])
+                b[BAD, 1, 8::23], b[BAD, 1, 9::23], b[BAD, 1, 10::23] = INF, NAN, 0.0
+                b[BAD, 2, 8::46] = INF
+            want = compare(x, mats, off, ad, scale, dtype, odt)
+            assert bool((want == INF).any())
