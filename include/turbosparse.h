@@ -465,7 +465,8 @@ size_t ts_adapter_workspace_bytes(int rows, int rank, int products, int w_kn, in
 /*
  * Low-rank adapters of many requests beside a shared projection.  Rows come in
  * `segments` (requests): offsets [segments + 1] ascending, adapter [segments]; a
- * segment whose adapter is outside [0, n_adapters) has none.
+ * segment whose adapter is outside [0, n_adapters) has none.  Offsets are brought into
+ * [0, rows]; where they then descend anywhere, no row has an adapter.
  *   out[r] = x[r] w^T + scale[a] (x[r] a[a]^T) b[a]^T
  *   x [rows][k], w [n][k], a [n_adapters][rank][k], b [n_adapters][n][rank]; with
  *   w_kn 1: w [k][n], b [n_adapters][rank][n]; scale fp32 [n_adapters] or NULL (ones).

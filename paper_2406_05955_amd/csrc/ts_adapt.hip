@@ -38,14 +38,23 @@ struct AdaptRowsArgs {
 struct Segments {
     const AdaptRowsArgs &a;
     int first = 0, behind = 0, adapter = 0;  // lane s: segment s's
-    bool held;
+    bool held, ordered = true;               // (ordered: of held ones)
     __device__ __forceinline__ int clamped(int s) const { return min(max(a.offsets[s], 0), a.rows); }
     __device__ __forceinline__ Segments(const AdaptRowsArgs &args, int lane) : a(args), held(args.segs <= 64) {
         if (held) {
             first = clamped(min(lane, a.segs - 1));
             behind = clamped(min(lane, a.segs - 1) + 1);
             adapter = a.adapter[min(lane, a.segs - 1)];
+            ordered = !__any(first > behind);
         }
+    }
+    // Whether the offsets ascend, by all of a workgroup of THREADS.
+    template <int THREADS>
+    __device__ __forceinline__ bool all_ordered() const {
+        if (held) return ordered;
+        int bad = 0;
+        for (int s = threadIdx.x; s < a.segs; s += THREADS) bad |= clamped(s) > clamped(s + 1);
+        return !__syncthreads_or(bad);
     }
     // (s uniform)
     __device__ __forceinline__ int begin(int s) const { return held ? __builtin_amdgcn_readlane(first, s) : clamped(s); }
@@ -83,13 +92,15 @@ struct Segments {
 // Slots of the adapters of rows r0 ... of one of the product's waves (a.wr rows: lane
 // l has row r0 + l), by one wave: a slot for each adapter, in the order of their
 // first rows.  Runs of rows with one adapter are looked up one after another: prompts
-// have few.
-__device__ __forceinline__ void wave_slots(const AdaptRowsArgs &a, const Segments &seg, int block, int lane) {
+// have few.  Offsets that descend anywhere leave all rows without an adapter: two
+// segments may then have the same row, whose t is whichever's comes last, and nothing
+// reads it.
+__device__ __forceinline__ void wave_slots(const AdaptRowsArgs &a, const Segments &seg, bool ordered, int block, int lane) {
     const int b = seg.begin(0), e = seg.end(a.segs - 1);
     const int r0 = b + block * a.wr, row = r0 + lane;
     if (r0 >= e) return;
     int id = seg.id_of_row(row);
-    if (lane >= a.wr || row >= e || id < 0 || id >= a.adapters) id = -1;
+    if (!ordered || lane >= a.wr || row >= e || id < 0 || id >= a.adapters) id = -1;
     const int before = __shfl_up(id, 1);
     uint64_t starts = __ballot(id >= 0 && (lane == 0 || id != before));
     int list = -1, n = 0, slot = -1;
@@ -140,10 +151,13 @@ __global__ __launch_bounds__(64 * W) void adapter_rows(AdaptRowsArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Segments segments(a, lane);
     if ((int)blockIdx.x >= a.pieces) {
+        if (blockIdx.y > 0) return;
+        const bool ordered = segments.all_ordered<64 * W>();
         const int block = ((int)blockIdx.x - a.pieces) * W + wave;
-        if (blockIdx.y == 0 && block < a.blocks) wave_slots(a, segments, block, lane);
+        if (block < a.blocks) wave_slots(a, segments, ordered, block, lane);
         return;
     }
+    if (!segments.ordered) return;
     const int seg = __builtin_amdgcn_readfirstlane(segments.of_piece<Q>(blockIdx.x, lane));
     const int b = segments.begin(seg), e = segments.end(seg);
     const int piece = (int)blockIdx.x - (b / Q + seg);
