@@ -28,6 +28,7 @@ struct AdaptRowsArgs {
     char *t = nullptr;
     int32_t *slots = nullptr, *slot_ad = nullptr, *slot_count = nullptr;
     int rows = 0, segs = 0, adapters = 0, rank = 0, ranks = 0, parts = 1, k = 0;  // ranks: of both matrices
+    int first = 0;                // workgroups of earlier launches
     int pieces = 0, per = 16;     // ranks of a workgroup
     int wr = 0, blocks = 0;       // rows of one of the product's waves, their number
 };
@@ -150,17 +151,18 @@ __global__ __launch_bounds__(64 * W) void adapter_rows(AdaptRowsArgs a) {
     const int lane = threadIdx.x & 63, lm = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Segments segments(a, lane);
-    if ((int)blockIdx.x >= a.pieces) {
+    const int wg = a.first + (int)blockIdx.x;
+    if (wg >= a.pieces) {
         if (blockIdx.y > 0) return;
         const bool ordered = segments.all_ordered<64 * W>();
-        const int block = ((int)blockIdx.x - a.pieces) * W + wave;
+        const int block = (wg - a.pieces) * W + wave;
         if (block < a.blocks) wave_slots(a, segments, ordered, block, lane);
         return;
     }
     if (!segments.ordered) return;
-    const int seg = __builtin_amdgcn_readfirstlane(segments.of_piece<Q>(blockIdx.x, lane));
+    const int seg = __builtin_amdgcn_readfirstlane(segments.of_piece<Q>(wg, lane));
     const int b = segments.begin(seg), e = segments.end(seg);
-    const int piece = (int)blockIdx.x - (b / Q + seg);
+    const int piece = wg - (b / Q + seg);
     if (piece < 0 || b + (long long)piece * Q >= e) return;
     const int r0 = b + piece * Q, r1 = min(r0 + Q, e);
     const int id = segments.id(seg);
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(64 * W) void adapter_rows(AdaptRowsArgs a) {
     f32x4 acc[NR][RT] = {};
     // (from another step on in each workgroup: rows of 2^n bytes lie in one channel of
     // the L2 at the same step)
-    const int turns = (s1 - s0 + U - 1) / U, ahead = turns > 0 ? (int)(blockIdx.x + blockIdx.y) % turns : 0;
+    const int turns = (s1 - s0 + U - 1) / U, ahead = turns > 0 ? (int)((unsigned)wg + blockIdx.y) % turns : 0;
     for (int i = 0; i < turns; ++i) {
         const int s = s0 + (i + ahead < turns ? i + ahead : i + ahead - turns) * U;
         u32x4 af[U][NR], xf[U][RT];
@@ -369,11 +371,17 @@ ts_status run_rows(AdaptRowsArgs r, hipStream_t st) {
     r.per = 16 * NR;
     while (NR == 1 && r.per > 4 && pieces * ceil_div(r.ranks, r.per) < 128) r.per /= 2;
     const int tall = ceil_div(r.ranks, r.per);
-    const long long wide = pieces + ceil_div(r.blocks, W);
-    if (wide * tall * 64 * W >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
+    // (a launch takes less than 2^32 threads)
+    const long long wide = pieces + ceil_div(r.blocks, W), most = ((1LL << 32) - 1) / (64 * W * tall);
     r.pieces = (int)pieces;
-    launch<AdaptRowsArgs>("adapter_rows", adapter_rows<KIND, RT, NR, W, RU>, dim3((unsigned)wide, tall), dim3(64 * W), st, r);
-    return check_launch("adapter_rows");
+    for (long long first = 0; first < wide; first += most) {
+        r.first = (int)first;
+        launch<AdaptRowsArgs>("adapter_rows", adapter_rows<KIND, RT, NR, W, RU>,
+                              dim3((unsigned)std::min(most, wide - first), tall), dim3(64 * W), st, r);
+        const ts_status s = check_launch("adapter_rows");
+        if (s != TS_OK) return s;
+    }
+    return TS_OK;
 }
 
 template <GmmKind KIND>

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import adapt_util as ref
+import group_util as gref
 from adapt_util import BF16, F32
 from gpu_util import DEV
 from test_gpu_group import dev, gen, randn, within
@@ -53,3 +54,40 @@ def test_descending_offsets_leave_no_adapter(rows, S, how):
     for fill in (0, 0x3F, 0xFF):
         for g, t in zip(run(o, ad, fill), want):
             assert torch.equal(g, t)
+
+
+# rows, segments, rank, products, dtype: more workgroups of the ranks' values than a launch
+# takes (2^32 threads), by rows and ranks and by segments
+@pytest.mark.parametrize("rows,S,rank,products,dtype", [(270000, 270000, 128, 2, BF16), (530001, 530001, 128, 1, F32),
+                                                        (3, 1 << 23, 8, 1, BF16)])
+def test_more_workgroups_than_a_launch_takes(rows, S, rank, products, dtype):
+    n, k, N = 16, 8, 5
+    g = gen(111, rows)
+    d = lambda *s: randn(g, *s, dtype=dtype, scale=0.5)  # noqa: E731
+    x, mats = d(rows, k), [(d(n, k), d(N, rank, k), d(N, n, rank)) for _ in range(products)]
+    if S == rows:
+        off = torch.arange(S + 1, dtype=torch.int32)
+    else:
+        off = torch.full((S + 1,), rows, dtype=torch.int32)
+        off[0], off[1:S // 2], off[S // 2:S - 1] = 0, 1, 2  # rows of segments 0, S / 2 - 1, S - 2
+    ad = torch.randint(0, N, (S,), generator=g, dtype=torch.int32)
+    o = dev(off, ad)
+    (w, a, b), (v, c, e) = mats[0], mats[-1]
+    if products == 1:
+        got = ts.adapter_mm(*dev(x, w, a, b), *o, out_dtype=F32)
+    else:
+        got = ts.adapter_drelu(*dev(x, w, v, a, b, c, e), *o, out_dtype=F32)
+    parts = 2 if dtype == BF16 else 0
+    if S == rows:
+        at = torch.cat([torch.randint(0, rows, (200,), generator=g), torch.tensor([0, rows - 1]),
+                        torch.arange(rows // 2 - 20, rows // 2 + 20), torch.arange(262100, 262200)])
+        own = ad[at]
+    else:
+        at, own = torch.arange(3), ad[torch.tensor([0, S // 2 - 1, S - 2])]
+    ys = [ref.adapted(x[at], *m, torch.arange(len(at) + 1), own, None, False, parts) for m in mats]
+    want, bound = ys[0]
+    if products == 2:
+        (p, ep), (q, eq) = ys
+        want, bound = gref.drelu(p, q), gref.drelu_bound(p, q, ep, eq)
+        bound = bound + 2.0 ** -23 * (want + bound)
+    within(got[at.to(DEV)], want, bound)
