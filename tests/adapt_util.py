@@ -12,6 +12,14 @@ TILES = [(1, 144, 136), (1, 144, 2056), (1500, 528, 136), (1500, 1040, 136), (1,
          (700, 2064, 4104), (200, 1040, 4104), (700, 4112, 4104), (700, 1040, 4104), (1000, 1040, 4104), (500, 2064, 8192),
          (500, 4112, 8192), (1700, 528, 28672), (1700, 1040, 28672)]
 
+# ... and every tile with every split that a grid of sizes chooses for it
+SPLITS = [(1, 8, 136), (1, 8, 2056), (1, 8, 8200), (33, 14336, 136), (1500, 8, 4104), (1500, 1040, 136), (33, 2064, 4104),
+          (1, 2064, 8200), (700, 144, 8200), (1500, 4112, 136), (1, 2064, 2056), (700, 8, 8200), (1, 8, 4104), (3000, 8, 4104),
+          (2000, 4112, 136), (200, 1040, 14344), (700, 528, 136), (1, 1040, 28672), (130, 528, 14344), (700, 2064, 8200),
+          (6000, 8, 8200), (33, 8208, 14344), (700, 1040, 8200), (1, 4112, 4104), (300, 1040, 28672), (1, 8208, 14344),
+          (130, 264, 14344), (2000, 144, 4104), (1000, 144, 8200), (700, 4112, 8200), (33, 4112, 8200),
+          (500, 4112, 14344), (1000, 144, 14344), (1000, 1040, 28672), (1000, 528, 57352), (200, 4112, 8200), (200, 1040, 57352)]
+
 
 def segments(rows, S, N, gen, lead=0, tail=0):
     """Ascending offsets over [lead, rows - tail) (one row each where rows == S,

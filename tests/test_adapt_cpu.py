@@ -103,3 +103,21 @@ def test_the_gpu_tests_reach_every_tile(tmp_path):
             tiles = {1, 2, 3, 6} if kind else {0, 2, 3, 4, 5, 6}
             want = {(t, s) for t in tiles - ({6} if drelu else set()) for s in (False, True)}
             assert want <= got, (kind, drelu, w_kn, want - got)
+
+
+def test_the_gpu_tests_reach_every_split(tmp_path):
+    """Every tile with every split that is chosen for it over a grid of sizes (as large as
+    a test's matrices may be)."""
+    exe = build_tile_check(tmp_path)
+    grid = [(r, n, k) for r in (1, 8, 33, 64, 130, 200, 300, 500, 700, 1000, 1500, 2000, 3000, 6000)
+            for n in (8, 144, 264, 528, 1040, 2064, 4112, 8208, 14336)
+            for k in (136, 520, 1032, 2056, 4104, 8200, 14344, 28672, 57352)
+            if r * n * k <= 6e10 and (r + n) * k <= 1.2e8 and r * n <= 2e7 and 4 * n * k < 1 << 32]
+    for kind in (0, 1):
+        for drelu, w_kn in ((0, 0), (0, 1), (1, 0)):
+            got = []
+            for sizes in (grid, ref.TILES + ref.SPLITS):
+                lines = "\n".join(f"{kind} {drelu} {w_kn} {rows} {n} {k}" for rows, n, k in sizes)
+                r = subprocess.run([exe, "-"], input=lines, capture_output=True, text=True, check=True)
+                got.append(set(r.stdout.splitlines()))
+            assert len(got[0]) > 10 and got[0] <= got[1], (kind, drelu, w_kn, got[0] - got[1])

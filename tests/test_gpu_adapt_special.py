@@ -1,7 +1,8 @@
-"""Adapters whose matrices hold infinities and NaN: each value of the result is the
-definition's, signs included, and other requests' rows keep theirs.  All finite
-values are small whole numbers (times powers of two), so that every sum is exact in
-any order and results are compared for equality."""
+"""Adapters of whole numbers, and of infinities and NaN among them: each value of the
+result is the definition's, signs included, and other requests' rows keep theirs.
+All finite values are small whole numbers (times powers of two), so that every sum is
+exact in any order, a step that is left out or taken twice shows, and results are
+compared for equality."""
 import pytest
 import torch
 
@@ -137,3 +138,30 @@ def test_infinite_t_beside_infinities_of_b(rows, S, rank, n, k, dtype, odt):
                 b[BAD, 2, 8::46] = INF
             want = compare(x, mats, off, ad, scale, dtype, odt)
             assert bool((want == INF).any())
+
+
+@pytest.mark.parametrize("rows,n,k", ref.TILES + ref.SPLITS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_every_step_counts_once(rows, n, k, dtype):
+    """Every tile and split: each step of the contraction is in the sums, once (a bound
+    of the sums' rounding is wider than a step's share where the contraction is long)."""
+    g = torch.Generator(device=DEV).manual_seed(rows + n + k)
+    r = lambda *s: torch.randint(-2, 3, s, generator=g, device=DEV, dtype=torch.int8)  # noqa: E731
+    x = r(rows, k).to(dtype)
+    for S, rank in ((rows, 16), (max(rows // 60, 1), 24)):
+        off, ad = ref.segments(rows, S, N, torch.Generator().manual_seed(k))
+        scale = torch.exp2(torch.randint(-1, 3, (N,), generator=torch.Generator().manual_seed(n)).float())
+        # (few values of a, so that t is a whole number below 2^8)
+        mats = [(r(n, k).to(dtype), (r(N, rank, k) * (torch.rand(N, rank, k, generator=g, device=DEV) < 100 / k)).to(dtype),
+                 r(N, n, rank).to(dtype)) for _ in range(2)]
+        for _, a, _ in mats:
+            assert float((x.float() @ a.float().view(-1, k).t()).abs().max()) <= 256
+        ys = [ref.adapted(x, *m, off, ad, scale, False, 0)[0] for m in mats]
+        assert all(bool((y.abs() < 2 ** 22).all()) for y in ys)
+        o = dev(off, ad)
+        (w, a, b), (v, c, d) = mats
+        for kn in (False, True):
+            m = (w.t().contiguous(), a, b.transpose(1, 2).contiguous()) if kn else (w, a, b)
+            assert torch.equal(ts.adapter_mm(x, *m, *o, scale=dev(scale), w_kn=kn, out_dtype=F32).double(), ys[0]), (S, kn)
+        got = ts.adapter_drelu(x, w, v, a, b, c, d, *o, scale=dev(scale), out_dtype=F32)
+        assert torch.equal(got, gref.drelu(*[y.float() for y in ys])), S
