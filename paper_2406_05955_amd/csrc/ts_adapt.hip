@@ -433,7 +433,6 @@ ts_status run_adapt(const AdaptCall &c) {
     a.slot_count = r.slot_count;
     a.sums = reinterpret_cast<float *>(r.t + plan.t + plan.slots);
     a.segs = c.segments;
-    a.adapters = c.adapters;
     a.rank = c.rank;
     a.parts = r.parts;
     if (c.products == 2) s = run_fwd<KIND, kDreluAdapt, false>("adapter_drelu", a, c.stream);

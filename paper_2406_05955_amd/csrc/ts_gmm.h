@@ -1171,6 +1171,15 @@ constexpr bool gmm_in_table() {
     return false;
 }
 
+// Whether wave_rows, by which the adapters' slots are laid out, says what the kernel's
+// waves hold.
+template <int BP, int BQ, int WQ>
+constexpr bool gmm_wave_rows() {
+    for (int t = 0; t < kTiles; ++t)
+        if (kTileSize[t].p == BP && kTileSize[t].q == BQ) return wave_rows((GmmTileId)t) == BQ / WQ;
+    return false;
+}
+
 // Launches it; a grid beyond the runtime's 2^32 threads is refused.
 inline unsigned gmm_split(const GmmArgs &) { return 1; }
 inline unsigned gmm_split(const GmmAdaptArgs &a) { return (unsigned)a.split; }
@@ -1178,6 +1187,7 @@ inline unsigned gmm_split(const GmmAdaptArgs &a) { return (unsigned)a.split; }
 template <GmmKind KIND, GmmMode MODE, bool ACOL, int BP, int BQ, int WP, int WQ, int AR, int BR, int KW = 1, bool WIDE = false>
 ts_status run_tiled(const char *name, const typename GmmArgsOf<MODE>::type &a, hipStream_t st) {
     static_assert(MODE == kGradW || WIDE || gmm_in_table<KIND, BP, BQ, WP, WQ, AR, BR, KW>(), "the tile's line in kTileSize");
+    static_assert(!is_adapt(MODE) || gmm_wave_rows<BP, BQ, WQ>(), "rows of a wave");
     const long long grid = gmm_grid<MODE, BP, BQ>(a);
     if (grid * gmm_split(a) * (64 * WP * WQ * KW) >= (1LL << 32)) return TS_ERR_UNSUPPORTED;
     launch<typename GmmArgsOf<MODE>::type>(name, gmm_tiled<KIND, MODE, ACOL, BP, BQ, WP, WQ, AR, BR, KW, WIDE>, dim3((unsigned)grid, gmm_split(a)),

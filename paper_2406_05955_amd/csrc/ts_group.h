@@ -67,7 +67,7 @@ struct GmmAdaptArgs : GmmArgs {
     const int32_t *slots = nullptr, *slot_ad = nullptr, *slot_count = nullptr;
     const char *b[2] = {nullptr, nullptr};
     float *sums = nullptr;    // [split][rows][gate, up][n]
-    int segs = 0, adapters = 0, rank = 0, parts = 1, split = 1;
+    int segs = 0, rank = 0, parts = 1, split = 1;
     GmmTileId tile = kTile128x64;
 };
 // Rows of a wave of each tile.
