@@ -367,7 +367,10 @@ struct AdaptCall {
 template <GmmKind KIND, int RT, int NR, int W, int RU>
 ts_status run_rows(AdaptRowsArgs r, hipStream_t st) {
     const long long pieces = (long long)r.rows / (16 * RT) + r.segs;
-    // few pieces: fewer ranks a workgroup (its A comes through one unit's loads)
+    // few pieces: fewer ranks a workgroup, whose A comes through one unit's loads (us, 16
+    // / 8 / 4 ranks: k 14336, 1 row x 16 ranks 9.8 / 6.4 / 6.5, 32 rows of as many requests
+    // 11.7 / 7.3 / 6.2, x 32 11.2 / 7.9 / 10.0; 256 rows of one request, 128 ranks 32 / 49
+    // / 65; a row each of 32 requests x 128 ranks 26 / 25 / 24)
     r.per = 16 * NR;
     while (NR == 1 && r.per > 4 && pieces * ceil_div(r.ranks, r.per) < 128) r.per /= 2;
     const int tall = ceil_div(r.ranks, r.per);
@@ -382,6 +385,25 @@ ts_status run_rows(AdaptRowsArgs r, hipStream_t st) {
         if (s != TS_OK) return s;
     }
     return TS_OK;
+}
+
+// Rows x ranks of a workgroup, by how much there is to do.  16 x 16 reads a row once for
+// every 16 ranks and a rank's A once for every 16 rows; 32 x 64 and 64 x 64 read less
+// and leave units idle, or lanes where there are fewer ranks or shorter segments.  us,
+// 16 x 16 / 32 x 64 / 64 x 64: bf16, k 4096, 40 segments: 2048 rows x 16 ranks 12 / 18
+// / 22, 8192 x 16 27 / 29 / 26; 1024 x 64 19 / 23 / 27, 2048 x 64 28 / 25 / 30 (2^17), 6001
+// x 64 61 / 25 / 33, 8192 x 64 77 / 47 / 33 (2^19), 16384 x 256 547 / 218 / 189; in 750
+// segments of 8 rows 6001 x 32 55 / 44 / 53, x 256 390 / 218 / 271, in 2048 of one row
+// 2048 x 64 146 / 135 / 177, and of k 14336 370 / 517 / 531.  fp32, whose matrix instructions take eight times as long: 2048 x 64 55 / 56 /
+// 104, 6001 x 128 213 / 120 / 200, 16384 x 256 1024 / 529 / 556.  Over 1400 calls (512
+// to 40000 rows, 1 segment to one a row, 8 to 256 ranks) 4% above each one's best.
+template <GmmKind KIND>
+ts_status run_ranks(const AdaptRowsArgs &r, hipStream_t st) {
+    const long long each = (long long)r.rows * r.ranks;
+    if (r.ranks <= 16 || each < 1 << 17 || r.rows < 8LL * r.segs) return run_rows<KIND, 1, 1, 16, 8>(r, st);
+    if constexpr (KIND == kGmmBf16)
+        if (each >= 1 << 19 && r.rows >= 32LL * r.segs) return run_rows<KIND, 4, 4, 8, 2>(r, st);
+    return run_rows<KIND, 2, 4, 8, 2>(r, st);
 }
 
 template <GmmKind KIND>
@@ -409,11 +431,7 @@ ts_status run_adapt(const AdaptCall &c) {
     r.ranks = c.rank * c.products;
     r.parts = adapt_parts(c.dtype, c.odtype);
     r.k = c.k;
-    ts_status s;
-    if (c.rows < 2048 || c.rows < 16LL * c.segments) s = run_rows<KIND, 1, 1, 16, 8>(r, c.stream);
-    else if (r.ranks <= 16) s = run_rows<KIND, 4, 1, 8, 4>(r, c.stream);
-    else if (r.ranks <= 64) s = run_rows<KIND, 2, 4, 8, 2>(r, c.stream);
-    else s = run_rows<KIND, 4, 4, 8, 2>(r, c.stream);
+    ts_status s = run_ranks<KIND>(r, c.stream);
     if (s != TS_OK) return s;
 
     a.x[0] = static_cast<const char *>(c.x);

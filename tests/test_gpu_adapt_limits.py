@@ -7,6 +7,7 @@ import adapt_util as ref
 import group_util as gref
 from adapt_util import BF16, F32
 from gpu_util import DEV
+from test_gpu_adapt import check
 from test_gpu_group import dev, gen, randn, within
 
 pytestmark = pytest.mark.gpu
@@ -91,3 +92,21 @@ def test_more_workgroups_than_a_launch_takes(rows, S, rank, products, dtype):
         want, bound = gref.drelu(p, q), gref.drelu_bound(p, q, ep, eq)
         bound = bound + 2.0 ** -23 * (want + bound)
     within(got[at.to(DEV)], want, bound)
+
+
+# rows, segments, rank: the ranks' values by workgroups of 16 x 16, 32 x 64 and (bf16) 64
+# x 64 rows x ranks, on both sides of the sizes where one gives way to the next
+@pytest.mark.parametrize("rows,S,rank,products,shape", [
+    (2500, 40, 48, 1, 0), (1365, 1, 48, 2, 0), (1366, 1, 48, 2, 1), (9001, 30, 16, 1, 0), (9001, 30, 24, 1, 1),
+    (3001, 370, 128, 1, 1), (3001, 380, 128, 1, 0), (4095, 40, 128, 1, 1), (4097, 40, 128, 1, 2), (4097, 130, 128, 1, 1),
+    (2500, 7, 120, 2, 2)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_every_shape_of_the_ranks_workgroups(rows, S, rank, products, shape, dtype):
+    each = rows * rank * products
+    small = rank * products <= 16 or each < 1 << 17 or rows < 8 * S
+    assert shape == (0 if small else 2 if each >= 1 << 19 and rows >= 32 * S else 1)
+    n, k, N = 40, 1144, 6
+    g = torch.Generator(device=DEV).manual_seed(rows + rank)
+    x, mats, off, ad, scale = ref.case(rows, S, N, rank, n, k, dtype, False, g, products, lead=3, tail=2)
+    check(x, mats, off, ad, scale, False, F32)
+    check(x, mats, off, ad, scale, False, dtype)
