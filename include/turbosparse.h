@@ -476,7 +476,7 @@ size_t ts_adapter_workspace_bytes(int rows, int rank, int products, int w_kn, in
  *   (w_gate, w_up [n][k], a pair of a and b for each).
  * Rows outside the segments are not written.  The product in the middle (rank values a
  * row) is summed in fp32; with TS_BF16 operands it enters the second product as
- * bf16, or as two bf16 parts (16 bits) where the output is fp32.  An adapter's
+ * two bf16 parts (16 bits), or three (24) where the output is fp32.  An adapter's
  * infinities and NaN reach the rows that have it, no others.
  */
 ts_status ts_adapter_mm(const void *x, const void *w, const void *a, const void *b, const float *scale, ts_dtype dtype,

@@ -121,21 +121,38 @@ __device__ __forceinline__ void wave_slots(const AdaptRowsArgs &a, const Segment
     if (lane == 0) a.slot_count[block] = n;
 }
 
-// Where t of a row and rank stands: gate's parts, then up's.
-__device__ __forceinline__ size_t t_at(const AdaptRowsArgs &a, int row, int r) {
-    return (size_t)row * a.ranks * a.parts + r + (r >= a.rank ? (size_t)a.rank * (a.parts - 1) : 0);
-}
+// Where t stands of a row (counted from the first segment's) and rank; parts are 16
+// a.rank behind one another.
 template <GmmKind KIND>
-__device__ __forceinline__ void store_t(const AdaptRowsArgs &a, int row, int r, float v) {
-    const size_t at = t_at(a, row, r);
+__device__ __forceinline__ size_t t_at(const AdaptRowsArgs &a, int row, int r) {
+    constexpr int CE = 16 / GmmElem<KIND>::SZ;
+    const int room = adapt_room(a.parts), second = r >= a.rank;
+    const size_t place = (size_t)(row / 16) * a.ranks * room + r + (second ? a.rank * (room - 1) : 0);
+    return place / CE * CE * 16 + row % 16 * CE + place % CE;
+}
+// N neighbouring ranks (1 or 4, of one matrix).
+template <GmmKind KIND, int N>
+__device__ __forceinline__ void store_t(const AdaptRowsArgs &a, int row, int r, const float (&x)[N]) {
+    size_t at = t_at<KIND>(a, row, r);
     if constexpr (KIND == kGmmF32) {
-        reinterpret_cast<float *>(a.t)[at] = v;
+        float *const t = reinterpret_cast<float *>(a.t) + at;
+        if constexpr (N == 4) *reinterpret_cast<f32x4 *>(t) = f32x4{x[0], x[1], x[2], x[3]};
+        else *t = x[0];
     } else {
-        __bf16 *const t = reinterpret_cast<__bf16 *>(a.t);
-        const __bf16 hi = (__bf16)v;
-        t[at] = hi;
-        // what the first rounding left (nothing of what has no remainder)
-        if (a.parts == 2) t[at + a.rank] = (__bf16)(fabsf((float)hi) < INFINITY ? v - (float)hi : 0.f);
+        typedef __bf16 b16xn __attribute__((ext_vector_type(N)));
+        float v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = x[i];
+        // each part is what the ones before left (nothing of what has no remainder)
+        for (int p = 0; p < a.parts; ++p, at += 16 * a.rank) {
+            b16xn hi;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                hi[i] = (__bf16)v[i];
+                v[i] = fabsf((float)hi[i]) < INFINITY ? v[i] - (float)hi[i] : 0.f;
+            }
+            *reinterpret_cast<b16xn *>(reinterpret_cast<__bf16 *>(a.t) + at) = hi;
+        }
     }
 }
 
@@ -163,7 +180,9 @@ __global__ __launch_bounds__(64 * W) void adapter_rows(AdaptRowsArgs a) {
     const int seg = __builtin_amdgcn_readfirstlane(segments.of_piece<Q>(wg, lane));
     const int b = segments.begin(seg), e = segments.end(seg);
     const int piece = wg - (b / Q + seg);
-    if (piece < 0 || b + (long long)piece * Q >= e) return;
+    // (a segment in front of the first one's rows: offsets that descend)
+    const int row0 = segments.begin(0);
+    if (piece < 0 || b < row0 || b + (long long)piece * Q >= e) return;
     const int r0 = b + piece * Q, r1 = min(r0 + Q, e);
     const int id = segments.id(seg);
     if (id < 0 || id >= a.adapters) return;
@@ -213,7 +232,7 @@ __global__ __launch_bounds__(64 * W) void adapter_rows(AdaptRowsArgs a) {
             if (i >= a.per || rr >= k1) return;
             float v = part[i * g];
             for (int w = 1; w < g; ++w) v += part[i * g + w];
-            store_t<KIND>(a, r0, rr, v * scale);
+            store_t<KIND, 1>(a, r0 - row0, rr, {v * scale});
             return;
         }
     }
@@ -271,12 +290,7 @@ __global__ __launch_bounds__(64 * W) void adapter_rows(AdaptRowsArgs a) {
         // lane (lm, lq): ranks 4 lq ... of row lm
         const int row = r0 + i % RT * 16 + lm, r = k0 + i / RT * 16 + 4 * lq;
         if (row >= r1 || r >= k1) continue;
-        if constexpr (KIND == kGmmF32) {
-            *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.t) + t_at(a, row, r)) = v;
-        } else {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) store_t<KIND>(a, row, r + c, v[c]);
-        }
+        store_t<KIND, 4>(a, row - row0, r, {v[0], v[1], v[2], v[3]});
     }
 }
 
@@ -308,15 +322,14 @@ __global__ __launch_bounds__(256) void adapter_sum_kernel(GmmAdaptArgs a) {
 
 namespace {
 
-constexpr int kMaxRank = 128;
-
-// The ranks' intermediate: bf16 operands hold t in one bf16 where the output is
-// rounded to bf16 as well, and in two (16 significant bits) where it is fp32: one
-// rounding of t is 2^-9 of the adapter's share.
-int adapt_parts(ts_dtype dtype, ts_dtype odtype) { return dtype == TS_BF16 && odtype == TS_F32 ? 2 : 1; }
+// The ranks' intermediate: fp32 sums, which beside bf16 operands are held in bf16 parts of
+// 8 bits: all 24 in three where the output is fp32, 16 in two where it is bf16 (a
+// rounding of t to 8 bits, 2^-9 of the adapter's share, is what the output's own is: 0.0020
+// from the result in 64 bits where 16 bits leave 0.0017, the output's rounding).
+int adapt_parts(ts_dtype dtype, ts_dtype odtype) { return dtype == TS_F32 ? 1 : odtype == TS_F32 ? 3 : 2; }
 
 size_t adapt_t_bytes(int rows, int rank, int products, ts_dtype dtype, ts_dtype odtype) {
-    return align_up256((size_t)rows * rank * products * adapt_parts(dtype, odtype) * (dtype == TS_F32 ? 4 : 2));
+    return align_up256((size_t)ceil_div(rows, 16) * 16 * rank * products * adapt_room(adapt_parts(dtype, odtype)) * (dtype == TS_F32 ? 4 : 2));
 }
 
 bool adapt_dims_ok(int rows, int rank, ts_dtype dtype) {

@@ -873,18 +873,50 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
         constexpr int both = DRELU ? 2 : 1, CE = 16 / SZ, CK = 64 / SZ;
         constexpr int NG = DRELU ? 2 : MI > 4 ? 2 : 1, MG = MI / NG;
         constexpr int REGS = (MG + MJ) * 4, LEFT = (DRELU ? 192 : 176) - MI * MJ * 4;
-        constexpr int U = REGS <= 8 && !ACOL ? 8 : LEFT >= 4 * REGS ? 4 : LEFT >= 2 * REGS ? 2 : 1;
-        const int per = a.rank * a.parts, all = __builtin_amdgcn_readfirstlane(slots) * per;
-        const size_t stride = (size_t)both * per;
+        constexpr int U = LEFT >= 4 * REGS ? 4 : LEFT >= 2 * REGS ? 2 : 1;
+        const int per = a.rank, all = __builtin_amdgcn_readfirstlane(slots) * per;
+        const int stride = both * per * adapt_room(a.parts);
+        const char *const t_rows = a.t + (size_t)((q0 - b) / 16 + wq * MJ) * stride * (16 * SZ) + lm * 16;
+        // v / per, of the ranks of up to 64 slots: the quotient is off by less than 2^-15, and
+        // v + 1/2 is 1 / 256 of it or more from where it changes
+        const float per_one = 1.f / (float)per;
+        auto slot_of = [&](int v) { return (int)(((float)v + 0.5f) * per_one); };
+        // where the ranks of the rows' slots begin
+        int first_q[MJ];
+#pragma unroll
+        for (int j = 0; j < MJ; ++j) first_q[j] = slot_q[j] < 0 ? -per : slot_q[j] * per;
         // [ranks][columns] matrices go through a part of LDS of this wave's own, for
         // the transposing reads
         using TW = GmmTile<KIND, true, MG * 16, 64>;
         static_assert(!ACOL || (WP * WQ * KW * U * TW::CHUNKS <= 2 * KW * ALL), "half a step a wave");
         [[maybe_unused]] const int widx = kg * (WP * WQ) + wave;
+        // t's parts all meet the same B, which is loaded once, one after another (two in
+        // registers at a time: the 64 x 32 tile of gate and up takes 195 of them, and a unit
+        // holds one workgroup of it, not two).  The first comes with B, the others of all of
+        // the workgroup's rows into LDS meanwhile: [rows / 16][gate, up][parts][ranks' 16
+        // bytes][16 rows].  (From memory, another round trip each: gate + up of 128
+        // requests of rank 16 128 us, this 110, one part 106.)  The 256 x 256 tile, whose
+        // registers are full, and the one of 64-bit offsets, whose LDS is too small, read
+        // them from memory (6001 rows of rank 64: 1350 us, through LDS 1373, one part 1305).
+        constexpr int OWN = ACOL ? WP * WQ * KW * U * TW::CHUNKS / 2 : 0;  // chunks
+        constexpr bool STAGE = KIND == kGmmBf16 && MI <= 4 && OWN + BQ / 16 * both * 2 * kMaxRank * SZ <= KW * ALL;
+        [[maybe_unused]] const int run = (a.parts - 1) * per * SZ;
+        [[maybe_unused]] bool arrived = false;
+        if constexpr (STAGE) {
+            const int staged_chunks = BQ / 16 * both * run;
+            const int block0 = (q0 - b) / 16, last_block = (a.rows - 1) / 16;
+            const uint32_t l = lds_addr(s_all + OWN);
+            const float run_one = 1.f / (float)run;
+            for (int i0 = widx * 64; i0 < staged_chunks; i0 += WP * WQ * KW * 64) {
+                const int i = min(i0 + lane, staged_chunks - 1), r = (int)(((float)i + 0.5f) * run_one);
+                const size_t at = (size_t)min(block0 + r / both, last_block) * stride + (r % both * adapt_room(a.parts) + 1) * per;
+                ld_lds16(a.t + at * (16 * SZ) + (i - r * run) * 16, l + 16 * i0);
+            }
+        }
         // An adapter's infinities and NaN concern its own rows: the first pass leaves them
         // out of B (0 x inf with the others' zeros) and notes that there are any; then
         // a second one adds their products to the rows that have the adapter, 16 bytes of
-        // ranks at a time.  Of t in two parts the first alone: an infinity takes its sign,
+        // ranks at a time.  Of t's parts the first alone: an infinity takes its sign,
         // and the remainder, 0 or of the other sign, would make it NaN.  Where t is
         // infinite too, 0 in B's place (first pass) or beside its infinity (second) would
         // be a NaN: 2^-126 of B's sign stands in the first pass, beside what the
@@ -897,24 +929,33 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
                     constexpr int G = decltype(g)::value;
                     constexpr auto block = [](int e) constexpr { return DRELU ? 2 * e + G : G * MG + e; };
                     u32x4 af[U][MG], bf[U][MJ];
-                    int f0[U], f1[U];
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const int w0 = (s0 + u) * CK, v = w0 + lq * CE, own = v / per, rv = v - own * per;
-                        const bool in = v < all;
-                        f0[u] = w0 / per;
-                        f1[u] = (w0 + CK - 1) / per;
+                    // whether a column of block j has an adapter of sub-step u
+                    auto met = [&](int u, int j) {
+                        return __any(first_q[j] < (s0 + u + 1) * CK && first_q[j] + per > (s0 + u) * CK);
+                    };
+                    // t of sub-step u, from rank rv of its part on, where the row has that adapter
+                    // (small tiles do not ask for blocks without one: 128 requests 120 -> 110
+                    // us; the large ones have no registers for the branches)
+                    auto load_t = [&](int t_part, int u, bool in, int own_first, int rv) {
+                        const int at = ((DRELU ? G * adapt_room(a.parts) : 0) + t_part) * per + rv;
 #pragma unroll
                         for (int j = 0; j < MJ; ++j) {
-                            const char *p = a.t + ((size_t)(q0 + (wq * MJ + j) * 16 + lm) * stride + (DRELU ? G * per : 0) + rv) * SZ;
-                            bf[u][j] = ld_cached(in && slot_q[j] == own ? p : zero);
+                            const char *p = t_rows + (uint32_t)(j * stride + at) * (16 * SZ);
+                            if (MI * MJ > 8 || met(u, j)) bf[u][j] = ld_cached(in && first_q[j] == own_first ? p : zero);
                         }
+                    };
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int v = (s0 + u) * CK + lq * CE, own = slot_of(v), rv = v - own * per;
+                        const bool in = v < all;
+                        load_t(0, u, in, v - rv, rv);
                         if constexpr (!ACOL) {
-                            const int m = __shfl(ad, in ? own : 0), r = rv >= a.rank ? rv - a.rank : rv;  // (parts: the same B)
+                            const int m = __shfl(ad, in ? own : 0);
+                            const char *const pm = a.b[DRELU ? G : 0] + (size_t)m * ((uint32_t)a.n * per * SZ) + rv * SZ;
 #pragma unroll
                             for (int e = 0; e < MG; ++e) {
                                 const int n = min(p0 + (wp * MI + block(e)) / both * 16 + lm, a.n - 1);
-                                const char *p = a.b[DRELU ? G : 0] + (((size_t)m * a.n + n) * a.rank + r) * SZ;
+                                const char *p = pm + (uint32_t)n * (uint32_t)(per * SZ);
                                 af[u][e] = ld_cached(in ? p : zero);
                             }
                         }
@@ -927,9 +968,9 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
                         unroll<U * TW::NJ / 2>([&](auto j) {
                             int row, ch;
                             TW::at(lane + 64 * j, row, ch);
-                            const int v = s0 * CK + row, own = v / per, rv = v - own * per;
-                            const int m = __shfl(ad, v < all ? own : 0), r = rv >= a.rank ? rv - a.rank : rv;
-                            const char *p = a.b[0] + ((size_t)m * a.rank + r) * ((size_t)a.n * SZ) + min(pc + ch * 16, a.n * SZ - 16);
+                            const int v = s0 * CK + row, own = slot_of(v), rv = v - own * per;
+                            const int m = __shfl(ad, v < all ? own : 0);
+                            const char *p = a.b[0] + ((size_t)m * per + rv) * ((size_t)a.n * SZ) + min(pc + ch * 16, a.n * SZ - 16);
                             ld_lds16(v < all ? p : zero, l + 1024 * j);
                         });
                         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -941,15 +982,14 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
                         // (the next round's loads may overwrite them)
                         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                     }
+                    if constexpr (second_pass) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        if constexpr (second_pass) {
+                        for (int u = 0; u < U; ++u) {
 #pragma unroll
                             for (int j = 0; j < MJ; ++j) bf[u][j] = one_for_infinite<KIND>(bf[u][j]);
 #pragma unroll 1
                             for (int h = 0; h < 4; ++h) {
-                                const int v = (s0 + u) * CK + h * CE, own = v / per;
-                                if (v - own * per >= a.rank) continue;
+                                const int own_first = slot_of((s0 + u) * CK + h * CE) * per;
 #pragma unroll
                                 for (int e = 0; e < MG; ++e) {
                                     const u32x4 bad = only_not_finite<KIND>(af[u][e]), one = lq == h ? bad : u32x4{0u, 0u, 0u, 0u};
@@ -958,29 +998,58 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
                                     for (int j = 0; j < MJ; ++j) {
                                         const f32x4 d = mma<KIND>(one, bf[u][j], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-                                        for (int c = 0; c < 4; ++c) acc[block(e)][j][c] += slot_q[j] == own ? d[c] : 0.f;
+                                        for (int c = 0; c < 4; ++c) acc[block(e)][j][c] += first_q[j] == own_first ? d[c] : 0.f;
                                     }
                                 }
                             }
-                            continue;
                         }
-                        if (__any(not_finite<KIND>(af[u]))) {
-                            broken = true;
+                        return;
+                    }
+                    for (int t_part = 0;;) {
 #pragma unroll
-                            for (int e = 0; e < MG; ++e) af[u][e] = tiny_for_not_finite<KIND>(af[u][e]);
+                        for (int u = 0; u < U; ++u) {
+                            if (__any(not_finite<KIND>(af[u]))) {
+                                broken = true;
+#pragma unroll
+                                for (int e = 0; e < MG; ++e) af[u][e] = tiny_for_not_finite<KIND>(af[u][e]);
+                            }
+#pragma unroll
+                            for (int j = 0; j < MJ; ++j)
+                                if (met(u, j))
+#pragma unroll
+                                    for (int e = 0; e < MG; ++e) acc[block(e)][j] = mma<KIND>(af[u][e], bf[u][j], acc[block(e)][j]);
                         }
+                        if (KIND == kGmmF32 || ++t_part == a.parts) break;
+                        if (STAGE && !arrived) {
+                            gmm_barrier<0>();
+                            arrived = true;
+                        }
+                        // (the ranks computed again: kept, they cost the registers of a
+                        // second workgroup a unit)
+                        int again = s0;
+                        asm volatile("" : "+s"(again));
 #pragma unroll
-                        for (int j = 0; j < MJ; ++j)
-                            if (__any(slot_q[j] >= f0[u] && slot_q[j] <= f1[u]))  // a column has a row of these ranks
+                        for (int u = 0; u < U; ++u) {
+                            const int v = (again + u) * CK + lq * CE, own_first = slot_of(v) * per, rv = v - own_first;
+                            if constexpr (!STAGE) {
+                                load_t(t_part, u, v < all, own_first, rv);
+                                continue;
+                            }
 #pragma unroll
-                                for (int e = 0; e < MG; ++e) acc[block(e)][j] = mma<KIND>(af[u][e], bf[u][j], acc[block(e)][j]);
+                            for (int j = 0; j < MJ; ++j) {
+                                const int at = ((wq * MJ + j) * both + (DRELU ? G : 0)) * run + ((t_part - 1) * per + rv) * SZ + lm;
+                                const u32x4 t = s_all[OWN + at];
+                                bf[u][j] = v < all && first_q[j] == own_first ? t : u32x4{0u, 0u, 0u, 0u};
+                            }
+                        }
                     }
                 });
             }
         };
         ranks(std::false_type{});
         if (broken) ranks(std::true_type{});
-        if constexpr (KW > 1 && ACOL) __syncthreads();  // (the sums go where other waves' matrices are)
+        if (STAGE && !arrived) gmm_barrier<0>();
+        if constexpr (KW > 1) __syncthreads();  // (the sums go where other waves' matrices and parts are)
     }
     if constexpr (KW > 1) {
         static_assert((KW - 1) * BP * BQ / 4 <= KW * ALL, "the groups' sums fit the stages");

@@ -63,13 +63,18 @@ constexpr int tiles_per_unit(GmmKind kind, int t) {
 // Of the rows of each wave of the product: the rows' slots (-1: no adapter), the
 // slots' adapters, how many slots.
 struct GmmAdaptArgs : GmmArgs {
-    const char *t = nullptr;  // [rows][gate, up][parts][rank]: scale x A^T
+    // scale x A^T: [rows / 16][gate, up][room of parts][ranks' 16 bytes][16 rows][16 bytes],
+    // the rows from the first segment's on: what a wave loads of a part is 1 KB in a row
+    const char *t = nullptr;
     const int32_t *slots = nullptr, *slot_ad = nullptr, *slot_count = nullptr;
     const char *b[2] = {nullptr, nullptr};
     float *sums = nullptr;    // [split][rows][gate, up][n]
     int segs = 0, rank = 0, parts = 1, split = 1;
     GmmTileId tile = kTile128x64;
 };
+constexpr int kMaxRank = 128;
+// Places that a row's parts of t take (a power of two: its lines begin alike).
+constexpr int adapt_room(int parts) { return parts == 3 ? 4 : parts; }
 // Rows of a wave of each tile.
 constexpr int wave_rows(GmmTileId t) { return t == kTile64x32 || t == kTile32x32 ? 16 : t == kTile64x64 ? 32 : 64; }
 void adapt_tile(GmmKind kind, bool drelu, bool w_kn, int rows, int n, int k, GmmTileId *tile, int *split);

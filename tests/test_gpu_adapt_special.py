@@ -20,8 +20,8 @@ INF, NAN = float("inf"), float("nan")
 N, BAD = 6, 2  # adapters, the broken one
 
 # rows, segments, rank, n, k: a single row, one row a request, a split contraction (its
-# last three), prompts, the large tiles
-SHAPES = [(1, 1, 16, 264, 136), (40, 40, 16, 264, 136), (300, 7, 64, 264, 136), (2500, 40, 24, 1552, 136),
+# last three), prompts, the large tiles (the last with more of t than LDS holds)
+SHAPES = [(1, 1, 16, 264, 136), (40, 40, 16, 264, 136), (300, 7, 64, 264, 136), (2500, 40, 24, 1552, 136), (3000, 33, 128, 4112, 136),
           (1, 1, 8, 144, 4104), (33, 5, 24, 144, 4104), (300, 300, 40, 144, 4104)]
 
 
@@ -165,3 +165,31 @@ def test_every_step_counts_once(rows, n, k, dtype):
             assert torch.equal(ts.adapter_mm(x, *m, *o, scale=dev(scale), w_kn=kn, out_dtype=F32).double(), ys[0]), (S, kn)
         got = ts.adapter_drelu(x, w, v, a, b, c, d, *o, scale=dev(scale), out_dtype=F32)
         assert torch.equal(got, gref.drelu(*[y.float() for y in ys])), S
+
+
+@pytest.mark.parametrize("odt", [BF16, F32])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,S,rank,n,k", SHAPES)
+def test_the_ranks_values_keep_their_bits(rows, S, rank, n, k, dtype, odt):
+    """t of 16 bits (bf16 output; differences of two that leave 8) and of 22 (fp32
+    output): what the output can hold of them is exact."""
+    g = torch.Generator().manual_seed(7 + rows + k)
+    off, ad = ref.segments(rows, S, N, g)
+    scale = torch.exp2(torch.randint(-1, 3, (N,), generator=g).float())
+    top = 15 if odt == BF16 else 120
+    x = whole(g, rows, k, top=top)
+    mats, r = [], torch.arange(rank)
+    for _ in range(2):
+        a = whole(g, N, 1, k, top=top, keep=min(1.0, 136 / k)).repeat(1, rank, 1)
+        a[:, r, r] += r % 4 + 1.0  # ranks differ in one place each
+        b = torch.zeros(N, rank, n)
+        j = torch.arange(n)
+        b[:, j % rank, j] = 1
+        if odt == BF16:
+            b[:, (j + 1) % rank, j] = -1
+        mats.append((torch.zeros(n, k), a, b))
+        t = (x @ a.view(-1, k).t()).abs()
+        assert float(t.max()) < (1 << 16 if odt == BF16 else 1 << 22)
+        assert rows == 1 or float(t.max()) > (1 << 11 if odt == BF16 else 1 << 17)
+    compare(x, mats[:1], off, ad, scale, dtype, odt)
+    compare(x, mats, off, ad, scale, dtype, odt)
