@@ -143,13 +143,16 @@ __device__ __forceinline__ void store_t(const AdaptRowsArgs &a, int row, int r, 
         float v[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = x[i];
-        // each part is what the ones before left (nothing of what has no remainder)
+        // each part is what the ones before left (nothing of what has no remainder; of a value
+        // that would round to infinity the first is the largest finite one)
+        constexpr float most = 0x1.FEp127f;
         for (int p = 0; p < a.parts; ++p, at += 16 * a.rank) {
             b16xn hi;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                hi[i] = (__bf16)v[i];
-                v[i] = fabsf((float)hi[i]) < INFINITY ? v[i] - (float)hi[i] : 0.f;
+                const bool finite = fabsf(v[i]) < INFINITY;
+                hi[i] = (__bf16)(finite ? fminf(fmaxf(v[i], -most), most) : v[i]);
+                v[i] = finite ? v[i] - (float)hi[i] : 0.f;
             }
             *reinterpret_cast<b16xn *>(reinterpret_cast<__bf16 *>(a.t) + at) = hi;
         }

@@ -193,3 +193,19 @@ def test_the_ranks_values_keep_their_bits(rows, S, rank, n, k, dtype, odt):
         assert rows == 1 or float(t.max()) > (1 << 11 if odt == BF16 else 1 << 17)
     compare(x, mats[:1], off, ad, scale, dtype, odt)
     compare(x, mats, off, ad, scale, dtype, odt)
+
+
+@pytest.mark.parametrize("dtype,odt", [(BF16, BF16), (BF16, F32), (F32, F32), (F32, BF16)])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_finite_t_above_the_largest_bf16(rows, dtype, odt):
+    """t between the largest finite values of bf16 and of fp32 stays finite."""
+    n, k, rank = 144, 136, 16
+    x, mats, off, ad, _ = inputs(rows, rows, rank, n, k, 1, 5)
+    w, a, b = (torch.zeros_like(t) for t in mats[0])
+    x[:, 0], x[:, 1] = 255 * 2.0 ** 120, 2.0 ** 119 * (1 + 2.0 ** -7)
+    ad[:] = BAD
+    a[BAD, 3, :2], a[BAD, 7, :2] = 1, -1  # t = +-(2^128 - 2^119 + 2^112)
+    b[BAD, 3, ::2], b[BAD, 7, 1::2] = 2.0 ** -20, 2.0 ** -2
+    assert float(torch.tensor(float(x[0, 0]) + float(x[0, 1])).bfloat16()) == INF
+    want = compare(x, [(w, a, b)], off, ad, torch.ones(N), dtype, odt)
+    assert bool(torch.isfinite(want).all()) and bool((want.abs() > 2.0 ** 107).all())
