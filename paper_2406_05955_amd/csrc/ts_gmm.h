@@ -865,8 +865,9 @@ __global__ __launch_bounds__(64 * WP * WQ * KW) void gmm_tiled(typename GmmArgsO
         // registers, several steps' together: no other wave's loads are waited for, and a
         // wave takes what its own rows need.  (Through LDS with all of the workgroup, two
         // stages: 8 rounds of loads for 32 requests of rank 16, and for prompts
-        // each wave takes the steps of its neighbours' adapters too: gate + up 58 us, 6001
-        // rows 1390 to 1420; this 50 and 1120 to 1150, without adapters 44 and 1070.)
+        // each wave takes the steps of its neighbours' adapters too: with t in one part gate
+        // + up 58 us, 6001 rows of rank 64 1390 to 1420, this 50 and 1120 to 1150.  As it is,
+        // t in two parts, 51 and 1280; one adapter for all rows 48 and 1125, none 43 and 1060.)
         // A wave's blocks of P in groups (gate's and up's; eight in two halves), a group's
         // operands of U steps at a time: whole lines of 64 ranks where U is even (gate
         // and up together, 64 bytes of each line at a time: 6001 rows of rank 64 1145 us).
