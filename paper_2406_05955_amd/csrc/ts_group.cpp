@@ -126,9 +126,9 @@ GmmTileId pick_tile(GmmKind kind, bool drelu, int groups, int rows, int n, int k
 // sum: with few rows both count.  Rows of [k][n] that a tile cuts below 128 bytes
 // are fetched twice.  The constants are those of the least mean over 131 sizes (both
 // layouts and dReLU, 1 to 6000 rows, 512 x 1792 to 4096 x 14336) timed at every tile and
-// split: 2% above each size's best, 23% at most.  Us, one workgroup a tile / this:
-// [k][n] 4096 x 14336 1 row 35 / 25, 64 rows 53 / 35, 300 rows 103 / 58; [n][k] 2048 x
-// 8192 32 rows 23 / 16; fp32 512 x 1792 1 row 14 / 11.
+// split: 2% above each size's best, 23% at most (116 sizes with t in its parts: 2%,
+// 24%).  Us, one workgroup a tile / this: [k][n] 4096 x 14336 1 row 35 / 25, 64 rows 54 /
+// 33, 300 rows 100 / 57; [n][k] 2048 x 8192 32 rows 23 / 16; fp32 512 x 1792 1 row 13 / 11.
 void adapt_tile(GmmKind kind, bool drelu, bool w_kn, int rows, int n, int k, GmmTileId *tile, int *split) {
     const int esz = kind == kGmmF32 ? 4 : 2, both = drelu ? 2 : 1;
     const double bytes = (double)n * k * esz * both / 2600;
