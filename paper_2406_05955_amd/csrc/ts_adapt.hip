@@ -407,12 +407,13 @@ ts_status run_rows(AdaptRowsArgs r, hipStream_t st) {
 // every 16 ranks and a rank's A once for every 16 rows; 32 x 64 and 64 x 64 read less
 // and leave units idle, or lanes where there are fewer ranks or shorter segments.  us,
 // 16 x 16 / 32 x 64 / 64 x 64: bf16, k 4096, 40 segments: 2048 rows x 16 ranks 12 / 18
-// / 22, 8192 x 16 27 / 29 / 26; 1024 x 64 19 / 23 / 27, 2048 x 64 28 / 25 / 30 (2^17), 6001
-// x 64 61 / 25 / 33, 8192 x 64 77 / 47 / 33 (2^19), 16384 x 256 547 / 218 / 189; in 750
-// segments of 8 rows 6001 x 32 55 / 44 / 53, x 256 390 / 218 / 271, in 2048 of one row
-// 2048 x 64 146 / 135 / 177, and of k 14336 370 / 517 / 531.  fp32, whose matrix instructions take eight times as long: 2048 x 64 55 / 56 /
-// 104, 6001 x 128 213 / 120 / 200, 16384 x 256 1024 / 529 / 556.  Over 1400 calls (512
-// to 40000 rows, 1 segment to one a row, 8 to 256 ranks) 4% above each one's best.
+// / 22, 8192 x 16 27 / 29 / 26; 1024 x 64 19 / 23 / 27, 2048 x 64 (2^17) 28 / 25 / 30,
+// 6001 x 64 61 / 25 / 33, 8192 x 64 (2^19) 77 / 47 / 33, 16384 x 256 547 / 218 / 189; in
+// 750 segments of 8 rows 6001 x 32 55 / 44 / 53, x 256 390 / 218 / 271, in 2048 of one
+// row 2048 x 64 146 / 135 / 177, and of k 14336 370 / 517 / 531.  fp32, whose matrix
+// instructions take eight times as long: 2048 x 64 55 / 56 / 104, 6001 x 128 213 / 120 /
+// 200, 16384 x 256 1024 / 529 / 556.  Over 1400 calls (512 to 40000 rows, 1 segment to
+// one a row, 8 to 256 ranks) 4% above each one's best.
 template <GmmKind KIND>
 ts_status run_ranks(const AdaptRowsArgs &r, hipStream_t st) {
     const long long each = (long long)r.rows * r.ranks;

@@ -3,6 +3,9 @@ result is the definition's, signs included, and other requests' rows keep theirs
 All finite values are small whole numbers (times powers of two), so that every sum is
 exact in any order, a step that is left out or taken twice shows, and results are
 compared for equality."""
+import math
+import random
+
 import pytest
 import torch
 
@@ -209,3 +212,21 @@ def test_finite_t_above_the_largest_bf16(rows, dtype, odt):
     assert float(torch.tensor(float(x[0, 0]) + float(x[0, 1])).bfloat16()) == INF
     want = compare(x, [(w, a, b)], off, ad, torch.ones(N), dtype, odt)
     assert bool(torch.isfinite(want).all()) and bool((want.abs() > 2.0 ** 107).all())
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_random_shapes(seed):
+    """Sizes over their ranges, types, layouts and broken values as they come."""
+    rng = random.Random(seed)
+    log = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))  # noqa: E731
+    for i in range(12):
+        dtype, odt, q = *rng.choice([(BF16, BF16), (BF16, F32), (F32, F32), (F32, BF16)]), 8
+        rows, rank, n, k = log(1, 3000), log(8, 128) // q * q, log(8, 4200) // q * q, log(8, 6000) // q * q
+        S, products, what = rng.choice([min(rows, log(1, 300)), log(1, 100)]), rng.choice([1, 2]), rng.choice(["", "b", "t"])
+        x, mats, off, ad, scale = inputs(rows, S, rank, n, k, products, 100 + 12 * seed + i)
+        if what == "t":
+            x[:, 5] = torch.where(torch.arange(rows) % 2 == 0, 1.0, -1.0)
+            mats[0][1][BAD, 1, 5] = -INF
+        if what:
+            break_b(mats[-1][2][BAD])
+        compare(x, mats, off, ad, scale, dtype, odt)
